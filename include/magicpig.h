@@ -269,6 +269,95 @@ MAGICPIG_API int magicpig_sampled_attention_tables(const magicpig_params* params
                                       int32_t* dbg_cand, int32_t* dbg_ncand, int64_t dbg_cand_cap,
                                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- paged cache and exact attention -----------------------------------------------------------
+ * What a server needs next to the sampled step: the layers that keep exact attention, prompts, and
+ * requests of different lengths.  The keys and values of all requests of a layer live in one pool of
+ * pages each, [n_pages] pages of page_size keys, [n_kv_heads] rows of 128 elements per key, addressed
+ * through element strides (page, key, head).  A request's cache is a row of the block table
+ * [batch, max_pages] int32: entry j is the page that holds its keys [j page_size, (j + 1) page_size).
+ * A slot, page * page_size + offset, names one key's place in the pool.
+ *
+ * magicpig_page_plan hands out pages and makes the slot map of a step, magicpig_page_append stores the
+ * step's keys and values in their slots, magicpig_paged_attention attends the step's tokens.  All
+ * three read what varies from step to step (lengths, token counts, tables) from device memory when
+ * their kernels run: one captured graph serves every step; the parameters are bounds.  Two calls that
+ * share a workspace or an output must be ordered.  Pool rows that no slot names are left as they are.
+ * Table entries and slots are checked by the kernels: one outside the pool is never followed. */
+typedef struct magicpig_paged_params {
+  int32_t batch;        /* requests (rows of the block table), 0 .. 65536                        */
+  int32_t n_q_heads, n_kv_heads;   /* query head h uses KV head h / (n_q_heads / n_kv_heads); up to
+                           64 query heads per KV head, 1024 KV heads                             */
+  int32_t head_dim;     /* must be 128 */
+  int32_t dtype;        /* MAGICPIG_BF16 | MAGICPIG_FP32: q, new keys and values, out            */
+  int32_t kv_dtype;     /* MAGICPIG_KV_SAME | MAGICPIG_KV_FP8_E4M3 (needs dtype BF16): the pools */
+  int32_t page_size;    /* keys per page: 16, 32, 64, .. 1024 (a power of two)                   */
+  int32_t max_pages;    /* entries in a row of the block table; max_pages * page_size <= 2^30    */
+  int32_t max_new;      /* new tokens of one request at most, 1 .. 2^24                          */
+  int32_t n_sink, n_local;   /* n_local 0: a token attends every key up to its own.  Otherwise the
+                           first n_sink keys and the n_local up to its own.  Each 0 .. 2^30      */
+  float scale;          /* of the logits q.k; 0 stands for 1/sqrt(128)                           */
+  int64_t n_pages;      /* pages in the pools, 1 .. 2^31 - 1                                     */
+  int64_t max_tokens;   /* rows of the token arrays (q, out, lse, new keys and values, slots),
+                           1 .. 2^24: the new tokens of all requests at most                     */
+  /* element strides, multiples of 8 (of the pools: of 16 when they hold e4m3), innermost dimension
+   * contiguous; a pool's key stride * page_size stays below 2^31 bytes */
+  int64_t k_stride_page, k_stride_key, k_stride_head;     /* pools */
+  int64_t v_stride_page, v_stride_key, v_stride_head;
+  int64_t q_stride_token, q_stride_head;                  /* q [max_tokens, n_q_heads, 128] */
+  int64_t k_new_stride_token, k_new_stride_head;          /* new keys [max_tokens, n_kv_heads, 128] */
+  int64_t v_new_stride_token, v_new_stride_head;          /* new values, alike */
+} magicpig_paged_params;
+
+/* Scratch that is enough for any of the three calls with these params (0 on invalid params); 256-byte
+ * aligned, its contents need not be initialised or preserved between calls. */
+MAGICPIG_API size_t magicpig_paged_workspace_bytes(const magicpig_paged_params* params);
+
+/* One step's bookkeeping.  new_tokens [batch] int32: n >= 0, the request gets n tokens behind its
+ * lengths[b] cached ones; -1, it has ended and its ceil(lengths[b] / page_size) pages come back.
+ * free_pages [n_pages] int32 is a stack of free pages, n_free its height.  The ended requests' pages
+ * are laid on it (requests in order, pages in order); then the requests that need pages take them
+ * off its top, in order.  Out:
+ *   lengths_out [batch] int32   lengths[b] + n, or 0 of an ended request  (may be `lengths`)
+ *   n_free_out  [1] int32       the stack's height afterwards              (may be `n_free`)
+ *   block_table                 new entries written, others left as they are (ended requests' too)
+ *   free_pages                  entries that the ended requests left on the stack written
+ *   token_start [batch + 1] int32   row of each request's first token in the token arrays, then all
+ *   slots [max_tokens] int64    the tokens' slots, and -1 in the rows behind the last token
+ *   status [1] int32            0; > 0: so many pages are missing; -1: an argument does not fit
+ *                               (a token count below -1 or above max_new, a length below 0 or beyond
+ *                               the table's row, more than max_tokens tokens, a stack beyond n_pages)
+ * With a status other than 0 nothing is handed out or taken back: lengths_out = lengths, n_free_out =
+ * n_free, token_start 0, slots -1, table and stack untouched.  Page ids are passed on as they are. */
+MAGICPIG_API int magicpig_page_plan(const magicpig_paged_params* params, const int32_t* new_tokens, const int32_t* lengths,
+                                    int32_t* block_table, int32_t* free_pages, const int32_t* n_free, int32_t* lengths_out,
+                                    int32_t* n_free_out, int32_t* token_start, int64_t* slots, int32_t* status,
+                                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Stores rows k_new[t], v_new[t] in slot slots[t] of the pools, every t < max_tokens whose slot lies in
+ * [0, n_pages * page_size).  e4m3 pools: the byte stored is x / scale of the KV head (k_scale, v_scale
+ * [n_kv_heads] float32, NULL: 1), clamped to +-448 and rounded to nearest, ties to even; a NaN stays one.
+ * Other pools take no scales (NULL).  Where two rows name one slot it holds a mixture of them. */
+MAGICPIG_API int magicpig_page_append(const magicpig_paged_params* params, const void* k_new, const void* v_new,
+                                      const int64_t* slots, const float* k_scale, const float* v_scale, void* k_pages,
+                                      void* v_pages, void* hip_stream);
+
+/* Exact attention of the step's tokens.  Request b has lengths[b] keys, the new ones among them, and its
+ * n_b = token_start[b + 1] - token_start[b] new tokens are rows token_start[b] .. of q; token i of them
+ * stands at position lengths[b] - n_b + i.  token_start NULL: one token per request, row b.  For the
+ * row of a token at position p and query head h with KV head g,
+ *   A = { i <= p : n_local == 0 or i < n_sink or i > p - n_local },
+ *   out = sum_A w_i v_i,  w = softmax_A(scale q.k_i),  lse = log sum_A exp(scale q.k_i),
+ * where e4m3 keys and values stand for byte * k_scale[g], byte * v_scale[g] (NULL: 1).  A row whose A is
+ * empty, or whose logits are all -inf, gives zeros and lse -inf.  What lies in keys outside A, NaN and infinities included, does not reach
+ * the row; keys of a page whose table entry lies outside [0, n_pages) count as outside A.  Lengths are clamped to [0, max_pages *
+ * page_size], token counts to [0, max_new], rows to [0, max_tokens).  out [max_tokens, n_q_heads, 128] of
+ * `dtype`; lse [max_tokens, n_q_heads] float32 or NULL (two attentions over disjoint keys are joined by
+ * it); rows that are no request's token are left as they are. */
+MAGICPIG_API int magicpig_paged_attention(const magicpig_paged_params* params, const void* q, const void* k_pages,
+                                          const void* v_pages, const float* k_scale, const float* v_scale,
+                                          const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,
+                                          void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Profiling aid, and the only setting the library keeps: a per-thread (thread_local) list of
  * events, empty unless this function was called on the calling host thread; production callers
  * never call it and pay one thread-local test per call.  When `events` is non-NULL it points to

@@ -39,6 +39,21 @@ class magicpig_params(ctypes.Structure):
     ]
 
 
+class magicpig_paged_params(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_new", ctypes.c_int32),
+        ("n_sink", ctypes.c_int32), ("n_local", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("n_pages", ctypes.c_int64), ("max_tokens", ctypes.c_int64),
+        ("k_stride_page", ctypes.c_int64), ("k_stride_key", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+        ("v_stride_page", ctypes.c_int64), ("v_stride_key", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+        ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+        ("k_new_stride_token", ctypes.c_int64), ("k_new_stride_head", ctypes.c_int64),
+        ("v_new_stride_token", ctypes.c_int64), ("v_new_stride_head", ctypes.c_int64),
+    ]
+
+
 EXPORTS = (
     "magicpig_code_words_per_key", "magicpig_code_words_per_query", "magicpig_key_code_bytes",
     "magicpig_query_code_bytes",
@@ -50,6 +65,7 @@ EXPORTS = (
     "magicpig_sampled_attention_noalloc",
     "magicpig_prepared_projector_bytes", "magicpig_prepare_projector", "magicpig_centering_bytes",
     "magicpig_prepare_centering", "magicpig_hash_query_prepared", "magicpig_hash_decode_step_prepared",
+    "magicpig_paged_workspace_bytes", "magicpig_page_plan", "magicpig_page_append", "magicpig_paged_attention",
 )
 
 _lib = None
@@ -96,6 +112,14 @@ def lib() -> ctypes.CDLL:
     L.magicpig_build_tables.argtypes = [P, vp, vp, vp, sz, vp]
     L.magicpig_sampled_attention_tables.restype = ctypes.c_int
     L.magicpig_sampled_attention_tables.argtypes = [P, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+    PP = ctypes.POINTER(magicpig_paged_params)
+    L.magicpig_paged_workspace_bytes.restype, L.magicpig_paged_workspace_bytes.argtypes = sz, [PP]
+    L.magicpig_page_plan.restype = ctypes.c_int
+    L.magicpig_page_plan.argtypes = [PP] + [vp] * 11 + [sz, vp]
+    L.magicpig_page_append.restype = ctypes.c_int
+    L.magicpig_page_append.argtypes = [PP] + [vp] * 8
+    L.magicpig_paged_attention.restype = ctypes.c_int
+    L.magicpig_paged_attention.argtypes = [PP] + [vp] * 11 + [sz, vp]
     L.magicpig_status_string.restype, L.magicpig_status_string.argtypes = ctypes.c_char_p, [ctypes.c_int]
     L.magicpig_last_hip_error.restype, L.magicpig_last_hip_error.argtypes = ctypes.c_char_p, []
     L.magicpig_profile_stage_events.restype = None
@@ -271,6 +295,131 @@ def magicpig_profile_stage_events(events) -> None:
         lib().magicpig_profile_stage_events(arr)
 
 
+# ---- paged cache -----------------------------------------------------------------------------
+def make_paged_params(*, batch, n_q_heads, n_kv_heads, dtype, page_size, max_pages, n_pages, max_tokens=None, max_new=1,
+                      kv_dtype=0, n_sink=0, n_local=0, scale=0.0, head_dim=128, k_strides=None, v_strides=None,
+                      q_strides=None, k_new_strides=None, v_new_strides=None) -> magicpig_paged_params:
+    """Parameter block of the paged calls.  Element strides default to contiguous pools
+    [n_pages, page_size, n_kv_heads, 128] and contiguous token arrays [max_tokens, heads, 128]; pool strides
+    are (page, key, head), those of token arrays (token, head).  max_tokens defaults to batch."""
+    kv_dtype = {"fp8": MAGICPIG_KV_FP8_E4M3, "": 0, None: 0}.get(kv_dtype, kv_dtype)
+    code = {"bf16": MAGICPIG_BF16, "fp32": MAGICPIG_FP32, torch.bfloat16: MAGICPIG_BF16,
+            torch.float32: MAGICPIG_FP32}.get(dtype, dtype)
+    row = n_kv_heads * head_dim
+    pool, new = (page_size * row, row, head_dim), (row, head_dim)
+    either = lambda given, default: default if given is None else tuple(given)
+    return magicpig_paged_params(batch, n_q_heads, n_kv_heads, head_dim, code, kv_dtype, page_size, max_pages, max_new,
+                                 n_sink, n_local, scale, n_pages, max(batch, 1) if max_tokens is None else max_tokens,
+                                 *either(k_strides, pool), *either(v_strides, pool),
+                                 *either(q_strides, (n_q_heads * head_dim, head_dim)),
+                                 *either(k_new_strides, new), *either(v_new_strides, new))
+
+
+_DTYPES = {MAGICPIG_BF16: torch.bfloat16, MAGICPIG_FP32: torch.float32}
+
+
+def _extent(n, *strides_and_sizes) -> int:
+    """Elements from the first to the last of an array of rows of n elements with these (stride, size) dimensions."""
+    return n + sum(stride * (size - 1) for stride, size in strides_and_sizes)
+
+
+def _expect(name, t, dtype, elements, device, optional=False, dense=True):
+    """dense: the call reads the tensor as one run of elements; otherwise by the strides of the parameters."""
+    if t is None:
+        if optional:
+            return
+        raise MagicpigError(f"{name} is missing")
+    if t.get_device() != device:
+        raise MagicpigError(f"{name} is on device {t.device}, the call runs on cuda:{device}")
+    if t.dtype is not dtype and t.dtype not in (dtype if isinstance(dtype, tuple) else ()):
+        raise MagicpigError(f"{name} has dtype {t.dtype}, not {dtype}")
+    if dense:
+        if not t.is_contiguous():
+            raise MagicpigError(f"{name} is not contiguous")
+        if t.numel() < elements:
+            raise MagicpigError(f"{name} has {t.numel()} elements, the parameters say {elements}")
+    elif t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < elements:
+        raise MagicpigError(f"{name} ends before the {elements} elements that the parameters' strides reach")
+
+
+def _device(t) -> int:
+    device = t.get_device() if t is not None else -1
+    if device < 0:
+        raise MagicpigError("the paged calls take tensors on a GPU")
+    return device
+
+
+def _pool_dtype(p):
+    return (torch.float8_e4m3fn, torch.uint8) if p.kv_dtype == MAGICPIG_KV_FP8_E4M3 else _DTYPES.get(p.dtype)
+
+
+def _pool_elements(p, page, key, head) -> int:
+    return _extent(p.head_dim, (page, p.n_pages), (key, p.page_size), (head, p.n_kv_heads))
+
+
+def _on_device(device, workspace, call):
+    """Runs call(stream) with the tensors' device current, on its current stream."""
+    if workspace is not None and workspace.get_device() != device:
+        raise MagicpigError(f"the workspace is on device {workspace.device}, the call runs on cuda:{device}")
+    if device == torch.cuda.current_device():
+        _check(call(torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(torch.cuda.current_stream(device).cuda_stream))
+
+
+def magicpig_paged_workspace_bytes(params) -> int:
+    return lib().magicpig_paged_workspace_bytes(ctypes.byref(params))
+
+
+def magicpig_page_plan(params, new_tokens, lengths, block_table, free_pages, n_free, lengths_out, n_free_out, token_start,
+                       slots, status, workspace=None) -> None:
+    p, device, i32 = params, _device(lengths), torch.int32
+    for name, t, dtype, n in (("new_tokens", new_tokens, i32, p.batch), ("lengths", lengths, i32, p.batch),
+                              ("block_table", block_table, i32, p.batch * p.max_pages), ("free_pages", free_pages, i32, p.n_pages),
+                              ("n_free", n_free, i32, 1), ("lengths_out", lengths_out, i32, p.batch),
+                              ("n_free_out", n_free_out, i32, 1), ("token_start", token_start, i32, p.batch + 1),
+                              ("slots", slots, torch.int64, p.max_tokens), ("status", status, i32, 1)):
+        _expect(name, t, dtype, n, device)
+    _on_device(device, workspace, lambda stream: lib().magicpig_page_plan(
+        ctypes.byref(p), new_tokens.data_ptr(), lengths.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+        n_free.data_ptr(), lengths_out.data_ptr(), n_free_out.data_ptr(), token_start.data_ptr(), slots.data_ptr(),
+        status.data_ptr(), _ptr(workspace), _nbytes(workspace), stream))
+
+
+def magicpig_page_append(params, k_new, v_new, slots, k_scale, v_scale, k_pages, v_pages) -> None:
+    p, device, at = params, _device(k_pages), _DTYPES.get(params.dtype)
+    _expect("k_new", k_new, at, _extent(p.head_dim, (p.k_new_stride_token, p.max_tokens), (p.k_new_stride_head, p.n_kv_heads)), device, dense=False)
+    _expect("v_new", v_new, at, _extent(p.head_dim, (p.v_new_stride_token, p.max_tokens), (p.v_new_stride_head, p.n_kv_heads)), device, dense=False)
+    _expect("slots", slots, torch.int64, p.max_tokens, device)
+    _expect("k_scale", k_scale, torch.float32, p.n_kv_heads, device, optional=True)
+    _expect("v_scale", v_scale, torch.float32, p.n_kv_heads, device, optional=True)
+    _expect("k_pages", k_pages, _pool_dtype(p), _pool_elements(p, p.k_stride_page, p.k_stride_key, p.k_stride_head), device, dense=False)
+    _expect("v_pages", v_pages, _pool_dtype(p), _pool_elements(p, p.v_stride_page, p.v_stride_key, p.v_stride_head), device, dense=False)
+    _on_device(device, None, lambda stream: lib().magicpig_page_append(
+        ctypes.byref(p), k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), _ptr(k_scale), _ptr(v_scale),
+        k_pages.data_ptr(), v_pages.data_ptr(), stream))
+
+
+def magicpig_paged_attention(params, q, k_pages, v_pages, k_scale, v_scale, block_table, lengths, token_start, out, lse=None,
+                             workspace=None) -> None:
+    p, device, at = params, _device(q), _DTYPES.get(params.dtype)
+    _expect("q", q, at, _extent(p.head_dim, (p.q_stride_token, p.max_tokens), (p.q_stride_head, p.n_q_heads)), device, dense=False)
+    _expect("k_pages", k_pages, _pool_dtype(p), _pool_elements(p, p.k_stride_page, p.k_stride_key, p.k_stride_head), device, dense=False)
+    _expect("v_pages", v_pages, _pool_dtype(p), _pool_elements(p, p.v_stride_page, p.v_stride_key, p.v_stride_head), device, dense=False)
+    _expect("k_scale", k_scale, torch.float32, p.n_kv_heads, device, optional=True)
+    _expect("v_scale", v_scale, torch.float32, p.n_kv_heads, device, optional=True)
+    _expect("block_table", block_table, torch.int32, p.batch * p.max_pages, device)
+    _expect("lengths", lengths, torch.int32, p.batch, device)
+    _expect("token_start", token_start, torch.int32, p.batch + 1, device, optional=True)
+    _expect("out", out, at, p.max_tokens * p.n_q_heads * p.head_dim, device)
+    _expect("lse", lse, torch.float32, p.max_tokens * p.n_q_heads, device, optional=True)
+    _on_device(device, workspace, lambda stream: lib().magicpig_paged_attention(
+        ctypes.byref(p), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale), _ptr(v_scale),
+        block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start), out.data_ptr(), _ptr(lse), _ptr(workspace),
+        _nbytes(workspace), stream))
+
+
 # ---- buffer helpers (allocation and layout only) ---------------------------------------------
 def alloc_key_codes(params, device="cuda") -> torch.Tensor:
     return torch.zeros(max(magicpig_key_code_bytes(params) // 4, 4), dtype=torch.int32, device=device)
@@ -305,6 +454,10 @@ def alloc_centering(params, device="cuda") -> torch.Tensor:
 
 def alloc_workspace(params, device="cuda") -> torch.Tensor:
     return torch.empty(max(magicpig_workspace_bytes(params), 256), dtype=torch.uint8, device=device)
+
+
+def alloc_paged_workspace(params, device="cuda") -> torch.Tensor:
+    return torch.empty(max(magicpig_paged_workspace_bytes(params), 256), dtype=torch.uint8, device=device)
 
 
 def key_code_gather_index(params) -> np.ndarray:

@@ -82,4 +82,58 @@ inline int hash_f32_keys(int K, int64_t groups32, int64_t groups64) {
   return K >= 5 && 7 * fullest(groups64) < 4 * fullest(groups32) ? 64 : 32;
 }
 
+// Whether one workgroup does a step's page plan (its prefix sums lie in LDS, its slots are filled in by 1024 threads) or
+// two launches do.
+constexpr int kPlanInOneRequests = 2048, kPlanInOneTokens = 8192;
+inline bool page_plan_in_one(int batch, int64_t max_tokens) { return batch <= kPlanInOneRequests && max_tokens <= kPlanInOneTokens; }
+
+// ---- paged attention ------------------------------------------------------------------------------
+// rows: query rows (new tokens times the query heads of a KV head) that a workgroup takes at once; key_tile:
+// keys by which the work is counted.  tile_tokens, head_blocks: see PagedArgs.  items, pieces, units, slots: at most so many row
+// tiles of all KV heads, workgroups, row tiles that are cut, partials.
+struct PagedForm {
+  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles;
+  int64_t items, pieces, units, slots;
+};
+
+constexpr int kPagedTarget = 3 * kNumCU;     // pieces that the work is cut into (three workgroups per compute unit)
+constexpr int kPagedMinKeys = 256;           // of a piece
+
+// Row tiles of all KV heads and requests, whatever token counts (each at most max_new) the device memory holds.
+inline int64_t paged_most_items(int batch, int kv_heads, int group, bool fp32, int max_new) {
+  const int rows = !fp32 && (int64_t)max_new * group > 16 ? 32 : 16;
+  const int64_t tokens = group <= rows ? rows / group : 1, blocks = group <= rows ? 1 : (group + rows - 1) / rows;
+  return (int64_t)batch * ((max_new + tokens - 1) / tokens) * blocks * kv_heads;
+}
+
+// group: query heads per KV head.  starts: the requests' token counts differ (else one token each).
+inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64_t max_tokens, int max_new, bool starts, int64_t max_len,
+                            int n_sink, int n_local) {
+  PagedForm f{};
+  const int64_t rows = (int64_t)max_new * group;
+  f.rows = !fp32 && rows > 16 ? 32 : 16;
+  f.key_tile = fp32 ? 16 : 32;
+  f.tile_tokens = group <= f.rows ? f.rows / group : 1;
+  f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
+  f.target = kPagedTarget;
+  f.min_tiles = kPagedMinKeys / f.key_tile;
+  int64_t tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens);
+  if (starts && max_tokens / f.tile_tokens + batch < tiles) tiles = max_tokens / f.tile_tokens + batch;
+  f.items = tiles * f.head_blocks * kv_heads;
+  int64_t charge = (max_len + f.key_tile - 1) / f.key_tile;
+  if (n_local > 0) {
+    const int64_t w = (n_sink + f.key_tile - 1) / f.key_tile + (n_local + f.tile_tokens - 2) / f.key_tile + 2;
+    charge = charge < w ? charge : w;
+  }
+  const int64_t most = (charge + f.min_tiles - 1) / f.min_tiles;
+  f.pieces = f.items;
+  if (most > 1) {
+    const int64_t cut = 2 * f.target + 64;
+    f.pieces = f.items * most < f.items + cut ? f.items * most : f.items + cut;
+    f.slots = f.items * most < cut ? f.items * most : cut;
+    f.units = f.items < f.target ? f.items : f.target;
+  }
+  return f;
+}
+
 }  // namespace mp

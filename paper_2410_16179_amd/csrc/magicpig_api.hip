@@ -356,6 +356,8 @@ int run_attention_impl(const magicpig_params* p, const void* q, const void* K_ca
 
 }  // namespace
 
+int mp::hip_status(hipError_t e) { return e == hipSuccess ? MAGICPIG_OK : fail_hip(e); }
+
 extern "C" {
 
 size_t magicpig_code_words_per_key(const magicpig_params* p) {

@@ -263,6 +263,9 @@ constexpr int kFusedIters = 8;             // its gather batch: rows per quarter
 constexpr int words_of(int L) { return (L + 31) / 32; }
 constexpr int tail_of(int L) { return L - 32 * (words_of(L) - 1); }
 
+// MAGICPIG_OK, or MAGICPIG_LAUNCH_FAILED with the error's text kept for magicpig_last_hip_error()
+int hip_status(hipError_t e);
+
 // host-side launchers (defined next to their kernels)
 hipError_t launch_finish_hash_keys(const HashMfmaArgs& m, const HashDirectArgs& a, hipStream_t s);
 hipError_t launch_hash_rows(const HashDirectArgs& a, const HashDirectArgs* b, hipStream_t s, hipEvent_t start = nullptr, hipEvent_t stop = nullptr);

@@ -1,0 +1,593 @@
+// Exact attention over a paged key-value cache: the form for few rows per KV head, and the joining of pieces.
+#include "paged_common.h"
+
+#include <type_traits>
+
+namespace mp {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef const int __attribute__((address_space(4))) * const_i32_ptr;
+
+constexpr int kPartialRow = kPartialStride;   // floats of a row's partial: 128 outputs, maximum, sum, pad
+
+// Eight e4m3 bytes as eight bf16 (exact), two per instruction.
+__device__ inline u32x4 e4m3_to_bf16(u32x2 w) {
+  u32x4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, true));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, false));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, true));
+  return r;
+}
+
+__device__ inline uint32_t pack_bf16(float lo, float hi) {
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Loads through a buffer descriptor, not kept in the caches (nt): a step reads a row once.
+constexpr int kBufferWord3 = 0x00020000;
+constexpr int kNonTemporal = 2;
+__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
+  to = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, kNonTemporal));
+}
+__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
+  to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, kNonTemporal));
+}
+
+// Clears the infinities and NaN among a lane's V elements (float32, or two bf16 a register).
+template <bool F32>
+__device__ inline void clear_not_finite(u32x4 (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w = v[i][e];
+      if constexpr (F32) v[i][e] = (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+      else v[i][e] = ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+    }
+}
+
+// ---- few rows ------------------------------------------------------------------------------------
+// A wavefront attends tiles of KT keys with up to 16 NR query rows.  Scores are formed transposed,
+// S^T = K Q^T: MFMA A = 16 keys (lane c = lane % 16 holds a key, the lane's quarter u = lane / 16 an eighth of every 32
+// elements, loaded as it lies in memory), B = the query rows, so a lane ends up with four keys of one row
+// per MFMA: the row's maximum, its weights and its output live in the lanes of one column c.  The output
+// is transposed too, O^T = V^T P^T: B = the weights exactly where the first product left them (the order of
+// the summed keys is free as long as A has the same), A = V with lane c holding elements 8c .. 8c + 7 of
+// eight keys: sixteen lanes read a whole row, and one v_perm per register pairs two keys' elements.
+// Neither K nor V passes through LDS.
+// bf16 weights are taken as a sum of two bf16 (2^-17): the matrix unit has time, the output is rounded once.
+//
+// m: running maximum (log2 units) of the column's row, raised only when a tile exceeds it by 8
+// (weights stay below 2^8; the sum and the output are float32), so most tiles need no rescaling and no
+// exchange between lanes.  l: this lane's share of the sum.
+template <int ET, int NR>
+struct FewRows {
+  static constexpr bool kF32 = ET == kFP32;
+  static constexpr int kTile = kF32 ? 16 : 32;           // keys per tile
+  static constexpr int kHalves = kTile / 16;
+  static constexpr int kFrags = 8;                       // K fragments per tile, and V fragments
+  typedef typename std::conditional<ET == kFP8, u32x2, u32x4>::type Raw;
+
+  u32x4 q[NR][kF32 ? 8 : 4];                             // query rows, as the B operand
+  f32x4 o[NR][8];
+  float m[NR], l[NR];
+  Raw kf[kFrags], vf[kFrags];
+};
+
+// The pages of a tile's 16-key halves: ids as the table has them.
+template <int KT>
+struct TilePages {
+  int id[KT / 16];
+};
+
+template <int ET, int NR>
+__global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(const PagedArgs a) {
+  using F = FewRows<ET, NR>;
+  constexpr bool kF32 = F::kF32;
+  constexpr int KT = F::kTile, R = 16 * NR;
+  constexpr int kElem = ET == kFP32 ? 4 : (ET == kFP8 ? 1 : 2);
+  __shared__ float joined[4][R][kPartialRow];
+
+  PagedPiece pc;
+  if (!paged_locate<KT, false>(a, blockIdx.x, pc)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, u = lane >> 4;
+  const int len = pc.r.len, tokens = pc.r.tokens;
+  const int tt = pc.tile / a.head_blocks, hb = pc.tile - tt * a.head_blocks;
+  const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, tokens) - 1;
+  const int heads = min(a.G - hb * R, R);                // query heads of the tile: all G where a tile holds whole tokens
+  const int rows = a.head_blocks > 1 ? heads : (last - first + 1) * a.G;
+  const PagedSpan span = paged_span<KT>(a, len, tokens, first, last);
+  int t_begin, t_end;
+  paged_piece_range(span.count, pc.piece, pc.pieces, t_begin, t_end);
+
+  // row of this lane's column: token and head
+  int hi[NR], lo[NR];                                    // keys it attends: [lo, hi], and those below n_sink
+  F f;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int row = c + 16 * n;
+    const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
+    const bool ok = row < rows;
+    hi[n] = ok ? len - tokens + first + t : -1;
+    lo[n] = a.n_local > 0 ? hi[n] - a.n_local + 1 : 0;
+    const int64_t at = (int64_t)(pc.r.row + first + t) * a.q_t + (int64_t)(pc.g * a.G + h) * a.q_h;
+#pragma unroll
+    for (int s = 0; s < (kF32 ? 8 : 4); ++s) {
+      f.q[n][s] = u32x4{0, 0, 0, 0};
+      if (ok) {
+        if (kF32) f.q[n][s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(a.q) + at + 16 * s + 4 * u);
+        else f.q[n][s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + at + 32 * s + 8 * u);
+      }
+    }
+  }
+  const int min_hi = len - tokens + first;               // what every row of the tile attends: [max_lo, min_hi]
+  const int max_lo = a.n_local > 0 ? len - tokens + last - a.n_local + 1 : 0;
+  const int end = len - tokens + last + 1;               // what some row attends: [any_lo, end), and the keys below n_sink
+  const int any_lo = a.n_local > 0 ? len - tokens + first - a.n_local + 1 : 0;
+  const float to_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f);
+
+  const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)pc.b * a.max_pages);
+  const char* kbase = reinterpret_cast<const char*>(a.k) + (int64_t)pc.g * a.k_head * kElem;
+  const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)pc.g * a.v_head * kElem;
+  const int page_mask = (1 << a.page_shift) - 1;
+  const uint32_t k_key = (uint32_t)a.k_key * kElem, v_key = (uint32_t)a.v_key * kElem;
+  // this lane's place in 16 keys: of K key c, of V the keys 4u .. 4u + 3
+  const uint32_t k_lane = c * k_key + (kF32 ? 16 * u : 8 * u * kElem);
+  const uint32_t v_lane = 4 * u * v_key + (kF32 ? 16 * c : 8 * c * kElem);
+
+  auto tile_key = [&](int v) { return (v < span.sink ? v : v + span.skip) * KT; };
+  auto tile_pages = [&](int v, TilePages<KT>& p) {
+    const int key0 = tile_key(v);
+#pragma unroll
+    for (int h = 0; h < F::kHalves; ++h) {
+      const int at = (key0 + 16 * h) >> a.page_shift;
+      p.id[h] = table[at < a.max_pages ? at : a.max_pages - 1];
+    }
+  };
+  auto page_ok = [&](int id) { return (uint32_t)id < (uint32_t)a.n_pages; };
+  // Rows are read through buffer descriptors of 16 keys, `valid` of which are there: the others lie beyond the descriptor's
+  // end and read as zeros, without an access.
+  auto rows16 = [&](const char* pool, int64_t page_stride, uint32_t key_stride, int id, int key, int valid) {
+    const char* base = pool + (valid ? id : 0) * page_stride + (uint32_t)(key & page_mask) * key_stride;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, valid * key_stride, kBufferWord3);
+  };
+  auto request_k = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
+#pragma unroll
+    for (int h = 0; h < F::kHalves; ++h) {
+      const auto rows = rows16(kbase, a.k_page * kElem, k_key, p.id[h], key0 + 16 * h, valid[h]);
+#pragma unroll
+      for (int s = 0; s < 8 / F::kHalves; ++s)
+        load_once(rows, k_lane + (kF32 ? 64 : 32 * kElem) * s, f.kf[h * (8 / F::kHalves) + s]);
+    }
+  };
+  auto request_v = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
+#pragma unroll
+    for (int h = 0; h < F::kHalves; ++h) {
+      const auto rows = rows16(vbase, a.v_page * kElem, v_key, p.id[h], key0 + 16 * h, valid[h]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (kF32) {
+#pragma unroll
+          for (int d = 0; d < 2; ++d) load_once(rows, v_lane + j * v_key + 256 * d, f.vf[2 * j + d]);
+        } else {
+          load_once(rows, v_lane + j * v_key, f.vf[4 * h + j]);
+        }
+      }
+    }
+  };
+  constexpr int kScores = 4 * F::kHalves;                // of a lane: key 16 (i / 4) + 4 u + i % 4 of the tile is number i
+  auto scores = [&](float (&s)[NR][kScores]) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (kF32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.kf[i][e]), __uint_as_float(f.q[n][i][e]), acc, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (ET == kFP8) acc = mfma_bf16(e4m3_to_bf16(f.kf[4 * h + i]), f.q[n][i], acc);
+            else acc = mfma_bf16(f.kf[4 * h + i], f.q[n][i], acc);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][4 * h + i] = acc[i] * to_log2;
+      }
+    }
+  };
+  // scores -> weights, in place; the state is raised where they ask for it
+  auto weigh = [&](float (&s)[NR][kScores]) {
+    bool raise = false;
+    float top[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      top[n] = s[n][0];
+#pragma unroll
+      for (int i = 1; i < kScores; ++i) top[n] = fmaxf(top[n], s[n][i]);
+      raise = raise || top[n] > f.m[n] + 8.f;
+    }
+    if (__any(raise)) {
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        float t = fmaxf(top[n], __shfl_xor(top[n], 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float m1 = fmaxf(f.m[n], t);
+        const float by = f.m[n] == m1 ? 1.f : __builtin_amdgcn_exp2f(f.m[n] - m1);
+        f.m[n] = m1;
+        f.l[n] *= by;
+#pragma unroll
+        for (int t8 = 0; t8 < 8; ++t8) f.o[n][t8] *= by;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const float ref = f.m[n] == -INFINITY ? 0.f : f.m[n];
+#pragma unroll
+      for (int i = 0; i < kScores; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - ref);
+        f.l[n] += s[n][i];
+      }
+    }
+  };
+  auto add_values = [&](const float (&s)[NR][kScores], const u32x4 (&v)[8]) {
+    if constexpr (kF32) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              f.o[n][4 * d + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[2 * i + d][e]), s[n][i], f.o[n][4 * d + e], 0, 0, 0);
+    } else {
+      u32x4 ph[NR], pl[NR];                              // a weight as two bf16
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ph[n][i] = pack_bf16(s[n][2 * i], s[n][2 * i + 1]);
+          pl[n][i] = pack_bf16(s[n][2 * i] - __uint_as_float(ph[n][i] << 16), s[n][2 * i + 1] - __uint_as_float(ph[n][i] & 0xffff0000u));
+        }
+#pragma unroll
+      for (int t8 = 0; t8 < 8; ++t8) {                   // V^T of elements 8 c + t8, two keys a register
+        const uint32_t pick = t8 & 1 ? 0x07060302u : 0x05040100u;
+        u32x4 at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = __builtin_amdgcn_perm(v[2 * i + 1][t8 >> 1], v[2 * i][t8 >> 1], pick);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) f.o[n][t8] = mfma_bf16(at, pl[n], mfma_bf16(at, ph[n], f.o[n][t8]));
+      }
+    }
+  };
+  auto values = [&](u32x4 (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (ET == kFP8) v[i] = e4m3_to_bf16(f.vf[i]);
+      else v[i] = f.vf[i];
+    }
+  };
+
+  // Tiles whose keys every row attends, one after the other: the next one's K is requested when the scores have taken this
+  // one's, its V behind the products with this one's.
+  auto in_full = [&](int v) {
+    const int key0 = tile_key(v);
+    return key0 + KT - 1 <= min_hi && (key0 >= max_lo || key0 + KT <= a.n_sink);
+  };
+  auto pages_ok = [&](const TilePages<KT>& p) {
+    bool ok = true;
+#pragma unroll
+    for (int h = 0; h < F::kHalves; ++h) ok = ok && page_ok(p.id[h]);
+    return ok;
+  };
+  bool bad_page = false;
+  // the first such tile from v on, its pages read
+  auto find = [&](int v, TilePages<KT>& p) {
+    for (; v < t_end; v += 4) {
+      if (!in_full(v)) continue;
+      tile_pages(v, p);
+      if (pages_ok(p)) break;
+      bad_page = true;
+    }
+    return v;
+  };
+  int whole[F::kHalves];
+#pragma unroll
+  for (int h = 0; h < F::kHalves; ++h) whole[h] = 16;
+  TilePages<KT> now, next, after;
+  auto reset = [&]() {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+      for (int t8 = 0; t8 < 8; ++t8) f.o[n][t8] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f.m[n] = -INFINITY;
+      f.l[n] = 0.f;
+    }
+  };
+  reset();
+  int v = find(t_begin + wave, now), v1 = t_end;
+  if (v < t_end) {
+    request_k(tile_key(v), now, whole);
+    request_v(tile_key(v), now, whole);
+    v1 = find(v + 4, next);
+  }
+#pragma unroll 1
+  while (v < t_end) {
+    const int v2 = v1 + 4;
+    if (v2 < t_end) tile_pages(v2, after);
+    float s[NR][kScores];
+    scores(s);
+    if (v1 < t_end) request_k(tile_key(v1), next, whole);
+    weigh(s);
+    u32x4 vb[8];
+    values(vb);
+    add_values(s, vb);
+    if (v1 < t_end) request_v(tile_key(v1), next, whole);
+    v = v1;
+    v1 = v2;
+    next = after;
+    if (v1 < t_end && !(in_full(v1) && pages_ok(next))) {
+      bad_page = bad_page || in_full(v1);
+      v1 = find(v1 + 4, next);
+    }
+  }
+
+  // The others: the last ones, the borders of the window and of the sink, tiles with a page that is none.
+  auto others = [&](auto all) {
+    constexpr bool CAREFUL = decltype(all)::value;
+    int v = t_begin + wave;
+    if (a.n_local == 0 && !bad_page && !CAREFUL) {   // only from the first key on that some row does not attend
+      const int from = (min_hi + 1 > 0 ? min_hi + 1 : 0) / KT;
+      if (from > v) v += (from - v + 3) / 4 * 4;
+    }
+#pragma unroll 1
+    for (; v < t_end; v += 4) {
+      const bool inside = in_full(v);
+      if (inside && !bad_page && !CAREFUL) continue;
+      tile_pages(v, now);
+      if (inside && !CAREFUL && pages_ok(now)) continue;
+      const int key0 = tile_key(v);
+      int valid[F::kHalves];
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) valid[h] = page_ok(now.id[h]) ? min(max(end - key0 - 16 * h, 0), 16) : 0;
+      request_k(key0, now, valid);
+      request_v(key0, now, valid);
+      float s[NR][kScores];
+      scores(s);
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) {
+        const int at = key0 + 16 * h + 4 * u;               // key i of this lane is at + i
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          const int to = valid[h] ? hi[n] - at : -1, from = lo[n] - at, sink = a.n_sink - at;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[n][4 * h + i] = i <= to && (i >= from || i < sink) ? s[n][4 * h + i] : -INFINITY;
+        }
+      }
+      weigh(s);
+      u32x4 vb[8];
+      values(vb);
+      // V of the keys before the window is cleared (those behind the last one were read as zeros)
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) {
+        const int at = key0 + 16 * h + 4 * u, from = any_lo - at, sink = a.n_sink - at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t keep = i >= from || i < sink ? ~0u : 0u;
+#pragma unroll
+          for (int d = 0; d < (kF32 ? 2 : 1); ++d) vb[kF32 ? 2 * i + d : 4 * h + i] &= keep;
+        }
+      }
+      if (CAREFUL) clear_not_finite<kF32>(vb);
+      add_values(s, vb);
+      if (!CAREFUL) continue;
+      // what was cleared, added key by key to the rows that attend the key; the weights change lanes through LDS
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int i = 0; i < kScores; ++i) joined[wave][c + 16 * n][16 * (i >> 2) + 4 * u + (i & 3)] = s[n][i];
+#pragma unroll 1
+      for (int k = 0; k < KT; ++k) {
+        const int key = key0 + k, id = F::kHalves == 2 && k >= 16 ? now.id[F::kHalves - 1] : now.id[0];
+        if (!page_ok(id) || key >= end) continue;
+        const char* row = vbase + id * (a.v_page * kElem) + (uint32_t)(key & page_mask) * v_key;
+#pragma unroll
+        for (int i = 0; i < (kF32 ? 8 : 4); ++i) {          // four elements at a time, or eight
+          float x[8];
+          if constexpr (kF32) {
+            const float4 w = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(row) + 64 * (i >> 2) + 16 * u + 4 * (i & 3));
+            x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+          } else {
+            load8<ET>(row, 32 * u + 8 * i, x);
+          }
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            const float w = joined[wave][c + 16 * n][k];
+            const bool attends = key <= hi[n] && (key >= lo[n] || key < a.n_sink);
+#pragma unroll
+            for (int e = 0; e < (kF32 ? 4 : 8); ++e) {
+              const int t8 = kF32 ? 4 * (i >> 2) + e : e;
+              if (attends && !(fabsf(x[e]) < INFINITY)) f.o[n][t8][i & 3] += w * x[e];
+            }
+          }
+        }
+      }
+    }
+  };
+  others(std::false_type{});
+
+  // The products take every row of a tile with every key's V: an infinity or a NaN there reaches rows that do not attend the key
+  // (a weight of 0 does not clear it), and an infinity may come out as a NaN (the two parts of a weight differ in sign).
+  // Either leaves a NaN in the output, so a wavefront that ends with one goes over its tiles again, carefully: what is
+  // not finite is left out of the products and added afterwards to the rows that attend its key.
+  float sum = 0.f;                                       // NaN if one of them is, or if infinities meet
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int t8 = 0; t8 < 8; ++t8) sum += (f.o[n][t8][0] + f.o[n][t8][1]) + (f.o[n][t8][2] + f.o[n][t8][3]);
+  if (__any(sum != sum)) {
+    reset();
+    others(std::true_type{});
+  }
+
+  // the four wavefronts' parts, joined in LDS
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    float l = f.l[n];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    float* to = joined[wave][c + 16 * n];
+    if (kF32) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(to + 64 * d + 16 * u + 4 * i) =
+              f32x4{f.o[n][4 * d][i], f.o[n][4 * d + 1][i], f.o[n][4 * d + 2][i], f.o[n][4 * d + 3][i]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+          *reinterpret_cast<f32x4*>(to + 32 * u + 8 * i + 4 * d) =
+              f32x4{f.o[n][4 * d][i], f.o[n][4 * d + 1][i], f.o[n][4 * d + 2][i], f.o[n][4 * d + 3][i]};
+    }
+    if (u == 0) { to[128] = f.m[n]; to[129] = l; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int row = (threadIdx.x >> 4) + 16 * n, e0 = (threadIdx.x & 15) * 8;
+    if (row >= rows) continue;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, joined[w][row][128]);
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = joined[w][row][128];
+      const float by = mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
+      l += by * joined[w][row][129];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += by * joined[w][row][e0 + e];
+    }
+    if (pc.pieces > 1) {
+      const int64_t slot = pc.slot + pc.piece;
+      if (slot >= a.slots) continue;
+      float* pp = a.partial + (slot * R + row) * kPartialRow;
+      *reinterpret_cast<f32x4*>(pp + e0) = f32x4{o[0], o[1], o[2], o[3]};
+      *reinterpret_cast<f32x4*>(pp + e0 + 4) = f32x4{o[4], o[5], o[6], o[7]};
+      if (e0 == 0) { pp[128] = m; pp[129] = l; }
+    } else {
+      const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
+      const int64_t to = (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h;
+      const float vs = (a.v_scale ? a.v_scale[pc.g] : 1.f);
+      paged_write_row<kF32>(a, to, e0, o, m, l, vs);
+    }
+  }
+}
+
+// ---- joining the pieces of an item ------------------------------------------------------------------
+// A workgroup takes a row of a cut item: eight half wavefronts take its partials in turn, four elements a
+// lane, four partials requested at once, and join what they have in LDS.
+template <bool FP32, int KT, int R>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
+  __shared__ float joined[8][kPartialRow];
+  PagedPiece pc;
+  if (!paged_locate<KT, true>(a, blockIdx.x, pc)) return;
+  const int row = blockIdx.y;
+  const int tt = pc.tile / a.head_blocks, hb = pc.tile - tt * a.head_blocks;
+  const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, pc.r.tokens) - 1;
+  const int rows = a.head_blocks > 1 ? min(a.G - hb * R, R) : (last - first + 1) * a.G;
+  if (row >= rows || pc.slot + pc.pieces > a.slots) return;
+  const int part = threadIdx.x >> 5, l32 = threadIdx.x & 31;
+  const float* pp = a.partial + ((int64_t)pc.slot * R + row) * kPartialRow;
+  const int64_t step = (int64_t)R * kPartialRow;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (int p = part; p < pc.pieces; p += 32) {
+    f32x4 o1[4];
+    float m1[4], l1[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool ok = p + 8 * i < pc.pieces;
+      const float* from = pp + (ok ? p + 8 * i : p) * step;
+      o1[i] = *reinterpret_cast<const f32x4*>(from + 4 * l32);
+      m1[i] = ok ? from[128] : -INFINITY;
+      l1[i] = ok ? from[129] : 0.f;
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, m1[i]);
+    if (top > -INFINITY) {
+      const float by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+      o *= by;
+      l *= by;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float b1 = m1[i] == top ? 1.f : (m1[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1[i] - top));
+        if (m1[i] > -INFINITY) {                           // (an empty partial, or one repeated behind the last)
+          o += b1 * o1[i];
+          l += b1 * l1[i];
+        }
+      }
+      m = top;
+    }
+  }
+  *reinterpret_cast<f32x4*>(&joined[part][4 * l32]) = o;
+  if (l32 == 0) { joined[part][128] = m; joined[part][129] = l; }
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  const int e0 = threadIdx.x * 8;
+  float top = -INFINITY, sum = 0.f, out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 8; ++w) top = fmaxf(top, joined[w][128]);
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    const float mw = joined[w][128];
+    const float by = mw == -INFINITY ? 0.f : (mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - top));
+    sum += by * joined[w][129];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] += by * joined[w][e0 + e];
+  }
+  const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
+  paged_write_row<FP32>(a, (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h, e0, out, top, sum, a.v_scale ? a.v_scale[pc.g] : 1.f);
+}
+
+template <int ET, int NR>
+hipError_t launch_few_rows(const PagedArgs& a, const PagedForm& form, hipStream_t s) {
+  constexpr int KT = FewRows<ET, NR>::kTile;
+  paged_few_rows_kernel<ET, NR><<<(unsigned)form.pieces, 256, 0, s>>>(a);
+  if (form.units > 0) {
+    const int rows = a.head_blocks > 1 ? form.rows : (a.tile_tokens < a.max_new ? a.tile_tokens : a.max_new) * a.G;
+    paged_join_kernel<ET == kFP32, KT, 16 * NR><<<dim3((unsigned)form.units, rows), 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s) {
+  if (element == kFP32) return launch_few_rows<kFP32, 1>(a, form, s);
+  if (form.rows == 16) return element == kFP8 ? launch_few_rows<kFP8, 1>(a, form, s) : launch_few_rows<kBF16, 1>(a, form, s);
+  return element == kFP8 ? launch_few_rows<kFP8, 2>(a, form, s) : launch_few_rows<kBF16, 2>(a, form, s);
+}
+
+}  // namespace mp

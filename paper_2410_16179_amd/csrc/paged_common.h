@@ -1,0 +1,200 @@
+// Launch descriptions of the paged cache's kernels, and how the work of paged attention is cut.
+#pragma once
+#include "mp_common.h"
+#include "device_utils.h"
+
+namespace mp {
+
+struct PagePlanArgs {
+  const int* new_tokens; const int* lengths; int* table; int* free_pages; const int* n_free;
+  int* lengths_out; int* n_free_out; int* token_start; int64_t* slots; int* status;
+  int* scan;              // workspace: the three prefix sums, [3][batch + 1] (the two-launch form)
+  int batch, page_shift, max_pages, max_new;
+  int64_t n_pages, max_tokens;
+};
+
+struct PageAppendArgs {
+  const void* k_new; const void* v_new; const int64_t* slots; const float* k_scale; const float* v_scale;
+  void* k_pages; void* v_pages;
+  int heads, page_shift, is_fp32, kv_fp8;
+  int64_t n_slots, tokens;
+  int64_t kn_t, kn_h, vn_t, vn_h;
+  int64_t k_page, k_key, k_head, v_page, v_key, v_head;
+};
+
+// Paged attention.  The rows of a request (its new tokens times the query heads of a KV head) are taken
+// in row tiles of whole tokens (tile_tokens each; where one token has more heads than a tile has rows,
+// head_blocks tiles per token).  An item is a row tile of one request and KV head; its keys are counted
+// in tiles, and a long item is cut into pieces of them, one workgroup each, joined by a second kernel.
+// Lengths are known on the device alone, so every workgroup works out the cut for itself: requests are
+// charged their keys (as if all row tiles reached the last one), pieces get at most 1/target of the sum.
+// A request that is cut has more than piece_tiles tiles per item, so cut items have at most twice
+// target pieces together.
+struct PagedArgs {
+  const void* q; const void* k; const void* v; const float* k_scale; const float* v_scale;
+  const int* table; const int* lengths; const int* token_start;
+  void* out; float* lse; float* partial;
+  int batch, Hq, Hkv, G, page_shift, max_pages, max_new, n_sink, n_local;
+  int max_len, max_tokens, n_pages;
+  int tile_tokens, head_blocks;
+  float scale_log2;       // logits scale * log2(e)
+  float per_piece;        // (1 + margin) / target pieces
+  int min_tiles;          // of a piece
+  int slots;              // partials that there is room for
+  int64_t k_page, k_key, k_head, v_page, v_key, v_head, q_t, q_h;
+};
+
+struct PagedRequest {
+  int len, tokens, row;   // keys, new tokens, row of the first one
+};
+
+__device__ inline PagedRequest paged_request(const PagedArgs& a, int b) {
+  PagedRequest r;
+  const int len = a.lengths[b];
+  r.len = len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
+  if (a.token_start) {
+    const int s0 = a.token_start[b], s1 = a.token_start[b + 1];
+    r.row = s0 < 0 ? 0 : (s0 > a.max_tokens ? a.max_tokens : s0);
+    const int end = s1 < r.row ? r.row : (s1 > a.max_tokens ? a.max_tokens : s1);
+    r.tokens = end - r.row < a.max_new ? end - r.row : a.max_new;
+  } else {
+    r.row = b;
+    r.tokens = 1;
+  }
+  return r;
+}
+
+// Key tiles that a row tile of the request has at most (what its items are charged).
+template <int KT>
+__device__ inline int paged_charge(const PagedArgs& a, int len) {
+  int n = (len + KT - 1) / KT;
+  if (a.n_local > 0) {
+    const int w = (a.n_sink + KT - 1) / KT + (a.n_local + a.tile_tokens - 2) / KT + 2;
+    n = n < w ? n : w;
+  }
+  return n > 1 ? n : 1;
+}
+
+// The key tiles of one row tile, tokens first .. last of the request: the sink's, then those of the window.
+// Tile v of `count` is tile v of the cache, or v + skip from `sink` on.
+struct PagedSpan {
+  int count, sink, skip;
+};
+template <int KT>
+__device__ inline PagedSpan paged_span(const PagedArgs& a, int len, int tokens, int first, int last) {
+  PagedSpan s{0, 0, 0};
+  const int end = len - tokens + last + 1;               // one behind the last key attended
+  if (end <= 0) return s;
+  s.count = (end + KT - 1) / KT;
+  if (a.n_local > 0) {
+    const int lo = len - tokens + first - a.n_local + 1;
+    if (lo > 0) {
+      const int kept = a.n_sink < lo ? a.n_sink : lo, sink = (kept + KT - 1) / KT, from = lo / KT;
+      if (from > sink) {
+        s.sink = sink;
+        s.skip = from - sink;
+        s.count -= s.skip;
+      }
+    }
+  }
+  return s;
+}
+
+struct PagedPiece {
+  int b, g, tile, piece, pieces;   // request, KV head, row tile, piece of the item and how many it has
+  PagedRequest r;
+  int slot;                        // of the item's first partial
+};
+
+__device__ inline int wave_prefix(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(v, d);
+    if (lane >= d) v += u;
+  }
+  return v;
+}
+
+// MERGE false: piece `index` of all; true: item `index` of those that are cut.  Called by whole wavefronts with
+// one index; false where there is none.
+template <int KT, bool MERGE>
+__device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& out) {
+  const int lane = threadIdx.x & 63;
+  float total = 0.f;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int b = b0 + lane;
+    float cost = 0.f;
+    if (b < a.batch) {
+      const PagedRequest r = paged_request(a, b);
+      const int tiles = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
+      cost = (float)tiles * (float)a.Hkv * (float)paged_charge<KT>(a, r.len);
+    }
+    total += wave_sum(cost);
+  }
+  const float want = fminf(ceilf(total * a.per_piece), 1073741824.f);
+  const int piece_tiles = max((int)want, a.min_tiles);
+  int base = 0, slot_base = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int b = b0 + lane;
+    PagedRequest r{0, 0, 0};
+    int items = 0, pieces = 1;
+    if (b < a.batch) {
+      r = paged_request(a, b);
+      items = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks * a.Hkv;
+      pieces = (paged_charge<KT>(a, r.len) + piece_tiles - 1) / piece_tiles;
+    }
+    const int cut = pieces > 1 ? items * pieces : 0;
+    const int count = MERGE ? (pieces > 1 ? items : 0) : items * pieces;
+    const int upto = wave_prefix(count, lane), slots = wave_prefix(cut, lane);
+    const uint64_t found = __ballot(base + upto > index);
+    if (found) {
+      const int f = __ffsll((unsigned long long)found) - 1;
+      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+      int i = index - base - at(upto - count);
+      out.b = b0 + f;
+      out.r.len = at(r.len); out.r.tokens = at(r.tokens); out.r.row = at(r.row);
+      out.pieces = at(pieces);
+      const int tiles = at(items) / a.Hkv;
+      out.g = i % a.Hkv;
+      i /= a.Hkv;
+      out.tile = tiles - 1 - i % tiles;                  // (the last row tile has most keys: first)
+      out.piece = MERGE ? 0 : i / tiles;
+      out.slot = slot_base + at(slots - cut) + (out.tile * a.Hkv + out.g) * out.pieces;
+      return true;
+    }
+    base += __builtin_amdgcn_readlane(upto, 63);
+    slot_base += __builtin_amdgcn_readlane(slots, 63);
+  }
+  return false;
+}
+
+// Tiles [begin, end) of an item's `count` that piece `piece` of `pieces` takes.
+__device__ inline void paged_piece_range(int count, int piece, int pieces, int& begin, int& end) {
+  const int each = count / pieces, more = count % pieces;
+  begin = piece * each + (piece < more ? piece : more);
+  end = begin + each + (piece < more ? 1 : 0);
+}
+
+// Eight elements, e0 .. e0 + 7, of a finished row: o / l (times the values' scale), and with the first ones the row's lse.
+template <bool FP32>
+__device__ inline void paged_write_row(const PagedArgs& a, int64_t row, int e0, const float (&o)[8], float m, float l, float v_scale) {
+  const float by = l == 0.f ? 0.f : v_scale / l;           // (a NaN stays one)
+  if constexpr (FP32) {
+    float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + row * kHeadDim + e0);
+    to[0] = make_float4(o[0] * by, o[1] * by, o[2] * by, o[3] * by);
+    to[1] = make_float4(o[4] * by, o[5] * by, o[6] * by, o[7] * by);
+  } else {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    bf16x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (__bf16)(o[e] * by);
+    *reinterpret_cast<bf16x8*>(reinterpret_cast<uint16_t*>(a.out) + row * kHeadDim + e0) = v;
+  }
+  if (a.lse && e0 == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
+hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s);
+hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s);
+hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s);
+
+}  // namespace mp

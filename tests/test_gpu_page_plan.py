@@ -1,0 +1,203 @@
+"""The page plan against a plain model, and the append against torch's own conversions."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2410_16179_amd import binding as mp
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+D = 128
+dev = lambda x, t=np.int32: torch.from_numpy(np.ascontiguousarray(x, t)).cuda()
+
+
+def state(rng, lengths, page, max_pages, spare):
+    held = [-(-n // page) for n in lengths]
+    n_pages = sum(held) + spare
+    ids = rng.permutation(n_pages)
+    table = np.full((len(lengths), max_pages), -7, np.int32)
+    at = 0
+    for b, h in enumerate(held):
+        table[b, :h] = ids[at:at + h]
+        at += h
+    free = np.full(n_pages, -9, np.int32)
+    free[:n_pages - at] = ids[at:]
+    return table, free, n_pages - at
+
+
+def run_plan(new, lengths, table, free, n_free, page, max_new, max_tokens, in_place=False, times=1):
+    p = mp.make_paged_params(batch=len(lengths), n_q_heads=1, n_kv_heads=1, dtype="bf16", page_size=page, max_pages=table.shape[1],
+                             n_pages=len(free), max_tokens=max_tokens, max_new=max_new)
+    t = {"table": dev(table), "free": dev(free), "lengths": dev(lengths), "n_free": dev([n_free])}
+    out = {"lengths": t["lengths"] if in_place else dev(np.full(len(lengths), 77)), "n_free": t["n_free"] if in_place else dev([77]),
+           "token_start": dev(np.full(len(lengths) + 1, 77)), "slots": dev(np.full(max_tokens, 77), np.int64), "status": dev([77])}
+    for _ in range(times):
+        mp.magicpig_page_plan(p, dev(new), t["lengths"], t["table"], t["free"], t["n_free"], out["lengths"], out["n_free"],
+                              out["token_start"], out["slots"], out["status"], mp.alloc_paged_workspace(p))
+    torch.cuda.synchronize()
+    got = {k: v.cpu().numpy() for k, v in out.items()}
+    return {**got, "table": t["table"].cpu().numpy(), "free": t["free"].cpu().numpy()}
+
+
+def compare(got, want):
+    for k in ("status", "n_free"):
+        assert int(got[k][0]) == want[k], k
+    for k in ("lengths", "token_start", "slots", "table", "free"):
+        np.testing.assert_array_equal(got[k], want[k], err_msg=k)
+
+
+def both(new, lengths, table, free, n_free, page, max_new, max_tokens, **how):
+    want = ref.plan(new, lengths, table, free, n_free, page, max_new, max_tokens)
+    compare(run_plan(new, lengths, table, free, n_free, page, max_new, max_tokens, **how), want)
+    return want
+
+
+@pytest.mark.parametrize("batch,page,longest,most", [(1, 16, 40, 5), (5, 16, 100, 40), (64, 32, 300, 3), (65, 64, 2000, 100),
+                                                     (1024, 16, 60, 4), (1025, 16, 60, 4), (2049, 16, 50, 6), (300, 16, 200, 90)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_mixed_steps(batch, page, longest, most, in_place):
+    rng = np.random.default_rng(batch + page)
+    lengths = [int(x) for x in rng.integers(0, longest + 1, batch)]
+    new = [int(x) for x in rng.integers(-1, most + 1, batch)]
+    max_pages = -(-(longest + most) // page)
+    table, free, n_free = state(rng, lengths, page, max_pages, spare=batch * (most // page + 1) + 3)
+    total = sum(max(n, 0) for n in new)
+    want = both(new, lengths, table, free, n_free, page, most, total + 37, in_place=in_place)
+    assert want["status"] == 0
+    both(new, lengths, table, free, n_free, page, most, max(total, 1), in_place=in_place)       # no row to spare
+    if not in_place:                                     # what the call reads is left as it was: it can be repeated
+        both(new, lengths, table, free, n_free, page, most, total + 37, times=2)
+
+
+def test_requests_of_no_tokens_and_no_requests():
+    rng = np.random.default_rng(0)
+    table, free, n_free = state(rng, [0, 0, 16], 16, 3, 4)
+    both([0, 0, 0], [0, 0, 16], table, free, n_free, 16, 1, 5)
+    both([0, -1, 0], [0, 0, 16], table, free, n_free, 16, 1, 5)
+    got = run_plan([], [], np.zeros((0, 3), np.int32), free, n_free, 16, 1, 5)
+    assert got["status"][0] == 0 and got["n_free"][0] == n_free and (got["slots"] == -1).all() and got["token_start"][0] == 0
+
+
+@pytest.mark.parametrize("spare", [0, 1, 2, 5])
+def test_pages_of_ended_requests_are_handed_out_at_once(spare):
+    rng = np.random.default_rng(spare)
+    lengths = [40, 33, 16, 0, 70]
+    table, free, n_free = state(rng, lengths, 16, 8, spare)
+    want = both([-1, 17, -1, 30, 1], lengths, table, free, n_free, 16, 40, 64)
+    assert want["status"] == (0 if spare else 0)
+    both([-1, 1, -1, 0, 1], lengths, table, free, n_free, 16, 40, 64, in_place=True)
+
+
+def test_more_pages_come_back_than_tokens_go_in():
+    rng = np.random.default_rng(3)
+    lengths = [16 * 3000, 5, 16 * 700 - 3]
+    table, free, n_free = state(rng, lengths, 16, 3001, 2)
+    both([-1, 1, -1], lengths, table, free, n_free, 16, 4, 2)
+    both([-1, 1, -1], lengths, table, free, n_free, 16, 9000, 9000)
+
+
+def test_shortage_hands_out_nothing():
+    rng = np.random.default_rng(4)
+    lengths = [16, 20, 48]
+    table, free, n_free = state(rng, lengths, 16, 9, 2)
+    for new in ([17, 13, 1], [60, -1, 60]):
+        want = both(new, lengths, table, free, n_free, 16, 64, 130)
+        assert want["status"] > 0
+        both(new, lengths, table, free, n_free, 16, 64, 130, in_place=True)
+
+
+@pytest.mark.parametrize("new,lengths,max_new,rows,n_free", [
+    ([-2, 1], [5, 5], 4, 8, 2), ([5, 1], [5, 5], 4, 8, 2), ([1, 1], [-1, 5], 4, 8, 2), ([1, 1], [49, 5], 4, 8, 2), ([4, 1], [45, 5], 4, 8, 2),
+    ([4, 4], [5, 5], 4, 7, 2), ([-1, 1], [49, 5], 4, 8, 2), ([1, 1], [5, 5], 4, 8, -1), ([1, 1], [5, 5], 4, 8, 9), ([-1, 1], [30, 5], 4, 8, 3),
+    ([2 ** 31 - 1, 2 ** 31 - 1], [5, 5], 4, 8, 2), ([1, 1], [2 ** 31 - 1, 5], 4, 8, 2), ([-2 ** 31, 1], [5, 5], 4, 8, 2)])
+def test_what_does_not_fit_changes_nothing(new, lengths, max_new, rows, n_free):
+    table = np.arange(6, dtype=np.int32).reshape(2, 3) % 4
+    want = ref.plan(new, lengths, table, np.arange(4, dtype=np.int32), n_free, 16, max_new, rows)
+    assert want["status"] == -1
+    for in_place in (False, True):
+        compare(run_plan(new, lengths, table, np.arange(4, dtype=np.int32), n_free, 16, max_new, rows, in_place=in_place), want)
+
+
+def test_many_requests_whose_counts_overflow_32_bits():
+    n = 3000
+    lengths, new = [5] * n, [2 ** 24 - 6] * n
+    table, free = np.zeros((n, 1 << 10), np.int32), np.arange(10, dtype=np.int32)
+    want = ref.plan([17] * n, lengths, table, free, 10, 16, 16, 100)          # (refused for the same reason, at a count a list can hold)
+    compare(run_plan(new, lengths, table, free, 10, 16, 100, 100), want)
+
+
+# ---- append ------------------------------------------------------------------------------------------
+def append(kind, tokens, heads, page, layout, slots, scales=None, wide=0, values=None, n_pages=None, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    it = torch.float32 if kind == "fp32" else torch.bfloat16
+    ot = torch.float8_e4m3fn if kind == "fp8" else it
+    new = [torch.randn(tokens, heads + wide, D, generator=g, device="cuda").mul(5.0).to(it)[:, wide:] for _ in range(2)]
+    if values is not None:
+        for x in new:
+            x[:] = values.to(it).cuda()
+    n_pages = max(slots) // page + 2 if n_pages is None else n_pages
+    shape = (n_pages, heads, page, D) if layout == "head" else (n_pages, page, heads, D)
+    pools = [(torch.rand(shape, generator=g, device="cuda") * 3).to(ot) for _ in range(2)]
+    if layout == "head":
+        pools = [x.permute(0, 2, 1, 3) for x in pools]
+    want = [x.clone() for x in pools]
+    slots_t = torch.tensor(slots, dtype=torch.int64, device="cuda")
+    ks, vs = (None, None) if scales is None else scales
+    p = mp.make_paged_params(batch=1, n_q_heads=heads, n_kv_heads=heads, dtype="fp32" if kind == "fp32" else "bf16",
+                             kv_dtype="fp8" if kind == "fp8" else "", page_size=page, max_pages=n_pages, n_pages=n_pages, max_tokens=tokens,
+                             max_new=tokens, k_strides=pools[0].stride()[:3], v_strides=pools[1].stride()[:3],
+                             k_new_strides=new[0].stride()[:2], v_new_strides=new[1].stride()[:2])
+    mp.magicpig_page_append(p, new[0], new[1], slots_t, ks, vs, pools[0], pools[1])
+    torch.cuda.synchronize()
+    for x, w, s in zip(new, want, (ks, vs)):
+        rows = x.cpu().float()
+        if s is not None:
+            rows = rows / s.cpu()[:, None]
+        if kind == "fp8":
+            rows = rows.clamp(-448.0, 448.0)
+        rows = rows.to(ot)
+        for t, slot in enumerate(slots):
+            if 0 <= slot < n_pages * page:
+                w[slot // page, slot % page] = rows[t].cuda()
+    return pools, want
+
+
+def same(pools, want):
+    for got, w in zip(pools, want):
+        if got.dtype == torch.float8_e4m3fn:
+            got, w = got.float(), w.float()
+        np.testing.assert_array_equal(got.float().cpu().numpy(), w.float().cpu().numpy())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("tokens,heads,page,layout,wide", [(1, 1, 16, "token", 0), (7, 3, 16, "head", 2), (65, 8, 64, "token", 32), (500, 2, 1024, "head", 0)])
+def test_append(kind, tokens, heads, page, layout, wide):
+    rng = np.random.default_rng(tokens)
+    slots = [int(x) for x in rng.permutation(tokens + 40)[:tokens]]
+    if tokens > 3:
+        slots[1], slots[2], slots[3] = -1, -2 ** 63, 2 ** 63 - 1
+    n_pages = (tokens + 40) // page + 1
+    scales = (torch.rand(heads, device="cuda") + 0.02, torch.rand(heads, device="cuda") * 0.01 + 1e-4) if kind == "fp8" else None
+    same(*append(kind, tokens, heads, page, layout, slots, scales, wide, n_pages=n_pages))
+    if kind == "fp8":
+        same(*append(kind, tokens, heads, page, layout, slots, None, wide, n_pages=n_pages))
+
+
+def test_append_rounds_to_e4m3_as_defined():
+    # every finite bf16 magnitude around and below the e4m3 range, ties, the ends, infinities, NaN, zeros of both signs
+    bits = torch.arange(0, 1 << 16, dtype=torch.int32).to(torch.int16)
+    values = bits.view(torch.bfloat16).view(-1, 1, D)
+    n = values.shape[0]
+    pools, want = append("fp8", n, 1, 64, "token", list(range(n)), None, values=values)
+    same(pools, want)
+    # signs of zeros as well
+    assert torch.equal(torch.signbit(pools[0].float()) & (pools[0].float() == 0), torch.signbit(want[0].float()) & (want[0].float() == 0))
+    scale = torch.full((1,), 0.37, device="cuda")
+    same(*append("fp8", n, 1, 64, "token", list(range(n)), (scale, scale), values=values))
+
+
+def test_a_grid_s_worth_and_more():
+    n = 40000
+    rng = np.random.default_rng(5)
+    pools, want = append("bf16", n, 8, 64, "token", [int(x) for x in rng.permutation(n)])
+    same(pools, want)

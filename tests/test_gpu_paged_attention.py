@@ -1,0 +1,229 @@
+"""Exact attention over the paged cache against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2410_16179_amd import binding as mp
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+D = 128
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32, "fp8": torch.bfloat16}
+
+
+class Problem:
+    """A paged cache with random keys in the slots that requests hold and NaN in all others."""
+
+    def __init__(self, *, kind, heads, kv_heads, page, lengths, new=None, layout="token", n_sink=0, n_local=0, scale=0.0, seed=0,
+                 spread=1.0, spare_rows=0, max_new=None, q_wide=0, bad=()):
+        rng = np.random.default_rng(seed)
+        self.kind, self.page, self.lengths, self.n_sink, self.n_local, self.scale = kind, page, lengths, n_sink, n_local, scale
+        batch = len(lengths)
+        held = [-(-n // page) for n in lengths]
+        max_pages, n_pages = max(max(held), 1) + 1, sum(held) + 3
+        ids = rng.permutation(n_pages)[:sum(held)]
+        self.table = np.full((batch, max_pages), -1, np.int32)
+        at = 0
+        for b, h in enumerate(held):
+            self.table[b, :h] = ids[at:at + h]
+            at += h
+        new = [1] * batch if new is None else new
+        self.start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        tokens = int(self.start[-1]) + spare_rows
+        dt = TYPES[kind]
+        store = (lambda x: torch.from_numpy(x).float().to(dt)) if kind != "fp8" else \
+            (lambda x: torch.from_numpy(np.clip(x, -448, 448)).float().to(torch.float8_e4m3fn))
+        size = 40.0 if kind == "fp8" else 1.0
+        shift = rng.standard_normal((kv_heads, D))
+        pool = lambda more: np.where(self._held(n_pages)[:, :, None, None],
+                                     size * (rng.standard_normal((n_pages, page, kv_heads, D)) + more), np.nan)
+        self.k, self.v = store(pool(shift)), store(pool(0.2))
+        self.q = torch.from_numpy(spread * rng.standard_normal((tokens, heads, D))).float().to(dt)
+        self.ks = self.vs = None
+        if kind == "fp8":
+            self.ks, self.vs = (torch.from_numpy(0.01 + 0.03 * rng.random(kv_heads)).float() for _ in range(2))
+        for b, j, value in bad:
+            self.table[b, j] = value
+        self.heads, self.kv_heads, self.layout = heads, kv_heads, layout
+        self.single = all(n == 1 for n in new) and spare_rows == 0
+        self.max_new = max(max(new), 1) if max_new is None else max_new
+        self.q_wide = q_wide
+        self.upload()
+
+    def _held(self, n_pages):
+        held = np.zeros((n_pages, self.page), bool)
+        for b, n in enumerate(self.lengths):
+            i = np.arange(n)
+            held[self.table[b, i // self.page], i % self.page] = True
+        return held
+
+    def upload(self):
+        def pool(x):
+            if self.layout == "head":
+                return x.permute(0, 2, 1, 3).contiguous().cuda().permute(0, 2, 1, 3)
+            if self.layout == "wide":                    # rows of 160 elements, other elements NaN
+                w = torch.full(x.shape[:3] + (160,), float("nan"), dtype=torch.float32).to(x.dtype)
+                w[..., :D] = x
+                return w.cuda()[..., :D]
+            return x.cuda()
+        self.dk, self.dv = pool(self.k), pool(self.v)
+        q = self.q
+        if self.q_wide:
+            wide = torch.full((q.shape[0], self.heads + self.q_wide, D), float("nan"), dtype=q.dtype)
+            wide[:, :self.heads] = q
+            self.dq = wide.cuda()[:, :self.heads]
+        else:
+            self.dq = q.cuda()
+        self.dtable, self.dlen, self.dstart = (torch.from_numpy(np.asarray(x, np.int32)).cuda() for x in (self.table, self.lengths, self.start))
+        self.dks, self.dvs = (None if s is None else s.cuda() for s in (self.ks, self.vs))
+
+    def params(self, **more):
+        return mp.make_paged_params(**{**dict(
+            batch=len(self.lengths), n_q_heads=self.heads, n_kv_heads=self.kv_heads, dtype="fp32" if self.kind == "fp32" else "bf16",
+            kv_dtype="fp8" if self.kind == "fp8" else "", page_size=self.page, max_pages=self.table.shape[1], n_pages=self.k.shape[0],
+            max_tokens=self.q.shape[0], max_new=self.max_new, n_sink=self.n_sink, n_local=self.n_local, scale=self.scale,
+            k_strides=self.dk.stride()[:3], v_strides=self.dv.stride()[:3], q_strides=self.dq.stride()[:2]), **more})
+
+    def run(self, with_start=None):
+        p = self.params()
+        out = torch.full((self.q.shape[0], self.heads, D), 7.0, dtype=TYPES[self.kind], device="cuda")
+        lse = torch.full(out.shape[:2], 7.0, device="cuda")
+        start = self.dstart if (not self.single if with_start is None else with_start) else None
+        mp.magicpig_paged_attention(p, self.dq, self.dk, self.dv, self.dks, self.dvs, self.dtable, self.dlen, start, out, lse,
+                                    mp.alloc_paged_workspace(p))
+        torch.cuda.synchronize()
+        return out.cpu().double().numpy(), lse.cpu().double().numpy()
+
+    def reference(self):
+        k, v = self.k.double().numpy(), self.v.double().numpy()
+        if self.ks is not None:
+            k, v = k * self.ks.double().numpy()[:, None], v * self.vs.double().numpy()[:, None]
+        return ref.attention(self.q.double().numpy(), k, v, self.table, self.lengths, None if self.single else self.start,
+                             self.n_sink, self.n_local, self.scale or None, self.max_new)
+
+    def check(self, with_start=None):
+        out, lse = self.run(with_start)
+        self.compare(out, lse)
+
+    def compare(self, out, lse):
+        want, want_lse, size, reach, count = self.reference()
+        rows = ~np.isnan(want_lse) | np.isnan(want).any(-1)
+        real = np.zeros(rows.shape, bool)
+        for b in range(len(self.lengths)):
+            real[self.start[b]:min(self.start[b + 1], self.start[b] + self.max_new)] = True
+        np.testing.assert_array_equal(out[~real], 7.0)    # rows of no request
+        np.testing.assert_array_equal(lse[~real], 7.0)
+        np.testing.assert_array_equal(np.isnan(out[real]), np.isnan(want[real]))
+        many = self.kind != "fp32" and self.max_new * (self.heads // self.kv_heads) > 32
+        tol = ref.tolerance(want, size, reach, count, self.kind, many)
+        fine = real[..., None] & np.isfinite(want)
+        off = np.abs(out - want)
+        assert (off[fine] <= tol[fine]).all(), (np.nanmax((off / tol)[fine]), np.argwhere(fine & (off > tol))[:4])
+        np.testing.assert_array_equal(out[real[..., None] & np.isinf(want)], want[real[..., None] & np.isinf(want)])
+        fine = real & np.isfinite(want_lse)
+        np.testing.assert_array_equal(lse[real & (want_lse == -np.inf)], -np.inf)
+        off = np.abs(lse - want_lse)
+        assert (off[fine] <= ref.lse_tolerance(want_lse, reach, count)[fine]).all(), np.nanmax(off[fine])
+
+
+EDGES = [0, 1, 15, 16, 17, 31, 32, 33, 64, 127, 300]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads", [(8, 2), (3, 3), (10, 2), (16, 1)])
+@pytest.mark.parametrize("page,layout", [(16, "token"), (64, "head"), (256, "wide")])
+def test_one_token_per_request(kind, heads, kv_heads, page, layout):
+    Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=page, lengths=EDGES, layout=layout, seed=page + heads).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads", [(20, 1), (64, 1), (128, 2)])
+def test_more_heads_per_kv_head_than_a_tile_has_rows(kind, heads, kv_heads):
+    Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=32, lengths=[40, 0, 513], seed=heads).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("lengths", [[20011], [5000, 3, 9000, 0, 700]])
+def test_long_caches_cut_into_pieces(kind, lengths):
+    Problem(kind=kind, heads=8, kv_heads=2, page=64, lengths=lengths, seed=3).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads,new", [(8, 2, [4, 1, 3, 0, 2]), (10, 2, [6, 6, 2, 5, 1]), (4, 4, [1, 9, 16, 0, 33]),
+                                                (8, 2, [70, 1, 33, 0, 8]), (16, 1, [40, 1, 1, 200, 5])])
+def test_new_tokens_attend_causally(kind, heads, kv_heads, new):
+    # (more new tokens than cached keys too: the first ones attend nothing)
+    Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=16, lengths=[70, 2, 33, 5, 530], new=new, spare_rows=2, seed=7).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("n_sink,n_local", [(0, 1), (4, 20), (0, 64), (40, 33), (100, 7), (5, 1 << 30), (1 << 30, 3)])
+@pytest.mark.parametrize("new", [None, [1, 5, 0, 2, 8, 1], [1, 90, 0, 33, 64, 200]])
+def test_sink_and_window(kind, n_sink, n_local, new):
+    Problem(kind=kind, heads=6, kv_heads=2, page=32, lengths=[1, 95, 0, 34, 257, 700], new=new, n_sink=n_sink, n_local=n_local,
+            spare_rows=1 if new else 0, seed=n_sink + n_local % 1000).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("new", [None, [3, 2, 4], [50, 9, 64]])
+def test_table_entries_that_are_no_page(kind, new):
+    bad = [(0, 1, -1), (0, 2, 1 << 30), (1, 0, -2 ** 31), (2, 3, 2 ** 31 - 1), (2, 0, 10 ** 6)]
+    Problem(kind=kind, heads=4, kv_heads=2, page=16, lengths=[90, 12, 64], new=new, bad=bad, seed=5, spare_rows=1 if new else 0).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("new,n_local", [([5, 4, 3], 0), ([5, 4, 3], 6), ([60, 33, 40], 0), ([60, 33, 40], 9)])
+def test_infinities_and_nan_reach_the_rows_that_attend_them_alone(kind, new, n_local):
+    p = Problem(kind=kind, heads=4, kv_heads=2, page=16, lengths=[80, 33, 40], new=new, n_local=n_local, n_sink=1 if n_local else 0, seed=9)
+
+    def place(b, pos):
+        return int(p.table[b, pos // 16]), pos % 16
+    for b, pos, e, value in [(0, 78, 3, "nan"), (0, 75, 90, "inf"), (1, 30, 127, "-inf"), (2, 39, 0, "nan"), (2, 36, 64, "inf")]:
+        pg, at = place(b, pos)
+        p.v[pg, at, b % 2, e] = float("nan") if p.kind == "fp8" else float(value)
+    pg, at = place(1, 32)
+    p.k[pg, at, 0, 5] = float("nan")                     # the last key of request 1: its row alone
+    p.upload()
+    p.check()
+
+
+def test_logits_beyond_the_exponential_s_range():
+    Problem(kind="fp32", heads=4, kv_heads=2, page=16, lengths=[300, 40], spread=300.0, seed=2).check()
+    Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[300, 40], new=[40, 40], spread=300.0, seed=2).check()
+    Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[300, 40], scale=-0.7, spread=3.0, seed=2).check()
+
+
+def test_strided_queries_and_either_form_of_single_tokens():
+    p = Problem(kind="bf16", heads=8, kv_heads=2, page=16, lengths=[300, 40, 1], q_wide=4, seed=4)
+    a, b = p.run(False), p.run(True)
+    np.testing.assert_array_equal(a[0], b[0])
+    np.testing.assert_array_equal(a[1], b[1])
+    p.check()
+
+
+def test_many_requests():
+    rng = np.random.default_rng(1)
+    Problem(kind="bf16", heads=4, kv_heads=1, page=16, lengths=[int(x) for x in rng.integers(0, 90, 333)], seed=1).check()
+    Problem(kind="bf16", heads=4, kv_heads=1, page=16, lengths=[int(x) for x in rng.integers(0, 90, 150)],
+            new=[int(x) for x in rng.integers(0, 12, 150)], seed=1).check()
+
+
+def test_token_counts_are_bounded_by_the_parameters():
+    # token_start promises more than max_new: the first max_new rows are taken, at the positions of the last ones
+    Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[50, 60], new=[9, 3], max_new=4, seed=8).check()
+
+
+def test_lse_joins_attentions_over_disjoint_keys():
+    p = Problem(kind="fp32", heads=4, kv_heads=2, page=16, lengths=[160], seed=6)
+    whole, lse = p.run()
+    parts = []
+    for pages in (slice(0, 4), slice(4, 10)):
+        part = Problem(kind="fp32", heads=4, kv_heads=2, page=16, lengths=[160], seed=6)
+        part.table = np.full_like(p.table, -1)
+        part.table[:, pages] = p.table[:, pages]
+        part.upload()
+        parts.append(part.run())
+    top = np.logaddexp(parts[0][1], parts[1][1])
+    joined = sum(o * np.exp(x - top)[..., None] for o, x in parts)
+    np.testing.assert_allclose(top, lse, atol=2e-6)
+    np.testing.assert_allclose(joined, whole, atol=1e-5)

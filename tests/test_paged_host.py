@@ -1,0 +1,184 @@
+"""The paged calls' host side, without a GPU: sizes, refusals of parameters and arguments, the binding's own checks,
+and the rules by which the work of paged attention is cut."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2410_16179_amd import binding as mp
+
+OK, INVALID, UNSUPPORTED, SMALL, LAUNCH = 0, -1, -2, -3, -4
+
+
+def params(**kw):
+    return mp.make_paged_params(**{**dict(batch=3, n_q_heads=8, n_kv_heads=2, dtype="bf16", page_size=16, max_pages=40, n_pages=100,
+                                          max_tokens=12, max_new=4), **kw})
+
+
+_MEMORY = (ctypes.c_char * 4096)()
+FAKE = ctypes.addressof(_MEMORY) + (-ctypes.addressof(_MEMORY)) % 256
+
+
+def plan(p, **kw):
+    names = ["new_tokens", "lengths", "block_table", "free_pages", "n_free", "lengths_out", "n_free_out", "token_start", "slots", "status"]
+    at = {n: FAKE for n in names} | {"workspace": FAKE, "bytes": 1 << 40} | kw
+    return mp.lib().magicpig_page_plan(ctypes.byref(p), *[at[n] for n in names], at["workspace"], at["bytes"], None)
+
+
+def append(p, **kw):
+    names = ["k_new", "v_new", "slots", "k_scale", "v_scale", "k_pages", "v_pages"]
+    at = {n: FAKE for n in names} | {"k_scale": None, "v_scale": None} | kw
+    return mp.lib().magicpig_page_append(ctypes.byref(p), *[at[n] for n in names], None)
+
+
+def attend(p, **kw):
+    names = ["q", "k_pages", "v_pages", "k_scale", "v_scale", "block_table", "lengths", "token_start", "out", "lse"]
+    at = {n: FAKE for n in names} | {"k_scale": None, "v_scale": None, "workspace": FAKE, "bytes": 1 << 40} | kw
+    return mp.lib().magicpig_paged_attention(ctypes.byref(p), *[at[n] for n in names], at["workspace"], at["bytes"], None)
+
+
+# (a call that gets past the checks fails to launch where there is no GPU; where there is one it is not made)
+accepted = pytest.mark.skipif(torch.cuda.is_available(), reason="the arguments are no device memory")
+
+
+@pytest.mark.parametrize("field,value,status", [
+    ("batch", -1, INVALID), ("batch", 65537, UNSUPPORTED), ("n_q_heads", 0, INVALID), ("n_kv_heads", 0, INVALID), ("n_kv_heads", 3, INVALID),
+    ("n_q_heads", 130, UNSUPPORTED), ("head_dim", 64, UNSUPPORTED), ("head_dim", 256, UNSUPPORTED), ("dtype", 2, UNSUPPORTED),
+    ("kv_dtype", 2, UNSUPPORTED), ("page_size", 0, UNSUPPORTED), ("page_size", 8, UNSUPPORTED), ("page_size", 24, UNSUPPORTED),
+    ("page_size", 2048, UNSUPPORTED), ("page_size", -16, UNSUPPORTED), ("max_pages", 0, INVALID), ("max_pages", (1 << 26) + 1, UNSUPPORTED),
+    ("n_pages", 0, INVALID), ("n_pages", 1 << 31, UNSUPPORTED), ("max_tokens", 0, INVALID), ("max_tokens", (1 << 24) + 1, UNSUPPORTED),
+    ("max_new", 0, INVALID), ("max_new", (1 << 24) + 1, UNSUPPORTED), ("n_sink", -1, INVALID), ("n_sink", (1 << 30) + 1, INVALID),
+    ("n_local", -1, INVALID), ("n_local", (1 << 30) + 1, INVALID), ("scale", math.inf, INVALID), ("scale", math.nan, INVALID)])
+def test_parameters_that_every_call_refuses(field, value, status):
+    p = params()
+    setattr(p, field, value)
+    assert plan(p) == append(p) == attend(p) == status
+    assert mp.magicpig_paged_workspace_bytes(p) == 0
+    assert plan(params(n_q_heads=2048, n_kv_heads=2048)) == UNSUPPORTED
+    assert plan(params(dtype="fp32", kv_dtype="fp8")) == UNSUPPORTED
+    assert mp.lib().magicpig_page_plan(None, *[FAKE] * 11, 0, None) == INVALID
+
+
+def test_more_work_than_a_grid_counts_is_refused():
+    assert attend(params(batch=65536, max_new=1 << 24, max_tokens=1 << 24, n_q_heads=1024, n_kv_heads=1024)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("part,value,status", [("page", -8, INVALID), ("key", 120, INVALID), ("key", 0, INVALID), ("head", -8, INVALID),
+                                               ("page", 4, UNSUPPORTED), ("key", 132, UNSUPPORTED), ("head", 129, UNSUPPORTED),
+                                               ("key", 1 << 26, UNSUPPORTED), ("key", 1 << 40, UNSUPPORTED)])
+def test_pool_strides(which, part, value, status):
+    p = params()
+    setattr(p, f"{which}_stride_{part}", value)
+    assert append(p) == attend(p) == status
+
+
+def test_e4m3_pools_need_rows_on_16_byte_boundaries():
+    p = params(kv_dtype="fp8", k_strides=(16 * 2 * 136, 2 * 136, 136))
+    assert append(p) == attend(p) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("field,value,status", [("token", -8, INVALID), ("head", -8, INVALID), ("token", 4, UNSUPPORTED), ("head", 12, UNSUPPORTED)])
+def test_strides_of_token_arrays(field, value, status):
+    for name, call in (("q", attend), ("k_new", append), ("v_new", append)):
+        p = params()
+        setattr(p, f"{name}_stride_{field}", value)
+        assert call(p) == status
+
+
+def test_missing_and_misaligned_arguments():
+    p = params()
+    for name in ("new_tokens", "lengths", "block_table", "free_pages", "n_free", "lengths_out", "n_free_out", "token_start", "slots", "status"):
+        assert plan(p, **{name: None}) == INVALID
+        assert plan(p, **{name: FAKE + 2}) == INVALID
+    assert plan(p, slots=FAKE + 4) == INVALID
+    for name in ("k_new", "v_new", "slots", "k_pages", "v_pages"):
+        assert append(p, **{name: None}) == INVALID
+        assert append(p, **{name: FAKE + 4}) == INVALID
+    for name in ("q", "k_pages", "v_pages", "block_table", "lengths", "out"):
+        assert attend(p, **{name: None}) == INVALID
+        assert attend(p, **{name: FAKE + 2}) == INVALID
+    for name in ("token_start", "lse", "k_scale"):
+        assert attend(p, **{name: FAKE + 2}) == INVALID
+    assert attend(p, workspace=FAKE + 8) == INVALID
+    # scales belong to e4m3 pools
+    for name in ("k_scale", "v_scale"):
+        assert append(p, **{name: FAKE}) == INVALID and attend(p, **{name: FAKE}) == INVALID
+    # without token_start row b is request b's
+    assert attend(params(batch=13, max_tokens=12), token_start=None) == INVALID
+
+
+def test_workspace():
+    long = params(max_pages=2000)
+    need = mp.magicpig_paged_workspace_bytes(long)
+    assert need > 0
+    assert attend(long, bytes=255) == SMALL and attend(long, workspace=None) == SMALL
+    many = params(batch=5000)
+    assert plan(many, bytes=100) == SMALL and plan(many, workspace=None) == SMALL
+    assert mp.magicpig_paged_workspace_bytes(many) >= 3 * 5001 * 4
+
+
+@accepted
+def test_what_is_accepted_gets_as_far_as_the_launch():
+    assert plan(params()) == append(params()) == attend(params()) == LAUNCH
+    assert plan(params(), workspace=None) == LAUNCH
+    assert attend(params(kv_dtype="fp8"), k_scale=FAKE, v_scale=FAKE, lse=None, token_start=None) == LAUNCH
+    assert attend(params(max_new=1 << 24)) == LAUNCH
+    p = params(max_pages=2000)
+    assert attend(p, bytes=mp.magicpig_paged_workspace_bytes(p)) == LAUNCH
+    assert attend(params(batch=0), block_table=None, lengths=None) == OK
+
+
+def test_struct_layout_matches_header():
+    assert ctypes.sizeof(mp.magicpig_paged_params) == 12 * 4 + 14 * 8
+    assert mp.magicpig_paged_params.n_pages.offset == 48
+    assert mp.magicpig_paged_params.v_new_stride_head.offset == 48 + 13 * 8
+
+
+# ---- the binding's checks (on CPU tensors posing as device ones) -----------------------------------------
+class _Posing(torch.Tensor):
+    device_index = 0
+
+    def get_device(self):
+        return self.device_index
+
+
+def posing(*shape, dtype=torch.int32, device=0):
+    t = torch.zeros(*shape, dtype=dtype).as_subclass(_Posing)
+    t.device_index = device
+    return t
+
+
+def attention_arguments(p):
+    bf = torch.bfloat16
+    return {"q": posing(p.max_tokens, 8, 128, dtype=bf), "k_pages": posing(p.n_pages, 16, 2, 128, dtype=bf),
+            "v_pages": posing(p.n_pages, 16, 2, 128, dtype=bf), "k_scale": None, "v_scale": None, "block_table": posing(3, p.max_pages),
+            "lengths": posing(3), "token_start": posing(4), "out": posing(p.max_tokens, 8, 128, dtype=bf),
+            "lse": posing(p.max_tokens, 8, dtype=torch.float32)}
+
+
+@pytest.mark.parametrize("name,change,says", [
+    ("q", lambda t: posing(11, 8, 128, dtype=torch.bfloat16), "q"), ("q", lambda t: posing(12, 8, 128, dtype=torch.float32), "dtype"),
+    ("q", lambda t: torch.zeros(12, 8, 128, dtype=torch.bfloat16), "GPU"), ("k_pages", lambda t: posing(99, 16, 2, 128, dtype=torch.bfloat16), "k_pages"),
+    ("v_pages", lambda t: posing(100, 16, 2, 128, dtype=torch.bfloat16, device=1), "device"), ("block_table", lambda t: posing(3, 39), "block_table"),
+    ("block_table", lambda t: t.t().contiguous().t(), "contiguous"), ("block_table", lambda t: t.to(torch.int64), "dtype"),
+    ("lengths", lambda t: posing(2), "lengths"), ("lengths", lambda t: None, "missing"), ("token_start", lambda t: posing(3), "token_start"),
+    ("out", lambda t: posing(12, 8, 127, dtype=torch.bfloat16), "out"), ("lse", lambda t: posing(12, 7, dtype=torch.float32), "lse"),
+    ("k_scale", lambda t: posing(1, dtype=torch.float32), "k_scale")])
+def test_binding_refuses_tensors_that_do_not_fit(name, change, says):
+    p = params()
+    got = attention_arguments(p)
+    changed = change(got[name])
+    if isinstance(changed, _Posing) and changed.device_index != 1:
+        changed.device_index = 0
+    got[name] = changed
+    with pytest.raises(mp.MagicpigError, match=says):
+        mp.magicpig_paged_attention(p, **got)
+    with pytest.raises(mp.MagicpigError, match="slots"):
+        mp.magicpig_page_append(p, posing(12, 2, 128, dtype=torch.bfloat16), posing(12, 2, 128, dtype=torch.bfloat16),
+                                posing(11, dtype=torch.int64), None, None, attention_arguments(p)["k_pages"], attention_arguments(p)["v_pages"])
+    with pytest.raises(mp.MagicpigError, match="n_free_out"):
+        mp.magicpig_page_plan(p, posing(3), posing(3), posing(3, 40), posing(100), posing(1), posing(3), posing(0), posing(4),
+                              posing(12, dtype=torch.int64), posing(1))
