@@ -89,19 +89,22 @@ inline bool page_plan_in_one(int batch, int64_t max_tokens) { return batch <= kP
 
 // ---- paged attention ------------------------------------------------------------------------------
 // rows: query rows (new tokens times the query heads of a KV head) that a workgroup takes at once; key_tile:
-// keys by which the work is counted.  tile_tokens, head_blocks: see PagedArgs.  items, pieces, units, slots: at most so many row
+// keys by which the work is counted.  tile_tokens, head_blocks: see PagedArgs.  target: pieces that the work is cut into;
+// min_tiles: key tiles of a piece at least.  items, pieces, units, slots: at most so many row
 // tiles of all KV heads, workgroups, row tiles that are cut, partials.
 struct PagedForm {
   int rows, key_tile, tile_tokens, head_blocks, target, min_tiles;
   int64_t items, pieces, units, slots;
 };
 
-constexpr int kPagedTarget = 3 * kNumCU;     // pieces that the work is cut into (three workgroups per compute unit)
-constexpr int kPagedMinKeys = 256;           // of a piece
+// Up to 32 rows are taken by the form that keeps keys in registers, 16 or 32 at a time; more (bf16) by the one that shares
+// keys among 128 rows through LDS.  float32: always 16.
+constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
+inline int paged_rows(bool fp32, int64_t rows) { return fp32 || rows <= 16 ? 16 : (rows <= 32 ? 32 : kPagedManyRows); }
 
 // Row tiles of all KV heads and requests, whatever token counts (each at most max_new) the device memory holds.
 inline int64_t paged_most_items(int batch, int kv_heads, int group, bool fp32, int max_new) {
-  const int rows = !fp32 && (int64_t)max_new * group > 16 ? 32 : 16;
+  const int rows = paged_rows(fp32, (int64_t)max_new * group);
   const int64_t tokens = group <= rows ? rows / group : 1, blocks = group <= rows ? 1 : (group + rows - 1) / rows;
   return (int64_t)batch * ((max_new + tokens - 1) / tokens) * blocks * kv_heads;
 }
@@ -110,13 +113,13 @@ inline int64_t paged_most_items(int batch, int kv_heads, int group, bool fp32, i
 inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64_t max_tokens, int max_new, bool starts, int64_t max_len,
                             int n_sink, int n_local) {
   PagedForm f{};
-  const int64_t rows = (int64_t)max_new * group;
-  f.rows = !fp32 && rows > 16 ? 32 : 16;
-  f.key_tile = fp32 ? 16 : 32;
+  f.rows = paged_rows(fp32, (int64_t)max_new * group);
+  const bool many = f.rows == kPagedManyRows;
+  f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : 32);
   f.tile_tokens = group <= f.rows ? f.rows / group : 1;
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
-  f.target = kPagedTarget;
-  f.min_tiles = kPagedMinKeys / f.key_tile;
+  f.target = many ? 2 * kNumCU : 3 * kNumCU;               // workgroups that are resident at once
+  f.min_tiles = (many ? 512 : 256) / f.key_tile;
   int64_t tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens);
   if (starts && max_tokens / f.tile_tokens + batch < tiles) tiles = max_tokens / f.tile_tokens + batch;
   f.items = tiles * f.head_blocks * kv_heads;

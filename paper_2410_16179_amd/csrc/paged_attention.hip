@@ -1,61 +1,10 @@
 // Exact attention over a paged key-value cache: the form for few rows per KV head, and the joining of pieces.
-#include "paged_common.h"
+#include "paged_device.h"
 
 #include <type_traits>
 
 namespace mp {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef const int __attribute__((address_space(4))) * const_i32_ptr;
-
-constexpr int kPartialRow = kPartialStride;   // floats of a row's partial: 128 outputs, maximum, sum, pad
-
-// Eight e4m3 bytes as eight bf16 (exact), two per instruction.
-__device__ inline u32x4 e4m3_to_bf16(u32x2 w) {
-  u32x4 r;
-  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false));
-  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, true));
-  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, false));
-  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, true));
-  return r;
-}
-
-__device__ inline uint32_t pack_bf16(float lo, float hi) {
-  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
-  return __builtin_bit_cast(uint32_t, v);
-}
-__device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Loads through a buffer descriptor, not kept in the caches (nt): a step reads a row once.
-constexpr int kBufferWord3 = 0x00020000;
-constexpr int kNonTemporal = 2;
-__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
-  to = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, kNonTemporal));
-}
-__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
-  to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, kNonTemporal));
-}
-
-// Clears the infinities and NaN among a lane's V elements (float32, or two bf16 a register).
-template <bool F32>
-__device__ inline void clear_not_finite(u32x4 (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t w = v[i][e];
-      if constexpr (F32) v[i][e] = (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
-      else v[i][e] = ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
-    }
-}
 
 // ---- few rows ------------------------------------------------------------------------------------
 // A wavefront attends tiles of KT keys with up to 16 NR query rows.  Scores are formed transposed,
@@ -83,12 +32,6 @@ struct FewRows {
   f32x4 o[NR][8];
   float m[NR], l[NR];
   Raw kf[kFrags], vf[kFrags];
-};
-
-// The pages of a tile's 16-key halves: ids as the table has them.
-template <int KT>
-struct TilePages {
-  int id[KT / 16];
 };
 
 template <int ET, int NR>
@@ -157,16 +100,10 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     }
   };
   auto page_ok = [&](int id) { return (uint32_t)id < (uint32_t)a.n_pages; };
-  // Rows are read through buffer descriptors of 16 keys, `valid` of which are there: the others lie beyond the descriptor's
-  // end and read as zeros, without an access.
-  auto rows16 = [&](const char* pool, int64_t page_stride, uint32_t key_stride, int id, int key, int valid) {
-    const char* base = pool + (valid ? id : 0) * page_stride + (uint32_t)(key & page_mask) * key_stride;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, valid * key_stride, kBufferWord3);
-  };
   auto request_k = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
-      const auto rows = rows16(kbase, a.k_page * kElem, k_key, p.id[h], key0 + 16 * h, valid[h]);
+      const auto rows = rows16(kbase, a.k_page * kElem, k_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
 #pragma unroll
       for (int s = 0; s < 8 / F::kHalves; ++s)
         load_once(rows, k_lane + (kF32 ? 64 : 32 * kElem) * s, f.kf[h * (8 / F::kHalves) + s]);
@@ -175,7 +112,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   auto request_v = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
-      const auto rows = rows16(vbase, a.v_page * kElem, v_key, p.id[h], key0 + 16 * h, valid[h]);
+      const auto rows = rows16(vbase, a.v_page * kElem, v_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (kF32) {
@@ -395,7 +332,10 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
           for (int d = 0; d < (kF32 ? 2 : 1); ++d) vb[kF32 ? 2 * i + d : 4 * h + i] &= keep;
         }
       }
-      if (CAREFUL) clear_not_finite<kF32>(vb);
+      if (CAREFUL) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) vb[i] = finite_part<kF32>(vb[i]);
+      }
       add_values(s, vb);
       if (!CAREFUL) continue;
       // what was cleared, added key by key to the rows that attend the key; the weights change lanes through LDS
@@ -571,14 +511,18 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
   paged_write_row<FP32>(a, (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h, e0, out, top, sum, a.v_scale ? a.v_scale[pc.g] : 1.f);
 }
 
+template <bool FP32, int KT, int R>
+void launch_join(const PagedArgs& a, const PagedForm& form, hipStream_t s) {
+  if (form.units == 0) return;
+  const int rows = a.head_blocks > 1 ? form.rows : (a.tile_tokens < a.max_new ? a.tile_tokens : a.max_new) * a.G;
+  paged_join_kernel<FP32, KT, R><<<dim3((unsigned)form.units, rows), 256, 0, s>>>(a);
+}
+
 template <int ET, int NR>
 hipError_t launch_few_rows(const PagedArgs& a, const PagedForm& form, hipStream_t s) {
   constexpr int KT = FewRows<ET, NR>::kTile;
   paged_few_rows_kernel<ET, NR><<<(unsigned)form.pieces, 256, 0, s>>>(a);
-  if (form.units > 0) {
-    const int rows = a.head_blocks > 1 ? form.rows : (a.tile_tokens < a.max_new ? a.tile_tokens : a.max_new) * a.G;
-    paged_join_kernel<ET == kFP32, KT, 16 * NR><<<dim3((unsigned)form.units, rows), 256, 0, s>>>(a);
-  }
+  launch_join<ET == kFP32, KT, 16 * NR>(a, form, s);
   return hipGetLastError();
 }
 
@@ -586,6 +530,11 @@ hipError_t launch_few_rows(const PagedArgs& a, const PagedForm& form, hipStream_
 
 hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s) {
   if (element == kFP32) return launch_few_rows<kFP32, 1>(a, form, s);
+  if (form.rows == kPagedManyRows) {
+    launch_paged_many_rows(a, element == kFP8, form, s);
+    launch_join<false, kPagedManyKeys, kPagedManyRows>(a, form, s);
+    return hipGetLastError();
+  }
   if (form.rows == 16) return element == kFP8 ? launch_few_rows<kFP8, 1>(a, form, s) : launch_few_rows<kBF16, 1>(a, form, s);
   return element == kFP8 ? launch_few_rows<kFP8, 2>(a, form, s) : launch_few_rows<kBF16, 2>(a, form, s);
 }

@@ -195,6 +195,7 @@ __device__ inline void paged_write_row(const PagedArgs& a, int64_t row, int e0, 
 
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s);
 hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s);
+void launch_paged_many_rows(const PagedArgs& a, bool fp8, const PagedForm& form, hipStream_t s);
 hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s);
 
 }  // namespace mp

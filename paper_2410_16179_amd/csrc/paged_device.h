@@ -1,0 +1,76 @@
+// Pieces shared by the kernels of paged attention: matrix products, conversions, loads of pool rows.
+#pragma once
+#include "paged_common.h"
+
+namespace mp {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef const int __attribute__((address_space(4))) * const_i32_ptr;
+
+constexpr int kPartialRow = kPartialStride;   // floats of a row's partial: 128 outputs, maximum, sum, pad
+
+// Eight e4m3 bytes as eight bf16 (exact), two per instruction.
+__device__ inline u32x4 e4m3_to_bf16(u32x2 w) {
+  u32x4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, true));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, false));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, true));
+  return r;
+}
+
+__device__ inline uint32_t pack_bf16(float lo, float hi) {
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Loads through a buffer descriptor, not kept in the caches (nt): a step reads a row once.
+constexpr int kBufferWord3 = 0x00020000;
+constexpr int kNonTemporal = 2;
+__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
+  to = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, kNonTemporal));
+}
+__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
+  to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, kNonTemporal));
+}
+// The same, kept: workgroups of other row tiles read the row too.
+__device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
+  to = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0));
+}
+__device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
+  to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, 0));
+}
+
+// w without infinities and NaN: a float32, or two bf16.
+template <bool F32>
+__device__ inline uint32_t finite_part(uint32_t w) {
+  if constexpr (F32) return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+  return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+}
+template <bool F32>
+__device__ inline u32x4 finite_part(u32x4 w) {
+  return u32x4{finite_part<F32>(w.x), finite_part<F32>(w.y), finite_part<F32>(w.z), finite_part<F32>(w.w)};
+}
+
+// The pages of a tile, one for every 16 keys: ids as the table has them.
+template <int KT>
+struct TilePages {
+  int id[KT / 16];
+};
+
+// Descriptor of 16 keys' rows of a pool, from key `at` of page `id` on, `valid` of which are there: the others lie beyond the
+// descriptor's end and read as zeros, without an access.  Strides in bytes.
+__device__ inline __amdgpu_buffer_rsrc_t rows16(const char* pool, int64_t page_stride, uint32_t key_stride, int id, int at, int valid) {
+  const char* base = pool + (valid ? id : 0) * page_stride + (uint32_t)at * key_stride;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, valid * key_stride, kBufferWord3);
+}
+
+}  // namespace mp

@@ -156,6 +156,13 @@ def test_new_tokens_attend_causally(kind, heads, kv_heads, new):
     Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=16, lengths=[70, 2, 33, 5, 530], new=new, spare_rows=2, seed=7).check()
 
 
+@pytest.mark.parametrize("kind,layout,page", [("bf16", "token", 16), ("bf16", "wide", 128), ("fp8", "head", 32), ("fp32", "head", 64)])
+@pytest.mark.parametrize("lengths,new,n_local", [([6000, 300, 1030], [150, 40, 129], 0), ([6000, 300, 1030], [150, 40, 129], 700), ([515], [515], 0)])
+def test_chunks_of_prompts(kind, layout, page, lengths, new, n_local):
+    Problem(kind=kind, heads=4, kv_heads=1, page=page, layout=layout, lengths=lengths, new=new, n_local=n_local, n_sink=3 if n_local else 0,
+            spare_rows=1, seed=12).check()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
 @pytest.mark.parametrize("n_sink,n_local", [(0, 1), (4, 20), (0, 64), (40, 33), (100, 7), (5, 1 << 30), (1 << 30, 3)])
 @pytest.mark.parametrize("new", [None, [1, 5, 0, 2, 8, 1], [1, 90, 0, 33, 64, 200]])
@@ -190,7 +197,8 @@ def test_infinities_and_nan_reach_the_rows_that_attend_them_alone(kind, new, n_l
 def test_logits_beyond_the_exponential_s_range():
     Problem(kind="fp32", heads=4, kv_heads=2, page=16, lengths=[300, 40], spread=300.0, seed=2).check()
     Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[300, 40], new=[40, 40], spread=300.0, seed=2).check()
-    Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[300, 40], scale=-0.7, spread=3.0, seed=2).check()
+    for new in (None, [40, 40]):
+        Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[300, 40], new=new, scale=-0.7, spread=3.0, seed=2).check()
 
 
 def test_strided_queries_and_either_form_of_single_tokens():
