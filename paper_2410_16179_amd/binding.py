@@ -53,6 +53,10 @@ class magicpig_paged_params(ctypes.Structure):
         ("v_new_stride_token", ctypes.c_int64), ("v_new_stride_head", ctypes.c_int64),
     ]
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("sizes", None)                     # (what _paged_sizes worked out from the fields)
+        super().__setattr__(name, value)
+
 
 EXPORTS = (
     "magicpig_code_words_per_key", "magicpig_code_words_per_query", "magicpig_key_code_bytes",
@@ -318,54 +322,81 @@ def make_paged_params(*, batch, n_q_heads, n_kv_heads, dtype, page_size, max_pag
 _DTYPES = {MAGICPIG_BF16: torch.bfloat16, MAGICPIG_FP32: torch.float32}
 
 
-def _extent(n, *strides_and_sizes) -> int:
-    """Elements from the first to the last of an array of rows of n elements with these (stride, size) dimensions."""
-    return n + sum(stride * (size - 1) for stride, size in strides_and_sizes)
+class _PagedSizes:
+    """What the paged calls' tensors have to be by a parameter block: types, and elements from the first to the last one used."""
+
+    def __init__(self, p):
+        reach = lambda *dims: p.head_dim + sum(stride * (size - 1) for stride, size in dims)
+        self.dtype = _DTYPES.get(p.dtype)
+        self.pool_dtype = (torch.float8_e4m3fn, torch.uint8) if p.kv_dtype == MAGICPIG_KV_FP8_E4M3 else (self.dtype,)
+        self.batch, self.heads, self.n_pages, self.tokens, self.table = p.batch, p.n_kv_heads, p.n_pages, p.max_tokens, p.batch * p.max_pages
+        self.k_pages = reach((p.k_stride_page, p.n_pages), (p.k_stride_key, p.page_size), (p.k_stride_head, p.n_kv_heads))
+        self.v_pages = reach((p.v_stride_page, p.n_pages), (p.v_stride_key, p.page_size), (p.v_stride_head, p.n_kv_heads))
+        self.q = reach((p.q_stride_token, p.max_tokens), (p.q_stride_head, p.n_q_heads))
+        self.k_new = reach((p.k_new_stride_token, p.max_tokens), (p.k_new_stride_head, p.n_kv_heads))
+        self.v_new = reach((p.v_new_stride_token, p.max_tokens), (p.v_new_stride_head, p.n_kv_heads))
+        self.lse = p.max_tokens * p.n_q_heads
+        self.out = self.lse * p.head_dim
+        self.params = ctypes.byref(p)
 
 
-def _expect(name, t, dtype, elements, device, optional=False, dense=True):
-    """dense: the call reads the tensor as one run of elements; otherwise by the strides of the parameters."""
-    if t is None:
-        if optional:
-            return
-        raise MagicpigError(f"{name} is missing")
-    if t.get_device() != device:
-        raise MagicpigError(f"{name} is on device {t.device}, the call runs on cuda:{device}")
-    if t.dtype is not dtype and t.dtype not in (dtype if isinstance(dtype, tuple) else ()):
-        raise MagicpigError(f"{name} has dtype {t.dtype}, not {dtype}")
-    if dense:
-        if not t.is_contiguous():
+def _paged_sizes(p) -> _PagedSizes:
+    s = p.__dict__.get("sizes")                              # (dropped when a field is set)
+    if s is None:
+        s = p.__dict__["sizes"] = _PagedSizes(p)
+    return s
+
+
+def _dense(t, device, dtype, elements) -> bool:
+    """Whether t is read as it should be where the call takes it for one run of elements."""
+    return t.get_device() == device and t.dtype is dtype and t.numel() >= elements and t.is_contiguous()
+
+
+def _strided(t, device, dtypes, elements) -> bool:
+    """The same where the call goes by the strides of the parameters: so many elements lie behind the tensor's first one."""
+    if t.get_device() != device or t.dtype not in dtypes:
+        return False
+    return t.untyped_storage().nbytes() >= (t.storage_offset() + elements) * t.element_size()
+
+
+def _refuse(device, **tensors):
+    """Says what is wrong: name=(tensor, dtypes, elements, dense, optional)."""
+    for name, (t, dtypes, elements, dense, optional) in tensors.items():
+        if t is None:
+            if optional:
+                continue
+            raise MagicpigError(f"{name} is missing")
+        if t.get_device() != device:
+            raise MagicpigError(f"{name} is on device {t.device}, the call runs on cuda:{device}")
+        if t.dtype not in dtypes:
+            raise MagicpigError(f"{name} has dtype {t.dtype}, not {dtypes[0]}")
+        if dense and not t.is_contiguous():
             raise MagicpigError(f"{name} is not contiguous")
-        if t.numel() < elements:
+        if dense and t.numel() < elements:
             raise MagicpigError(f"{name} has {t.numel()} elements, the parameters say {elements}")
-    elif t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < elements:
-        raise MagicpigError(f"{name} ends before the {elements} elements that the parameters' strides reach")
+        if not dense and not _strided(t, device, dtypes, elements):
+            raise MagicpigError(f"{name} ends before the {elements} elements that the parameters' strides reach")
+    raise MagicpigError("a tensor does not fit the parameters")
 
 
-def _device(t) -> int:
-    device = t.get_device() if t is not None else -1
+def _paged_device(t, workspace=None) -> int:
+    device = -1 if t is None else t.get_device()
     if device < 0:
         raise MagicpigError("the paged calls take tensors on a GPU")
+    if workspace is not None and workspace.get_device() != device:
+        raise MagicpigError(f"the workspace is on device {workspace.device}, the call runs on cuda:{device}")
     return device
 
 
-def _pool_dtype(p):
-    return (torch.float8_e4m3fn, torch.uint8) if p.kv_dtype == MAGICPIG_KV_FP8_E4M3 else _DTYPES.get(p.dtype)
-
-
-def _pool_elements(p, page, key, head) -> int:
-    return _extent(p.head_dim, (page, p.n_pages), (key, p.page_size), (head, p.n_kv_heads))
-
-
-def _on_device(device, workspace, call):
-    """Runs call(stream) with the tensors' device current, on its current stream."""
-    if workspace is not None and workspace.get_device() != device:
-        raise MagicpigError(f"the workspace is on device {workspace.device}, the call runs on cuda:{device}")
+def _paged_call(device, fn, *args) -> None:
+    """fn(*args, stream) with the tensors' device current, on that device's current stream."""
     if device == torch.cuda.current_device():
-        _check(call(torch.cuda.current_stream(device).cuda_stream))
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
-            _check(call(torch.cuda.current_stream(device).cuda_stream))
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    if status != 0:
+        _check(status)
 
 
 def magicpig_paged_workspace_bytes(params) -> int:
@@ -374,50 +405,62 @@ def magicpig_paged_workspace_bytes(params) -> int:
 
 def magicpig_page_plan(params, new_tokens, lengths, block_table, free_pages, n_free, lengths_out, n_free_out, token_start,
                        slots, status, workspace=None) -> None:
-    p, device, i32 = params, _device(lengths), torch.int32
-    for name, t, dtype, n in (("new_tokens", new_tokens, i32, p.batch), ("lengths", lengths, i32, p.batch),
-                              ("block_table", block_table, i32, p.batch * p.max_pages), ("free_pages", free_pages, i32, p.n_pages),
-                              ("n_free", n_free, i32, 1), ("lengths_out", lengths_out, i32, p.batch),
-                              ("n_free_out", n_free_out, i32, 1), ("token_start", token_start, i32, p.batch + 1),
-                              ("slots", slots, torch.int64, p.max_tokens), ("status", status, i32, 1)):
-        _expect(name, t, dtype, n, device)
-    _on_device(device, workspace, lambda stream: lib().magicpig_page_plan(
-        ctypes.byref(p), new_tokens.data_ptr(), lengths.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
-        n_free.data_ptr(), lengths_out.data_ptr(), n_free_out.data_ptr(), token_start.data_ptr(), slots.data_ptr(),
-        status.data_ptr(), _ptr(workspace), _nbytes(workspace), stream))
+    s, device, i32 = _paged_sizes(params), _paged_device(lengths, workspace), torch.int32
+    n, of = s.batch, lambda t, count: (t, (i32,), count, True, False)
+    try:
+        fits = (_dense(new_tokens, device, i32, n) and _dense(lengths, device, i32, n) and _dense(block_table, device, i32, s.table)
+                and _dense(free_pages, device, i32, s.n_pages) and _dense(n_free, device, i32, 1) and _dense(lengths_out, device, i32, n)
+                and _dense(n_free_out, device, i32, 1) and _dense(token_start, device, i32, n + 1)
+                and _dense(slots, device, torch.int64, s.tokens) and _dense(status, device, i32, 1))
+    except AttributeError:                                   # (None)
+        fits = False
+    if not fits:
+        _refuse(device, new_tokens=of(new_tokens, n), lengths=of(lengths, n), block_table=of(block_table, s.table),
+                free_pages=of(free_pages, s.n_pages), n_free=of(n_free, 1), lengths_out=of(lengths_out, n), n_free_out=of(n_free_out, 1),
+                token_start=of(token_start, n + 1), slots=(slots, (torch.int64,), s.tokens, True, False), status=of(status, 1))
+    _paged_call(device, lib().magicpig_page_plan, s.params, new_tokens.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
+                free_pages.data_ptr(), n_free.data_ptr(), lengths_out.data_ptr(), n_free_out.data_ptr(), token_start.data_ptr(),
+                slots.data_ptr(), status.data_ptr(), _ptr(workspace), _nbytes(workspace))
 
 
 def magicpig_page_append(params, k_new, v_new, slots, k_scale, v_scale, k_pages, v_pages) -> None:
-    p, device, at = params, _device(k_pages), _DTYPES.get(params.dtype)
-    _expect("k_new", k_new, at, _extent(p.head_dim, (p.k_new_stride_token, p.max_tokens), (p.k_new_stride_head, p.n_kv_heads)), device, dense=False)
-    _expect("v_new", v_new, at, _extent(p.head_dim, (p.v_new_stride_token, p.max_tokens), (p.v_new_stride_head, p.n_kv_heads)), device, dense=False)
-    _expect("slots", slots, torch.int64, p.max_tokens, device)
-    _expect("k_scale", k_scale, torch.float32, p.n_kv_heads, device, optional=True)
-    _expect("v_scale", v_scale, torch.float32, p.n_kv_heads, device, optional=True)
-    _expect("k_pages", k_pages, _pool_dtype(p), _pool_elements(p, p.k_stride_page, p.k_stride_key, p.k_stride_head), device, dense=False)
-    _expect("v_pages", v_pages, _pool_dtype(p), _pool_elements(p, p.v_stride_page, p.v_stride_key, p.v_stride_head), device, dense=False)
-    _on_device(device, None, lambda stream: lib().magicpig_page_append(
-        ctypes.byref(p), k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), _ptr(k_scale), _ptr(v_scale),
-        k_pages.data_ptr(), v_pages.data_ptr(), stream))
+    s, device, f32 = _paged_sizes(params), _paged_device(k_pages), torch.float32
+    try:
+        fits = (_strided(k_new, device, (s.dtype,), s.k_new) and _strided(v_new, device, (s.dtype,), s.v_new)
+                and _dense(slots, device, torch.int64, s.tokens) and _strided(k_pages, device, s.pool_dtype, s.k_pages)
+                and _strided(v_pages, device, s.pool_dtype, s.v_pages) and (k_scale is None or _dense(k_scale, device, f32, s.heads))
+                and (v_scale is None or _dense(v_scale, device, f32, s.heads)))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(device, k_new=(k_new, (s.dtype,), s.k_new, False, False), v_new=(v_new, (s.dtype,), s.v_new, False, False),
+                slots=(slots, (torch.int64,), s.tokens, True, False), k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False),
+                v_pages=(v_pages, s.pool_dtype, s.v_pages, False, False), k_scale=(k_scale, (f32,), s.heads, True, True),
+                v_scale=(v_scale, (f32,), s.heads, True, True))
+    _paged_call(device, lib().magicpig_page_append, s.params, k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), _ptr(k_scale),
+                _ptr(v_scale), k_pages.data_ptr(), v_pages.data_ptr())
 
 
 def magicpig_paged_attention(params, q, k_pages, v_pages, k_scale, v_scale, block_table, lengths, token_start, out, lse=None,
                              workspace=None) -> None:
-    p, device, at = params, _device(q), _DTYPES.get(params.dtype)
-    _expect("q", q, at, _extent(p.head_dim, (p.q_stride_token, p.max_tokens), (p.q_stride_head, p.n_q_heads)), device, dense=False)
-    _expect("k_pages", k_pages, _pool_dtype(p), _pool_elements(p, p.k_stride_page, p.k_stride_key, p.k_stride_head), device, dense=False)
-    _expect("v_pages", v_pages, _pool_dtype(p), _pool_elements(p, p.v_stride_page, p.v_stride_key, p.v_stride_head), device, dense=False)
-    _expect("k_scale", k_scale, torch.float32, p.n_kv_heads, device, optional=True)
-    _expect("v_scale", v_scale, torch.float32, p.n_kv_heads, device, optional=True)
-    _expect("block_table", block_table, torch.int32, p.batch * p.max_pages, device)
-    _expect("lengths", lengths, torch.int32, p.batch, device)
-    _expect("token_start", token_start, torch.int32, p.batch + 1, device, optional=True)
-    _expect("out", out, at, p.max_tokens * p.n_q_heads * p.head_dim, device)
-    _expect("lse", lse, torch.float32, p.max_tokens * p.n_q_heads, device, optional=True)
-    _on_device(device, workspace, lambda stream: lib().magicpig_paged_attention(
-        ctypes.byref(p), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale), _ptr(v_scale),
-        block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start), out.data_ptr(), _ptr(lse), _ptr(workspace),
-        _nbytes(workspace), stream))
+    s, device, i32, f32 = _paged_sizes(params), _paged_device(q, workspace), torch.int32, torch.float32
+    try:
+        fits = (_strided(q, device, (s.dtype,), s.q) and _strided(k_pages, device, s.pool_dtype, s.k_pages)
+                and _strided(v_pages, device, s.pool_dtype, s.v_pages) and _dense(block_table, device, i32, s.table)
+                and _dense(lengths, device, i32, s.batch) and (token_start is None or _dense(token_start, device, i32, s.batch + 1))
+                and _dense(out, device, s.dtype, s.out) and (lse is None or _dense(lse, device, f32, s.lse))
+                and (k_scale is None or _dense(k_scale, device, f32, s.heads)) and (v_scale is None or _dense(v_scale, device, f32, s.heads)))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(device, q=(q, (s.dtype,), s.q, False, False), k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False),
+                v_pages=(v_pages, s.pool_dtype, s.v_pages, False, False), k_scale=(k_scale, (f32,), s.heads, True, True),
+                v_scale=(v_scale, (f32,), s.heads, True, True), block_table=(block_table, (i32,), s.table, True, False),
+                lengths=(lengths, (i32,), s.batch, True, False), token_start=(token_start, (i32,), s.batch + 1, True, True),
+                out=(out, (s.dtype,), s.out, True, False), lse=(lse, (f32,), s.lse, True, True))
+    _paged_call(device, lib().magicpig_paged_attention, s.params, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale),
+                _ptr(v_scale), block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start), out.data_ptr(), _ptr(lse), _ptr(workspace),
+                _nbytes(workspace))
 
 
 # ---- buffer helpers (allocation and layout only) ---------------------------------------------

@@ -136,6 +136,8 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
     f.slots = f.items * most < cut ? f.items * most : cut;
     f.units = f.items < f.target ? f.items : f.target;
   }
+  // (pieces are dealt to the eight XCDs in rounds of eight)
+  if (!many) f.pieces = (f.pieces / kv_heads + 7) / 8 * 8 * kv_heads;
   return f;
 }
 

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   __shared__ float joined[4][R][kPartialRow];
 
   PagedPiece pc;
-  if (!paged_locate<KT, false>(a, blockIdx.x, pc)) return;
+  if (!paged_locate<KT, kPieces>(a, blockIdx.x, pc)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, u = lane >> 4;
   const int len = pc.r.len, tokens = pc.r.tokens;
@@ -451,7 +451,7 @@ template <bool FP32, int KT, int R>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
   __shared__ float joined[8][kPartialRow];
   PagedPiece pc;
-  if (!paged_locate<KT, true>(a, blockIdx.x, pc)) return;
+  if (!paged_locate<KT, kCutItems>(a, blockIdx.x, pc)) return;
   const int row = blockIdx.y;
   const int tt = pc.tile / a.head_blocks, hb = pc.tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, pc.r.tokens) - 1;

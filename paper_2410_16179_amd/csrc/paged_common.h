@@ -115,11 +115,24 @@ __device__ inline int wave_prefix(int v, int lane) {
   return v;
 }
 
-// MERGE false: piece `index` of all; true: item `index` of those that are cut.  Called by whole wavefronts with
-// one index; false where there is none.
-template <int KT, bool MERGE>
+// Which workgroup takes what.  kPieces: all pieces, the KV heads of a piece on one XCD (workgroups go to the eight XCDs in turn): in
+// pools that store keys token by token its heads' rows are neighbours.  kPiecesByHead: a KV head's pieces on one XCD
+// (where the number of KV heads goes with eight), whose L2 then serves the row tiles that read the same keys.  kCutItems: the items
+// that are cut, for the join.
+enum { kPieces, kPiecesByHead, kCutItems };
+
+// What workgroup `index` takes; called by whole wavefronts, false where there is nothing.
+template <int KT, int WHAT>
 __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& out) {
   const int lane = threadIdx.x & 63;
+  if (WHAT == kPieces) {
+    const int i = index >> 3;
+    out.g = i % a.Hkv;
+    index = (i / a.Hkv) * 8 + (index & 7);
+  } else {
+    out.g = index % a.Hkv;
+    index /= a.Hkv;
+  }
   float total = 0.f;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
@@ -137,29 +150,26 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
     PagedRequest r{0, 0, 0};
-    int items = 0, pieces = 1;
+    int tiles = 0, pieces = 1;
     if (b < a.batch) {
       r = paged_request(a, b);
-      items = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks * a.Hkv;
+      tiles = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
       pieces = (paged_charge<KT>(a, r.len) + piece_tiles - 1) / piece_tiles;
     }
-    const int cut = pieces > 1 ? items * pieces : 0;
-    const int count = MERGE ? (pieces > 1 ? items : 0) : items * pieces;
+    const int cut = pieces > 1 ? tiles * pieces : 0;
+    const int count = WHAT == kCutItems ? (pieces > 1 ? tiles : 0) : tiles * pieces;
     const int upto = wave_prefix(count, lane), slots = wave_prefix(cut, lane);
     const uint64_t found = __ballot(base + upto > index);
     if (found) {
       const int f = __ffsll((unsigned long long)found) - 1;
       auto at = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-      int i = index - base - at(upto - count);
+      const int i = index - base - at(upto - count), row_tiles = at(tiles);
       out.b = b0 + f;
       out.r.len = at(r.len); out.r.tokens = at(r.tokens); out.r.row = at(r.row);
       out.pieces = at(pieces);
-      const int tiles = at(items) / a.Hkv;
-      out.g = i % a.Hkv;
-      i /= a.Hkv;
-      out.tile = tiles - 1 - i % tiles;                  // (the last row tile has most keys: first)
-      out.piece = MERGE ? 0 : i / tiles;
-      out.slot = slot_base + at(slots - cut) + (out.tile * a.Hkv + out.g) * out.pieces;
+      out.piece = WHAT == kCutItems ? 0 : i / row_tiles;
+      out.tile = row_tiles - 1 - i % row_tiles;          // (the last row tile has most keys: first)
+      out.slot = (slot_base + at(slots - cut) + out.tile * out.pieces) * a.Hkv + out.g * out.pieces;
       return true;
     }
     base += __builtin_amdgcn_readlane(upto, 63);
