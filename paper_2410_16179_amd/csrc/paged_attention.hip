@@ -25,13 +25,15 @@ struct FewRows {
   static constexpr bool kF32 = ET == kFP32;
   static constexpr int kTile = kF32 ? 16 : 32;           // keys per tile
   static constexpr int kHalves = kTile / 16;
-  static constexpr int kFrags = 8;                       // K fragments per tile, and V fragments
+  static constexpr int kFrags = 8;                       // loads of a lane per tile for V, and for K, which e4m3 takes 16 elements at a time
+  static constexpr int kKeyFrags = ET == kFP8 ? 4 : 8;
   typedef typename std::conditional<ET == kFP8, u32x2, u32x4>::type Raw;
 
   u32x4 q[NR][kF32 ? 8 : 4];                             // query rows, as the B operand
   f32x4 o[NR][8];
   float m[NR], l[NR];
-  Raw kf[kFrags], vf[kFrags];
+  u32x4 kf[kKeyFrags];
+  Raw vf[kFrags];
 };
 
 template <int ET, int NR>
@@ -70,8 +72,9 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     for (int s = 0; s < (kF32 ? 8 : 4); ++s) {
       f.q[n][s] = u32x4{0, 0, 0, 0};
       if (ok) {
-        if (kF32) f.q[n][s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(a.q) + at + 16 * s + 4 * u);
-        else f.q[n][s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + at + 32 * s + 8 * u);
+        const int e = kF32 ? 64 * (s >> 2) + 16 * u + 4 * (s & 3) : 32 * u + 8 * s;
+        if (kF32) f.q[n][s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(a.q) + at + e);
+        else f.q[n][s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + at + e);
       }
     }
   }
@@ -86,8 +89,12 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)pc.g * a.v_head * kElem;
   const int page_mask = (1 << a.page_shift) - 1;
   const uint32_t k_key = (uint32_t)a.k_key * kElem, v_key = (uint32_t)a.v_key * kElem;
-  // this lane's place in 16 keys: of K key c, of V the keys 4u .. 4u + 3
-  const uint32_t k_lane = c * k_key + (kF32 ? 16 * u : 8 * u * kElem);
+  // This lane's place in 16 keys.  K: a quad of lanes takes keys 4 (c / 4) + i, one (e4m3: two) at a time, of which each lane
+  // 16 bytes; V: keys 4u .. 4u + 3.
+  const int quad = c >> 2, in_quad = c & 3;
+  const bool odd = c & 1, upper = c & 2;
+  const uint32_t k_lane = (ET == kFP8 ? 4 * quad + (in_quad >> 1) : 4 * quad) * k_key +
+                          (ET == kFP8 ? 32 * u + 16 * (in_quad & 1) : 64 * u + 16 * in_quad);
   const uint32_t v_lane = 4 * u * v_key + (kF32 ? 16 * c : 8 * c * kElem);
 
   auto tile_key = [&](int v) { return (v < span.sink ? v : v + span.skip) * KT; };
@@ -105,8 +112,10 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     for (int h = 0; h < F::kHalves; ++h) {
       const auto rows = rows16(kbase, a.k_page * kElem, k_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
 #pragma unroll
-      for (int s = 0; s < 8 / F::kHalves; ++s)
-        load_once(rows, k_lane + (kF32 ? 64 : 32 * kElem) * s, f.kf[h * (8 / F::kHalves) + s]);
+      for (int i = 0; i < F::kKeyFrags / F::kHalves; ++i) {
+        const uint32_t at = ET == kFP8 ? 2 * i * k_key : (i & 3) * k_key + 256 * (i >> 2);
+        load_once(rows, k_lane + at, f.kf[h * (F::kKeyFrags / F::kHalves) + i]);
+      }
     }
   };
   auto request_v = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
@@ -126,27 +135,45 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   };
   constexpr int kScores = 4 * F::kHalves;                // of a lane: key 16 (i / 4) + 4 u + i % 4 of the tile is number i
   auto scores = [&](float (&s)[NR][kScores]) {
+    // a key per lane: its elements 32 u .. 32 u + 31 (float32: 16 u .. 16 u + 15 of both halves of the row)
+    if constexpr (ET == kFP8) {
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
+      for (int h = 0; h < 2; ++h) join_halves(f.kf[2 * h], f.kf[2 * h + 1], upper);
+    } else {
 #pragma unroll
-      for (int h = 0; h < F::kHalves; ++h) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (kF32) {
+      for (int h = 0; h < 2; ++h) transpose_quads(f.kf[4 * h], f.kf[4 * h + 1], f.kf[4 * h + 2], f.kf[4 * h + 3], odd, upper);
+    }
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+    for (int h = 0; h < F::kHalves; ++h) {
+      f32x4 acc[NR];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.kf[i][e]), __uint_as_float(f.q[n][i][e]), acc, 0, 0, 0);
-        } else {
+      for (int n = 0; n < NR; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (kF32) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (ET == kFP8) acc = mfma_bf16(e4m3_to_bf16(f.kf[4 * h + i]), f.q[n][i], acc);
-            else acc = mfma_bf16(f.kf[4 * h + i], f.q[n][i], acc);
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+              acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.kf[i][e]), __uint_as_float(f.q[n][i][e]), acc[n], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x4 k;
+          if constexpr (ET == kFP8) {
+            const u32x4 w = f.kf[2 * h + (i >> 1)];
+            k = e4m3_to_bf16(i & 1 ? u32x2{w.z, w.w} : u32x2{w.x, w.y});
+          } else {
+            k = f.kf[4 * h + i];
           }
-        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][4 * h + i] = acc[i] * to_log2;
+          for (int n = 0; n < NR; ++n) acc[n] = mfma_bf16(k, f.q[n][i], acc[n]);
+        }
       }
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][4 * h + i] = acc[n][i] * to_log2;
     }
   };
   // scores -> weights, in place; the state is raised where they ask for it

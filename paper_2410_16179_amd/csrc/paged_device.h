@@ -60,6 +60,38 @@ __device__ inline u32x4 finite_part(u32x4 w) {
   return u32x4{finite_part<F32>(w.x), finite_part<F32>(w.y), finite_part<F32>(w.z), finite_part<F32>(w.w)};
 }
 
+// Keys are loaded with neighbouring lanes on neighbouring addresses - a quad of lanes reads 64 bytes of one key - and then
+// change lanes inside the quad, where an MFMA operand has a key per lane: with a key per lane from the start a load
+// meets 64 addresses apart from each other, which the L1 takes one by one (58 % of its time in e4m3 decoding).
+template <int CTRL>
+__device__ inline uint32_t quad_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+// (every lane takes part in an exchange: it stands before the choice, not inside it)
+// r[i] of lane j of a quad <-> r[j] of lane i.
+__device__ inline void transpose_quads(u32x4& r0, u32x4& r1, u32x4& r2, u32x4& r3, bool odd, bool upper) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x0 = quad_lane<0xb1>(r0[e]), x1 = quad_lane<0xb1>(r1[e]), x2 = quad_lane<0xb1>(r2[e]), x3 = quad_lane<0xb1>(r3[e]);   // lane ^ 1
+    const uint32_t a0 = odd ? x1 : r0[e], a1 = odd ? r1[e] : x0, a2 = odd ? x3 : r2[e], a3 = odd ? r3[e] : x2;
+    const uint32_t y0 = quad_lane<0x4e>(a0), y1 = quad_lane<0x4e>(a1), y2 = quad_lane<0x4e>(a2), y3 = quad_lane<0x4e>(a3);               // lane ^ 2
+    r0[e] = upper ? y2 : a0;
+    r1[e] = upper ? y3 : a1;
+    r2[e] = upper ? a2 : y0;
+    r3[e] = upper ? a3 : y1;
+  }
+}
+// Lane j of a quad has half j % 2 of keys j / 2 (r0) and 2 + j / 2 (r1) -> both halves of key j.
+__device__ inline void join_halves(u32x4& r0, u32x4& r1, bool upper) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x0 = quad_lane<0x88>(r0[e]), x1 = quad_lane<0x88>(r1[e]);                             // lanes 0, 2, 0, 2
+    const uint32_t y0 = quad_lane<0xdd>(r0[e]), y1 = quad_lane<0xdd>(r1[e]);                             // lanes 1, 3, 1, 3
+    r0[e] = upper ? x1 : x0;
+    r1[e] = upper ? y1 : y0;
+  }
+}
+
 // The pages of a tile, one for every 16 keys: ids as the table has them.
 template <int KT>
 struct TilePages {
