@@ -308,8 +308,12 @@ typedef struct magicpig_paged_params {
   int64_t v_new_stride_token, v_new_stride_head;          /* new values, alike */
 } magicpig_paged_params;
 
-/* Scratch that is enough for any of the three calls with these params (0 on invalid params); 256-byte
- * aligned, its contents need not be initialised or preserved between calls. */
+/* Scratch that is enough for any of the three calls with these params (0 on invalid params), 16-byte
+ * aligned.  Its first MAGICPIG_PAGED_COUNTER_BYTES have to be zero before its first use; the calls leave them
+ * zero again (they count, within magicpig_paged_attention, the parts of a row's sum that have arrived: a row whose count
+ * starts elsewhere is left unwritten, or is written before all parts are there).  The rest need not be initialised or
+ * preserved.  magicpig_page_plan needs a workspace for more than 2048 requests or 8192 token rows only. */
+#define MAGICPIG_PAGED_COUNTER_BYTES 4096u
 MAGICPIG_API size_t magicpig_paged_workspace_bytes(const magicpig_paged_params* params);
 
 /* One step's bookkeeping.  new_tokens [batch] int32: n >= 0, the request gets n tokens behind its

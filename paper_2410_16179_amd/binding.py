@@ -500,7 +500,7 @@ def alloc_workspace(params, device="cuda") -> torch.Tensor:
 
 
 def alloc_paged_workspace(params, device="cuda") -> torch.Tensor:
-    return torch.empty(max(magicpig_paged_workspace_bytes(params), 256), dtype=torch.uint8, device=device)
+    return torch.zeros(max(magicpig_paged_workspace_bytes(params), 256), dtype=torch.uint8, device=device)
 
 
 def key_code_gather_index(params) -> np.ndarray:

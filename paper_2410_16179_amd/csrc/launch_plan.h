@@ -93,13 +93,16 @@ inline bool page_plan_in_one(int batch, int64_t max_tokens) { return batch <= kP
 // min_tiles: key tiles of a piece at least.  items, pieces, units, slots: at most so many row
 // tiles of all KV heads, workgroups, row tiles that are cut, partials.
 struct PagedForm {
-  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles;
+  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles, shares, min_share, group_shift;
   int64_t items, pieces, units, slots;
 };
 
 // Up to 32 rows are taken by the form that keeps keys in registers, 16 or 32 at a time; more (bf16) by the one that shares
 // keys among 128 rows through LDS.  float32: always 16.
 constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
+constexpr int kPagedGroupShift = 3, kPagedGroup = 1 << kPagedGroupShift;   // few rows: wavefronts of a workgroup
+constexpr int kPagedMinShare = 1;
+constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share of a KV head (at most 3 kNumCU, or a share for each)
 inline int paged_rows(bool fp32, int64_t rows) { return fp32 || rows <= 16 ? 16 : (rows <= 32 ? 32 : kPagedManyRows); }
 
 // Row tiles of all KV heads and requests, whatever token counts (each at most max_new) the device memory holds.
@@ -118,8 +121,9 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : 32);
   f.tile_tokens = group <= f.rows ? f.rows / group : 1;
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
-  f.target = many ? 2 * kNumCU : 3 * kNumCU;               // workgroups that are resident at once
-  f.min_tiles = (many ? 512 : 256) / f.key_tile;
+  f.target = many ? 2 * kNumCU : kNumCU;               // workgroups that are resident at once
+  f.min_tiles = 512 / f.key_tile;
+  f.min_share = kPagedMinShare;
   int64_t tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens);
   if (starts && max_tokens / f.tile_tokens + batch < tiles) tiles = max_tokens / f.tile_tokens + batch;
   f.items = tiles * f.head_blocks * kv_heads;
@@ -136,8 +140,19 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
     f.slots = f.items * most < cut ? f.items * most : cut;
     f.units = f.items < f.target ? f.items : f.target;
   }
-  // (pieces are dealt to the eight XCDs in rounds of eight)
-  if (!many) f.pieces = (f.pieces / kv_heads + 7) / 8 * 8 * kv_heads;
+  if (!many) {
+    // (a group has at least a key tile for each wavefront; the groups of all row tiles are counted in 31 bits)
+    auto groups = [&](int shift) { return (charge + (1 << shift) - 1) >> shift; };
+    f.group_shift = kPagedGroupShift;
+    const int64_t row_tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens) * f.head_blocks;
+    while (row_tiles * groups(f.group_shift) > INT32_MAX - kPagedCounters) ++f.group_shift;
+    const int64_t least = (groups(f.group_shift) * (f.items / kv_heads) + f.min_share - 1) / f.min_share;
+    const int64_t shares = f.target / kv_heads > 1 ? f.target / kv_heads : 1;
+    f.shares = (int)(shares < least ? shares : (least > 1 ? least : 1));
+    f.pieces = (int64_t)(f.shares + 7) / 8 * 8 * kv_heads;   // (dealt to the eight XCDs in rounds of eight)
+    f.units = 0;
+    f.slots = 2 * (int64_t)f.shares * kv_heads;
+  }
   return f;
 }
 

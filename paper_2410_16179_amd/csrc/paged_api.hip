@@ -59,12 +59,12 @@ mp::PagedForm form_of(const Params* p, bool starts) {
   return mp::paged_form(p->batch, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->dtype == MAGICPIG_FP32, p->max_tokens, starts ? most_new(p) : 1,
                         starts, (int64_t)p->max_pages * p->page_size, p->n_sink, p->n_local);
 }
-size_t ws_attention(const Params* p, const mp::PagedForm& f) {
-  (void)p;
-  return align256((size_t)f.slots * f.rows * mp::kPartialStride * sizeof(float));
-}
+// The workspace: counters of arrived partials (zero between calls), then what a call keeps for itself.
+constexpr size_t kCounterBytes = MAGICPIG_PAGED_COUNTER_BYTES;
+static_assert(kCounterBytes == mp::kPagedCounters * sizeof(unsigned), "");
+size_t ws_attention(const mp::PagedForm& f) { return kCounterBytes + align256((size_t)f.slots * f.rows * mp::kPartialStride * sizeof(float)); }
 size_t ws_plan(const Params* p) {
-  return mp::page_plan_in_one(p->batch, p->max_tokens) ? 0 : align256((size_t)3 * (p->batch + 1) * sizeof(int));
+  return mp::page_plan_in_one(p->batch, p->max_tokens) ? 0 : kCounterBytes + align256((size_t)3 * (p->batch + 1) * sizeof(int));
 }
 
 }  // namespace
@@ -75,7 +75,7 @@ size_t magicpig_paged_workspace_bytes(const Params* p) {
   if (check(p) != MAGICPIG_OK) return 0;
   size_t m = ws_plan(p);
   for (const bool starts : {false, true}) {
-    const size_t a = ws_attention(p, form_of(p, starts));
+    const size_t a = ws_attention(form_of(p, starts));
     if (a > m) m = a;
   }
   return m < 256 ? 256 : m;
@@ -97,7 +97,7 @@ int magicpig_page_plan(const Params* p, const int32_t* new_tokens, const int32_t
   mp::PagePlanArgs a{};
   a.new_tokens = new_tokens; a.lengths = lengths; a.table = block_table; a.free_pages = free_pages; a.n_free = n_free;
   a.lengths_out = lengths_out; a.n_free_out = n_free_out; a.token_start = token_start; a.slots = slots; a.status = status;
-  a.scan = reinterpret_cast<int*>(workspace);
+  if (need > 0) a.scan = reinterpret_cast<int*>(reinterpret_cast<char*>(workspace) + kCounterBytes);
   a.batch = p->batch; a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages; a.max_new = p->max_new;
   a.n_pages = p->n_pages; a.max_tokens = p->max_tokens;
   return mp::hip_status(mp::launch_page_plan(a, reinterpret_cast<hipStream_t>(hip_stream)));
@@ -141,13 +141,15 @@ int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages
       !aligned(lengths, 4) || !aligned(token_start, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(workspace))
     return MAGICPIG_INVALID_ARG;
   const mp::PagedForm f = form_of(p, token_start != nullptr);
-  const size_t need = ws_attention(p, f);
-  if (need > 0 && (!workspace || workspace_bytes < need)) return MAGICPIG_WORKSPACE_TOO_SMALL;
+  const size_t need = ws_attention(f);
+  if (!workspace || workspace_bytes < need) return MAGICPIG_WORKSPACE_TOO_SMALL;
   if (p->batch == 0) return MAGICPIG_OK;
   mp::PagedArgs a{};
   a.q = q; a.k = k_pages; a.v = v_pages; a.k_scale = k_scale; a.v_scale = v_scale;
   a.table = block_table; a.lengths = lengths; a.token_start = token_start;
-  a.out = out; a.lse = lse; a.partial = reinterpret_cast<float*>(workspace);
+  a.out = out; a.lse = lse;
+  a.arrived = reinterpret_cast<unsigned*>(workspace);
+  a.partial = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + kCounterBytes);
   a.batch = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
   a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages; a.max_new = token_start ? most_new(p) : 1;
   a.n_sink = p->n_sink; a.n_local = p->n_local;
@@ -155,7 +157,8 @@ int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages
   a.tile_tokens = f.tile_tokens; a.head_blocks = f.head_blocks;
   a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * 1.4426950408889634f;
   a.per_piece = 1.0001f / (float)f.target;                  // (the margin keeps float32's rounding from making more pieces)
-  a.min_tiles = f.min_tiles; a.slots = (int)f.slots;
+  a.min_tiles = f.min_tiles; a.slots = (int)f.slots; a.shares = f.shares; a.min_share = f.min_share;
+  a.group_shift = f.group_shift; a.group_tiles = 1 << f.group_shift;
   a.k_page = p->k_stride_page; a.k_key = p->k_stride_key; a.k_head = p->k_stride_head;
   a.v_page = p->v_stride_page; a.v_key = p->v_stride_key; a.v_head = p->v_stride_head;
   a.q_t = p->q_stride_token; a.q_h = p->q_stride_head;

@@ -6,6 +6,134 @@
 namespace mp {
 namespace {
 
+constexpr int kFewThreads = 64 * kPagedGroup;
+
+// Joins the partials of a cut item, by one workgroup: groups of sixteen threads take a row each, eight elements a thread, and where
+// there are few rows several groups share a row's partials; eight partials are requested at once.  lds: room for as many rows as there are groups.
+template <bool F32, int R, class OutRow>
+__device__ inline void join_parts(const PagedArgs& a, float* lds, int first_share, int parts, int g, int rows, float v_scale, OutRow out_row) {
+  constexpr int kAtOnce = 8;
+  const int lot = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * 8;
+  constexpr int kLots = kFewThreads / 16;
+  const int per_row = rows < kLots ? kLots / rows : 1;
+  {
+    const int part = lot / rows, row = lot - part * rows;
+    const bool busy = part < per_row && row < rows;
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
+    if (busy) {
+      for (int p = part; p < parts; p += kAtOnce * per_row) {
+        f32x2 x[kAtOnce][4], ml[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int q = p + i * per_row;
+          ml[i] = f32x2{-INFINITY, 0.f};
+          if (q < parts) {
+            const float* from = a.partial + ((2 * ((int64_t)(first_share + q) * a.Hkv + g) + (q == 0 ? 1 : 0)) * R + row) * kPartialRow;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][e] = load_through(from + e0 + 2 * e);
+            ml[i] = load_through(from + 128);
+          }
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i].x);
+        if (top > -INFINITY) {
+          const float by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+          l *= by;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] *= by;
+          m = top;
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) {
+            if (ml[i].x == -INFINITY) continue;            // (an empty partial, or none)
+            const float b1 = ml[i].x == top ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+            l += b1 * ml[i].y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += b1 * x[i][e >> 1][e & 1];
+          }
+        }
+      }
+    }
+    if (per_row > 1) {
+      float* to = lds + lot * kPartialRow;
+      if (busy) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[e0 + e] = o[e];
+        if (e0 == 0) { to[128] = m; to[129] = l; }
+      }
+      __syncthreads();
+      if (busy && part == 0) {
+        for (int i = 1; i < per_row; ++i) {
+          const float* from = lds + (lot + i * rows) * kPartialRow;
+          const float m1 = from[128], top = fmaxf(m, m1);
+          if (m1 == -INFINITY) continue;
+          const float b0 = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), b1 = m1 == top ? 1.f : __builtin_amdgcn_exp2f(m1 - top);
+          l = b0 * l + b1 * from[129];
+          m = top;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = b0 * o[e] + b1 * from[e0 + e];
+        }
+      }
+    }
+    if (busy && part == 0) paged_write_row<F32>(a, out_row(row), e0, o, m, l, v_scale);
+  }
+}
+
+// Behind the wavefronts' parts in `joined`: the rows of the item they belong to are written, or, where other workgroups have keys of it
+// too, a partial; the last of these workgroups joins the partials.
+template <int KT, bool F32, int NR>
+__device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, float (&joined)[kPagedGroup][16 * NR][kPartialRow], int& last_one) {
+  constexpr int R = 16 * NR;
+  const PagedItem item = paged_item<KT>(a, share);
+  const int tt = item.tile / a.head_blocks, hb = item.tile - tt * a.head_blocks;
+  const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, item.r.tokens) - 1;
+  const int rows = a.head_blocks > 1 ? min(a.G - hb * R, R) : (last - first + 1) * a.G;
+  auto out_row = [&](int row) {
+    const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
+    return (int64_t)(item.r.row + first + t) * a.Hq + item.g * a.G + h;
+  };
+  const bool whole = item.from == 0 && item.to == item.groups;
+  const int slot = 2 * (share.j * a.Hkv + item.g) + (item.from == 0 ? 1 : 0);
+  const float v_scale = a.v_scale ? a.v_scale[item.g] : 1.f;
+  const int e0 = (threadIdx.x & 15) * 8;
+  for (int row = threadIdx.x >> 4; row < rows; row += kFewThreads / 16) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kPagedGroup; ++w) m = fmaxf(m, joined[w][row][128]);
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPagedGroup; ++w) {
+      const float mw = joined[w][row][128];
+      const float by = mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
+      l += by * joined[w][row][129];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += by * joined[w][row][e0 + e];
+    }
+    if (whole) {
+      paged_write_row<F32>(a, out_row(row), e0, o, m, l, v_scale);
+    } else {
+      float* pp = a.partial + ((int64_t)slot * R + row) * kPartialRow;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) store_through(pp + e0 + e, o[e], o[e + 1]);
+      if (e0 == 0) store_through(pp + 128, m, l);
+    }
+  }
+  if (whole) return;
+  const int first_share = item.from == 0 ? share.j : item.begin / share.each;
+  const int parts = (item.begin + item.groups - 1) / share.each - first_share + 1;
+  unsigned* const arrived = a.arrived + (int64_t)first_share * a.Hkv + item.g;
+  stored();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const unsigned before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last_one = before + 1 == (unsigned)parts;
+    if (last_one) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!last_one) return;
+  join_parts<F32, R>(a, &joined[0][0][0], first_share, parts, item.g, rows, v_scale, out_row);
+}
+
 // ---- few rows ------------------------------------------------------------------------------------
 // A wavefront attends tiles of KT keys with up to 16 NR query rows.  Scores are formed transposed,
 // S^T = K Q^T: MFMA A = 16 keys (lane c = lane % 16 holds a key, the lane's quarter u = lane / 16 an eighth of every 32
@@ -37,29 +165,42 @@ struct FewRows {
 };
 
 template <int ET, int NR>
-__global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const PagedArgs a) {
   using F = FewRows<ET, NR>;
   constexpr bool kF32 = F::kF32;
   constexpr int KT = F::kTile, R = 16 * NR;
   constexpr int kElem = ET == kFP32 ? 4 : (ET == kFP8 ? 1 : 2);
-  __shared__ float joined[4][R][kPartialRow];
+  __shared__ float joined[kPagedGroup][R][kPartialRow];
+  __shared__ int last_one;
 
-  PagedPiece pc;
-  if (!paged_locate<KT, kPieces>(a, blockIdx.x, pc)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, u = lane >> 4;
-  const int len = pc.r.len, tokens = pc.r.tokens;
-  const int tt = pc.tile / a.head_blocks, hb = pc.tile - tt * a.head_blocks;
+  // Where the workgroup is in its share lies in LDS: kept in registers over the loops below it would cost them their own.
+  __shared__ PagedShare at_share;
+  {
+    PagedShare share;
+    if (!paged_share<KT>(a, blockIdx.x, share)) return;
+    if (threadIdx.x == 0) at_share = share;
+  }
+  __syncthreads();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll 1
+  for (;;) {
+  // (unknown to the compiler, so that what follows from it is worked out per item and not kept in registers over all of them)
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, c = lane & 15, u = lane >> 4;
+  const PagedItem item = paged_item<KT>(a, at_share);
+  const PagedRequest req = item.r;
+  const int tile = item.tile, g = item.g;
+  const int len = req.len, tokens = req.tokens;
+  const int tt = tile / a.head_blocks, hb = tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, tokens) - 1;
   const int heads = min(a.G - hb * R, R);                // query heads of the tile: all G where a tile holds whole tokens
   const int rows = a.head_blocks > 1 ? heads : (last - first + 1) * a.G;
   const PagedSpan span = paged_span<KT>(a, len, tokens, first, last);
-  int t_begin, t_end;
-  paged_piece_range(span.count, pc.piece, pc.pieces, t_begin, t_end);
-
+  const int t_begin = item.from << a.group_shift, t_end = min(item.to << a.group_shift, span.count);
   // row of this lane's column: token and head
   int hi[NR], lo[NR];                                    // keys it attends: [lo, hi], and those below n_sink
-  F f;
+  F f{};                                                 // (all of it: what an earlier item left would stay in registers)
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const int row = c + 16 * n;
@@ -67,7 +208,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     const bool ok = row < rows;
     hi[n] = ok ? len - tokens + first + t : -1;
     lo[n] = a.n_local > 0 ? hi[n] - a.n_local + 1 : 0;
-    const int64_t at = (int64_t)(pc.r.row + first + t) * a.q_t + (int64_t)(pc.g * a.G + h) * a.q_h;
+    const int64_t at = (int64_t)(req.row + first + t) * a.q_t + (int64_t)(g * a.G + h) * a.q_h;
 #pragma unroll
     for (int s = 0; s < (kF32 ? 8 : 4); ++s) {
       f.q[n][s] = u32x4{0, 0, 0, 0};
@@ -82,11 +223,11 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   const int max_lo = a.n_local > 0 ? len - tokens + last - a.n_local + 1 : 0;
   const int end = len - tokens + last + 1;               // what some row attends: [any_lo, end), and the keys below n_sink
   const int any_lo = a.n_local > 0 ? len - tokens + first - a.n_local + 1 : 0;
-  const float to_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f);
+  const float to_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[g] : 1.f);
 
-  const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)pc.b * a.max_pages);
-  const char* kbase = reinterpret_cast<const char*>(a.k) + (int64_t)pc.g * a.k_head * kElem;
-  const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)pc.g * a.v_head * kElem;
+  const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)item.b * a.max_pages);
+  const char* kbase = reinterpret_cast<const char*>(a.k) + (int64_t)g * a.k_head * kElem;
+  const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)g * a.v_head * kElem;
   const int page_mask = (1 << a.page_shift) - 1;
   const uint32_t k_key = (uint32_t)a.k_key * kElem, v_key = (uint32_t)a.v_key * kElem;
   // This lane's place in 16 keys.  K: a quad of lanes takes keys 4 (c / 4) + i, one (e4m3: two) at a time, of which each lane
@@ -264,7 +405,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   bool bad_page = false;
   // the first such tile from v on, its pages read
   auto find = [&](int v, TilePages<KT>& p) {
-    for (; v < t_end; v += 4) {
+    for (; v < t_end; v += kPagedGroup) {
       if (!in_full(v)) continue;
       tile_pages(v, p);
       if (pages_ok(p)) break;
@@ -272,10 +413,10 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     }
     return v;
   };
-  int whole[F::kHalves];
+  int all16[F::kHalves];
 #pragma unroll
-  for (int h = 0; h < F::kHalves; ++h) whole[h] = 16;
-  TilePages<KT> now, next, after;
+  for (int h = 0; h < F::kHalves; ++h) all16[h] = 16;
+  TilePages<KT> now{}, next{}, after{};
   auto reset = [&]() {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -288,28 +429,28 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
   reset();
   int v = find(t_begin + wave, now), v1 = t_end;
   if (v < t_end) {
-    request_k(tile_key(v), now, whole);
-    request_v(tile_key(v), now, whole);
-    v1 = find(v + 4, next);
+    request_k(tile_key(v), now, all16);
+    request_v(tile_key(v), now, all16);
+    v1 = find(v + kPagedGroup, next);
   }
 #pragma unroll 1
   while (v < t_end) {
-    const int v2 = v1 + 4;
+    const int v2 = v1 + kPagedGroup;
     if (v2 < t_end) tile_pages(v2, after);
     float s[NR][kScores];
     scores(s);
-    if (v1 < t_end) request_k(tile_key(v1), next, whole);
+    if (v1 < t_end) request_k(tile_key(v1), next, all16);
     weigh(s);
     u32x4 vb[8];
     values(vb);
     add_values(s, vb);
-    if (v1 < t_end) request_v(tile_key(v1), next, whole);
+    if (v1 < t_end) request_v(tile_key(v1), next, all16);
     v = v1;
     v1 = v2;
     next = after;
     if (v1 < t_end && !(in_full(v1) && pages_ok(next))) {
       bad_page = bad_page || in_full(v1);
-      v1 = find(v1 + 4, next);
+      v1 = find(v1 + kPagedGroup, next);
     }
   }
 
@@ -319,10 +460,10 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     int v = t_begin + wave;
     if (a.n_local == 0 && !bad_page && !CAREFUL) {   // only from the first key on that some row does not attend
       const int from = (min_hi + 1 > 0 ? min_hi + 1 : 0) / KT;
-      if (from > v) v += (from - v + 3) / 4 * 4;
+      if (from > v) v += (from - v + kPagedGroup - 1) / kPagedGroup * kPagedGroup;
     }
 #pragma unroll 1
-    for (; v < t_end; v += 4) {
+    for (; v < t_end; v += kPagedGroup) {
       const bool inside = in_full(v);
       if (inside && !bad_page && !CAREFUL) continue;
       tile_pages(v, now);
@@ -414,7 +555,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     others(std::true_type{});
   }
 
-  // the four wavefronts' parts, joined in LDS
+  // the wavefronts' parts, joined in LDS
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     float l = f.l[n];
@@ -439,42 +580,17 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged_few_rows_kernel(co
     if (u == 0) { to[128] = f.m[n]; to[129] = l; }
   }
   __syncthreads();
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int row = (threadIdx.x >> 4) + 16 * n, e0 = (threadIdx.x & 15) * 8;
-    if (row >= rows) continue;
-    float m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, joined[w][row][128]);
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float mw = joined[w][row][128];
-      const float by = mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
-      l += by * joined[w][row][129];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += by * joined[w][row][e0 + e];
-    }
-    if (pc.pieces > 1) {
-      const int64_t slot = pc.slot + pc.piece;
-      if (slot >= a.slots) continue;
-      float* pp = a.partial + (slot * R + row) * kPartialRow;
-      *reinterpret_cast<f32x4*>(pp + e0) = f32x4{o[0], o[1], o[2], o[3]};
-      *reinterpret_cast<f32x4*>(pp + e0 + 4) = f32x4{o[4], o[5], o[6], o[7]};
-      if (e0 == 0) { pp[128] = m; pp[129] = l; }
-    } else {
-      const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
-      const int64_t to = (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h;
-      const float vs = (a.v_scale ? a.v_scale[pc.g] : 1.f);
-      paged_write_row<kF32>(a, to, e0, o, m, l, vs);
-    }
+  finish_item<KT, kF32, NR>(a, at_share, joined, last_one);
+  if (threadIdx.x == 0) paged_next<KT>(a, at_share);
+  __syncthreads();
+  if (at_share.pos >= at_share.end) return;
   }
 }
 
 // ---- joining the pieces of an item ------------------------------------------------------------------
 // A workgroup takes a row of a cut item: eight half wavefronts take its partials in turn, four elements a
 // lane, four partials requested at once, and join what they have in LDS.
-template <bool FP32, int KT, int R>
+template <int KT, int R>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
   __shared__ float joined[8][kPartialRow];
   PagedPiece pc;
@@ -535,21 +651,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
     for (int e = 0; e < 8; ++e) out[e] += by * joined[w][e0 + e];
   }
   const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
-  paged_write_row<FP32>(a, (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h, e0, out, top, sum, a.v_scale ? a.v_scale[pc.g] : 1.f);
-}
-
-template <bool FP32, int KT, int R>
-void launch_join(const PagedArgs& a, const PagedForm& form, hipStream_t s) {
-  if (form.units == 0) return;
-  const int rows = a.head_blocks > 1 ? form.rows : (a.tile_tokens < a.max_new ? a.tile_tokens : a.max_new) * a.G;
-  paged_join_kernel<FP32, KT, R><<<dim3((unsigned)form.units, rows), 256, 0, s>>>(a);
+  paged_write_row<false>(a, (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h, e0, out, top, sum, a.v_scale ? a.v_scale[pc.g] : 1.f);
 }
 
 template <int ET, int NR>
 hipError_t launch_few_rows(const PagedArgs& a, const PagedForm& form, hipStream_t s) {
-  constexpr int KT = FewRows<ET, NR>::kTile;
-  paged_few_rows_kernel<ET, NR><<<(unsigned)form.pieces, 256, 0, s>>>(a);
-  launch_join<ET == kFP32, KT, 16 * NR>(a, form, s);
+  paged_few_rows_kernel<ET, NR><<<(unsigned)form.pieces, kFewThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -559,7 +666,10 @@ hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedFo
   if (element == kFP32) return launch_few_rows<kFP32, 1>(a, form, s);
   if (form.rows == kPagedManyRows) {
     launch_paged_many_rows(a, element == kFP8, form, s);
-    launch_join<false, kPagedManyKeys, kPagedManyRows>(a, form, s);
+    if (form.units > 0) {
+      const int rows = a.head_blocks > 1 ? form.rows : (a.tile_tokens < a.max_new ? a.tile_tokens : a.max_new) * a.G;
+      paged_join_kernel<kPagedManyKeys, kPagedManyRows><<<dim3((unsigned)form.units, rows), 256, 0, s>>>(a);
+    }
     return hipGetLastError();
   }
   if (form.rows == 16) return element == kFP8 ? launch_few_rows<kFP8, 1>(a, form, s) : launch_few_rows<kBF16, 1>(a, form, s);

@@ -25,10 +25,13 @@ struct PageAppendArgs {
 // Paged attention.  The rows of a request (its new tokens times the query heads of a KV head) are taken
 // in row tiles of whole tokens (tile_tokens each; where one token has more heads than a tile has rows,
 // head_blocks tiles per token).  An item is a row tile of one request and KV head; its keys are counted
-// in tiles, and a long item is cut into pieces of them, one workgroup each, joined by a second kernel.
-// Lengths are known on the device alone, so every workgroup works out the cut for itself: requests are
-// charged their keys (as if all row tiles reached the last one), pieces get at most 1/target of the sum.
-// A request that is cut has more than piece_tiles tiles per item, so cut items have at most twice
+// in tiles.  Lengths are known on the device alone, so every workgroup works out by itself what it takes; a request is
+// charged its keys as if all its row tiles reached the last one.
+// Few rows: the items of a KV head, one behind the other, are cut into `shares` equal shares; a workgroup takes a share, whole
+// items and parts of the first and the last.  A partial of either goes to the workspace (slots 2 w and 2 w + 1 of workgroup w), and the
+// workgroup that finds all others of the item there joins them.
+// Many rows: a long item is cut into pieces, one workgroup each, joined by a second kernel.  Pieces get at most
+// 1/target of the sum; a request that is cut has more than piece_tiles tiles per item, so cut items have at most twice
 // target pieces together.
 struct PagedArgs {
   const void* q; const void* k; const void* v; const float* k_scale; const float* v_scale;
@@ -41,6 +44,9 @@ struct PagedArgs {
   float per_piece;        // (1 + margin) / target pieces
   int min_tiles;          // of a piece
   int slots;              // partials that there is room for
+  int shares, min_share;  // few rows: shares of a KV head, and groups of group_tiles key tiles of one at least
+  int group_tiles, group_shift;
+  unsigned* arrived;      // few rows: partials of the cut item that begins in a share which are there (0 between calls)
   int64_t k_page, k_key, k_head, v_page, v_key, v_head, q_t, q_h;
 };
 
@@ -106,33 +112,23 @@ struct PagedPiece {
   int slot;                        // of the item's first partial
 };
 
-__device__ inline int wave_prefix(int v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(v, d);
-    if (lane >= d) v += u;
-  }
-  return v;
+// Inclusive prefix sums over the wavefront's lanes.
+__device__ inline int wave_prefix(int v) {
+  v = half_prefix_sum32(v);
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
 }
 
-// Which workgroup takes what.  kPieces: all pieces, the KV heads of a piece on one XCD (workgroups go to the eight XCDs in turn): in
-// pools that store keys token by token its heads' rows are neighbours.  kPiecesByHead: a KV head's pieces on one XCD
-// (where the number of KV heads goes with eight), whose L2 then serves the row tiles that read the same keys.  kCutItems: the items
+// Many rows: which workgroup takes what.  kPieces: all pieces, a KV head's on one XCD (workgroups go to the eight XCDs in turn; where
+// the number of KV heads goes with eight), whose L2 then serves the row tiles that read the same keys.  kCutItems: the items
 // that are cut, for the join.
-enum { kPieces, kPiecesByHead, kCutItems };
+enum { kPieces, kCutItems };
 
 // What workgroup `index` takes; called by whole wavefronts, false where there is nothing.
 template <int KT, int WHAT>
 __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& out) {
   const int lane = threadIdx.x & 63;
-  if (WHAT == kPieces) {
-    const int i = index >> 3;
-    out.g = i % a.Hkv;
-    index = (i / a.Hkv) * 8 + (index & 7);
-  } else {
-    out.g = index % a.Hkv;
-    index /= a.Hkv;
-  }
+  out.g = index % a.Hkv;
+  index /= a.Hkv;
   float total = 0.f;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
@@ -158,7 +154,7 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
     }
     const int cut = pieces > 1 ? tiles * pieces : 0;
     const int count = WHAT == kCutItems ? (pieces > 1 ? tiles : 0) : tiles * pieces;
-    const int upto = wave_prefix(count, lane), slots = wave_prefix(cut, lane);
+    const int upto = wave_prefix(count), slots = wave_prefix(cut);
     const uint64_t found = __ballot(base + upto > index);
     if (found) {
       const int f = __ffsll((unsigned long long)found) - 1;
@@ -183,6 +179,110 @@ __device__ inline void paged_piece_range(int count, int piece, int pieces, int& 
   const int each = count / pieces, more = count % pieces;
   begin = piece * each + (piece < more ? piece : more);
   end = begin + each + (piece < more ? 1 : 0);
+}
+
+// Few rows: a workgroup's share of a KV head's items, in groups of key tiles: [begin, end) of all, which starts inside request b,
+// whose items begin at `base`; pos: where the workgroup is.
+struct PagedShare {
+  int g, j, b, base, pos, begin, end, each;
+  PagedRequest r;
+};
+// The item that `pos` lies in: its first group, and the groups [from, to) of its `groups` that the share has.
+struct PagedItem {
+  int g, b, tile, begin, from, to, groups;
+  PagedRequest r;
+};
+
+// (the host chooses group_tiles so that the groups of all row tiles stay below 2^31)
+template <int KT>
+__device__ inline int paged_groups(const PagedArgs& a, int len) {
+  return (paged_charge<KT>(a, len) + a.group_tiles - 1) >> a.group_shift;
+}
+__device__ inline int paged_row_tiles(const PagedArgs& a, int tokens) {
+  return (tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
+}
+
+// The KV heads of a share follow one another on one XCD (workgroups go to the eight XCDs in turn): in pools that store keys token by
+// token their rows are neighbours.
+template <int KT>
+__device__ inline bool paged_share(const PagedArgs& a, int index, PagedShare& out) {
+  const int lane = threadIdx.x & 63, i = index >> 3;
+  out.g = i % a.Hkv;
+  out.j = i / a.Hkv * 8 + (index & 7);
+  if (out.j >= a.shares) return false;
+  int total = 0;
+  for (int b0 = 64; b0 < a.batch; b0 += 64) {             // (the first 64 requests are counted below, once)
+    const int b = b0 + lane;
+    int v = 0;
+    if (b < a.batch) {
+      const PagedRequest r = paged_request(a, b);
+      v = paged_row_tiles(a, r.tokens) * paged_groups<KT>(a, r.len);
+    }
+    total += __builtin_amdgcn_readlane(wave_prefix(v), 63);
+  }
+  int base = 0;
+  out.each = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int b = b0 + lane;
+    PagedRequest r{0, 0, 0};
+    int v = 0;
+    if (b < a.batch) {
+      r = paged_request(a, b);
+      v = paged_row_tiles(a, r.tokens) * paged_groups<KT>(a, r.len);
+    }
+    const int upto = wave_prefix(v), sum = __builtin_amdgcn_readlane(upto, 63);
+    if (b0 == 0) {
+      total += sum;
+      if (total == 0) return false;
+      out.each = max((int)(((uint32_t)total + (uint32_t)a.shares - 1u) / (uint32_t)a.shares), a.min_share);
+      const int64_t begin = (int64_t)out.each * out.j;
+      if (begin >= total) return false;
+      out.begin = out.pos = (int)begin;
+      out.end = out.each < total - out.begin ? out.begin + out.each : total;
+    }
+    const uint64_t found = __ballot(base + upto > out.begin);
+    if (found) {
+      const int f = __ffsll((unsigned long long)found) - 1;
+      out.b = b0 + f;
+      out.r.len = __builtin_amdgcn_readlane(r.len, f);
+      out.r.tokens = __builtin_amdgcn_readlane(r.tokens, f);
+      out.r.row = __builtin_amdgcn_readlane(r.row, f);
+      out.base = base + __builtin_amdgcn_readlane(upto - v, f);
+      return true;
+    }
+    base += sum;
+  }
+  return false;
+}
+
+// (the share lies in LDS: the same for all lanes)
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <int KT>
+__device__ inline PagedItem paged_item(const PagedArgs& a, const PagedShare& s) {
+  PagedItem i;
+  i.g = uniform(s.g);
+  i.b = uniform(s.b);
+  i.r.len = uniform(s.r.len); i.r.tokens = uniform(s.r.tokens); i.r.row = uniform(s.r.row);
+  const int tiles = paged_row_tiles(a, i.r.tokens), pos = uniform(s.pos), base = uniform(s.base), end = uniform(s.end);
+  i.groups = paged_groups<KT>(a, i.r.len);
+  const int k = tiles > 1 ? (pos - base) / i.groups : 0;
+  i.begin = base + k * i.groups;
+  i.from = pos - i.begin;
+  i.to = min(i.groups, end - i.begin);
+  i.tile = k & 1 ? tiles - 1 - k / 2 : k / 2;              // (from both ends in turn: later tokens have more keys)
+  return i;
+}
+// Behind the item, by one thread: the next request that has rows, if the share goes on there.
+template <int KT>
+__device__ inline void paged_next(const PagedArgs& a, PagedShare& s) {
+  const int tiles = paged_row_tiles(a, s.r.tokens), groups = paged_groups<KT>(a, s.r.len);
+  const int next = s.base + tiles * groups, k = tiles > 1 ? (s.pos - s.base) / groups : 0;
+  s.pos = min(s.base + (k + 1) * groups, s.end);
+  if (s.pos < s.end && s.pos == next) {
+    s.base = next;
+    do s.r = paged_request(a, ++s.b);
+    while (s.r.tokens == 0);
+  }
 }
 
 // Eight elements, e0 .. e0 + 7, of a finished row: o / l (times the values' scale), and with the first ones the row's lse.

@@ -49,6 +49,19 @@ __device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32
   to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, 0));
 }
 
+// Partial results that another workgroup joins within the same launch.  Workgroups may sit on different XCDs, whose L2s do not see one
+// another's lines.  A release and an acquire at agent scope would write back and drop whole L2s, in every workgroup
+// (the step of one user at 96k took 220 us for 81); instead the values themselves go past the L2s, as relaxed atomics
+// of agent scope.  stored() waits until this wavefront's have arrived.
+__device__ inline void store_through(float* to, float x, float y) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline f32x2 load_through(const float* from) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+__device__ inline void stored() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // w without infinities and NaN: a float32, or two bf16.
 template <bool F32>
 __device__ inline uint32_t finite_part(uint32_t w) {

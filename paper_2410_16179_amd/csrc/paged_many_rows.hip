@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
   __shared__ __align__(16) char lds[2][2][kTileBytes];     // [buffer][keys, values]
 
   PagedPiece pc;
-  if (!paged_locate<KT, kPiecesByHead>(a, blockIdx.x, pc)) return;
+  if (!paged_locate<KT, kPieces>(a, blockIdx.x, pc)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, u = lane >> 5;
   const int len = pc.r.len, tokens = pc.r.tokens;
