@@ -587,71 +587,55 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   }
 }
 
-// ---- joining the pieces of an item ------------------------------------------------------------------
-// A workgroup takes a row of a cut item: eight half wavefronts take its partials in turn, four elements a
-// lane, four partials requested at once, and join what they have in LDS.
-template <int KT, int R>
-__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
-  __shared__ float joined[8][kPartialRow];
+// ---- joining the pieces of an item (many rows) --------------------------------------------------------
+// A workgroup takes half of the rows of a cut item, sixteen lanes a row, eight elements a lane, four partials requested at once.
+// (A workgroup per row, most of them without work, took 35 us of a prompt's 450.)
+constexpr int kJoinThreads = 16 * kPagedManyRows / 2;
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const PagedArgs a) {
+  constexpr int KT = kPagedManyKeys, R = kPagedManyRows;
   PagedPiece pc;
   if (!paged_locate<KT, kCutItems>(a, blockIdx.x, pc)) return;
-  const int row = blockIdx.y;
+  const int row = blockIdx.y * (R / 2) + (threadIdx.x >> 4), e0 = (threadIdx.x & 15) * 8;
   const int tt = pc.tile / a.head_blocks, hb = pc.tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, pc.r.tokens) - 1;
   const int rows = a.head_blocks > 1 ? min(a.G - hb * R, R) : (last - first + 1) * a.G;
   if (row >= rows || pc.slot + pc.pieces > a.slots) return;
-  const int part = threadIdx.x >> 5, l32 = threadIdx.x & 31;
   const float* pp = a.partial + ((int64_t)pc.slot * R + row) * kPartialRow;
   const int64_t step = (int64_t)R * kPartialRow;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
-  for (int p = part; p < pc.pieces; p += 32) {
-    f32x4 o1[4];
-    float m1[4], l1[4];
+  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
+  for (int p = 0; p < pc.pieces; p += 4) {
+    f32x4 x[4], y[4];
+    f32x2 ml[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool ok = p + 8 * i < pc.pieces;
-      const float* from = pp + (ok ? p + 8 * i : p) * step;
-      o1[i] = *reinterpret_cast<const f32x4*>(from + 4 * l32);
-      m1[i] = ok ? from[128] : -INFINITY;
-      l1[i] = ok ? from[129] : 0.f;
+      ml[i] = f32x2{-INFINITY, 0.f};
+      if (p + i < pc.pieces) {
+        const float* from = pp + (p + i) * step;
+        x[i] = *reinterpret_cast<const f32x4*>(from + e0);
+        y[i] = *reinterpret_cast<const f32x4*>(from + e0 + 4);
+        ml[i] = *reinterpret_cast<const f32x2*>(from + 128);
+      }
     }
     float top = m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, m1[i]);
-    if (top > -INFINITY) {
-      const float by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-      o *= by;
-      l *= by;
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i].x);
+    if (top == -INFINITY) continue;
+    const float by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    l *= by;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float b1 = m1[i] == top ? 1.f : (m1[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1[i] - top));
-        if (m1[i] > -INFINITY) {                           // (an empty partial, or one repeated behind the last)
-          o += b1 * o1[i];
-          l += b1 * l1[i];
-        }
-      }
-      m = top;
+    for (int e = 0; e < 8; ++e) o[e] *= by;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (ml[i].x == -INFINITY) continue;                  // (an empty partial, or none)
+      const float b1 = ml[i].x == top ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+      l += b1 * ml[i].y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { o[e] += b1 * x[i][e]; o[4 + e] += b1 * y[i][e]; }
     }
   }
-  *reinterpret_cast<f32x4*>(&joined[part][4 * l32]) = o;
-  if (l32 == 0) { joined[part][128] = m; joined[part][129] = l; }
-  __syncthreads();
-  if (threadIdx.x >= 16) return;
-  const int e0 = threadIdx.x * 8;
-  float top = -INFINITY, sum = 0.f, out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int w = 0; w < 8; ++w) top = fmaxf(top, joined[w][128]);
-#pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    const float mw = joined[w][128];
-    const float by = mw == -INFINITY ? 0.f : (mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - top));
-    sum += by * joined[w][129];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] += by * joined[w][e0 + e];
-  }
   const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
-  paged_write_row<false>(a, (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h, e0, out, top, sum, a.v_scale ? a.v_scale[pc.g] : 1.f);
+  paged_write_row<false>(a, (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + h, e0, o, m, l, a.v_scale ? a.v_scale[pc.g] : 1.f);
 }
 
 template <int ET, int NR>
@@ -666,10 +650,7 @@ hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedFo
   if (element == kFP32) return launch_few_rows<kFP32, 1>(a, form, s);
   if (form.rows == kPagedManyRows) {
     launch_paged_many_rows(a, element == kFP8, form, s);
-    if (form.units > 0) {
-      const int rows = a.head_blocks > 1 ? form.rows : (a.tile_tokens < a.max_new ? a.tile_tokens : a.max_new) * a.G;
-      paged_join_kernel<kPagedManyKeys, kPagedManyRows><<<dim3((unsigned)form.units, rows), 256, 0, s>>>(a);
-    }
+    if (form.units > 0) paged_join_kernel<<<dim3((unsigned)form.units, 2), kJoinThreads, 0, s>>>(a);
     return hipGetLastError();
   }
   if (form.rows == 16) return element == kFP8 ? launch_few_rows<kFP8, 1>(a, form, s) : launch_few_rows<kBF16, 1>(a, form, s);

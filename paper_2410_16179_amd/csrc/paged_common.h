@@ -142,6 +142,46 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
   }
   const float want = fminf(ceilf(total * a.per_piece), 1073741824.f);
   const int piece_tiles = max((int)want, a.min_tiles);
+  if (WHAT == kPieces && a.batch <= 64) {
+    // Items with most keys first, over all requests: what is dealt out last is short.  An item's level is its tiles up to its last token's key
+    // (at most what the request is charged); at_least(x): a request's row tiles of level x or more, the last ones.  The level of the
+    // item sought is found by halving.
+    PagedRequest r{0, 0, 0};
+    int tiles = 0, pieces = 1, top = -1;
+    if (lane < a.batch) {
+      r = paged_request(a, lane);
+      tiles = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
+      const int charge = paged_charge<KT>(a, r.len);
+      pieces = (charge + piece_tiles - 1) / piece_tiles;
+      top = tiles ? min((r.len + KT - 1) / KT, charge) : -1;
+    }
+    auto at_least = [&](int x) {
+      if (x > top) return 0;
+      if (x == 0) return tiles;                            // (more tokens than keys: the first ones attend nothing)
+      const int ahead = KT * (x - 1) - (r.len - r.tokens), t = ahead > 0 ? ahead / a.tile_tokens * a.head_blocks : 0;
+      return tiles - min(t, tiles - 1);
+    };
+    auto before = [&](int x) { return __builtin_amdgcn_readlane(wave_prefix(pieces * at_least(x)), 63); };
+    if (before(0) <= index) return false;
+    int lo = 0, hi = (int)wave_max((float)top) + 1;        // pieces of level lo or more: more than index; of hi or more: not
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before(mid) > index) lo = mid;
+      else hi = mid;
+    }
+    const int many = at_least(lo), more = lo < top ? at_least(lo + 1) : 0, count = pieces * (many - more);
+    const int rank = index - before(lo + 1), upto = wave_prefix(count), cut = pieces > 1 ? tiles * pieces : 0, slots = wave_prefix(cut);
+    const int f = __ffsll((unsigned long long)__ballot(upto > rank)) - 1;
+    auto at = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+    const int i = rank - at(upto - count), here = at(many - more);
+    out.b = f;
+    out.r.len = at(r.len); out.r.tokens = at(r.tokens); out.r.row = at(r.row);
+    out.pieces = at(pieces);
+    out.piece = i / here;
+    out.tile = at(tiles - many) + i % here;
+    out.slot = (at(slots - cut) + out.tile * out.pieces) * a.Hkv + out.g * out.pieces;
+    return true;
+  }
   int base = 0, slot_base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;

@@ -49,10 +49,15 @@ __device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32
   to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, 0));
 }
 
+// The lanes' 16 bytes one behind the other from `to` on (the same for the wavefront); there behind stored().
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t rows, uint32_t at, char* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
+}
+
 // Partial results that another workgroup joins within the same launch.  Workgroups may sit on different XCDs, whose L2s do not see one
 // another's lines.  A release and an acquire at agent scope would write back and drop whole L2s, in every workgroup
 // (the step of one user at 96k took 220 us for 81); instead the values themselves go past the L2s, as relaxed atomics
-// of agent scope.  stored() waits until this wavefront's have arrived.
+// of agent scope.  stored() waits until what this wavefront has under way has arrived.
 __device__ inline void store_through(float* to, float x, float y) {
   __hip_atomic_store(reinterpret_cast<uint64_t*>(to), (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

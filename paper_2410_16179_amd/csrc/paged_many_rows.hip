@@ -11,6 +11,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KT = kPagedManyKeys, R = kPagedManyRows;
 constexpr int kTileBytes = KT * kHeadDim * 2;             // a tile of keys or values as bf16
+constexpr int kAhead = 2;                                // operands read ahead of their product
 
 __device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -19,6 +20,15 @@ __device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
 __device__ inline u32x2 read_transposed(const char* lds) {
   typedef i16x4 __attribute__((address_space(3))) * lds_ptr;
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds)));
+}
+
+// f(BEGIN), .. f(END - 1), as constants
+template <int BEGIN, int END, class F>
+__device__ inline void each(F&& f) {
+  if constexpr (BEGIN < END) {
+    f(std::integral_constant<int, BEGIN>{});
+    each<BEGIN + 1, END>(f);
+  }
 }
 
 // Four wavefronts share tiles of 64 keys in LDS (two buffers); each has 32 query rows.  As in the form for few rows
@@ -35,9 +45,12 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
   constexpr int kElem = ET == kFP8 ? 1 : 2;
   typedef typename std::conditional<ET == kFP8, u32x2, u32x4>::type Raw;
   __shared__ __align__(16) char lds[2][2][kTileBytes];     // [buffer][keys, values]
+  __shared__ int bad_pages;                               // whether a tile had a page that is none
 
   PagedPiece pc;
   if (!paged_locate<KT, kPieces>(a, blockIdx.x, pc)) return;
+  if (threadIdx.x == 0) bad_pages = 0;
+  __syncthreads();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, u = lane >> 5;
   const int len = pc.r.len, tokens = pc.r.tokens;
@@ -59,7 +72,6 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
   const int min_hi = len - tokens + first + t0, wave_hi = busy ? len - tokens + first + t1 : -1;
   const int max_lo = a.n_local > 0 ? wave_hi - a.n_local + 1 : 0;
   const int end = len - tokens + last + 1;
-  const int any_lo = a.n_local > 0 ? len - tokens + first - a.n_local + 1 : 0;
   // a negative scale goes to the queries, so that the largest score is the largest product
   const float signed_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f), to_log2 = fabsf(signed_log2);
   const uint32_t flip = signed_log2 < 0.f ? 0x80008000u : 0u;
@@ -79,10 +91,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
   const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)pc.g * a.v_head * kElem;
   const int page_mask = (1 << a.page_shift) - 1;
   const uint32_t k_key = (uint32_t)a.k_key * kElem, v_key = (uint32_t)a.v_key * kElem;
-  // staging: sixteen lanes take a row, the workgroup sixteen rows at a time
-  const int srow = threadIdx.x >> 4, chunk = threadIdx.x & 15;
+  // Staging: a wavefront takes sixteen keys of a tile, K and V, four rows at a time (sixteen lanes a row): one page and two descriptors each.
+  const int srow = lane >> 4, chunk = lane & 15;
   const uint32_t k_from = srow * k_key + 8 * chunk * kElem, v_from = srow * v_key + 8 * chunk * kElem;
-  const int k_to = srow * 256 + ((chunk ^ srow) << 4), v_to = srow * 256 + ((chunk ^ (srow & 3) << 2) << 4);
+  const int k_to = (16 * wave + srow) * 256, k_chunk = (chunk ^ srow) << 4, v_to = (16 * wave + srow) * 256 + ((chunk ^ srow << 2) << 4);
   // reading
   const int k_at = c * 256, k_swap = (u ^ (c & 15)) << 4;
   const int i16 = lane & 15, quad = i16 >> 2;
@@ -90,40 +102,85 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
 
   auto tile_key = [&](int v) { return (v < span.sink ? v : v + span.skip) * KT; };
   auto page_ok = [&](int id) { return (uint32_t)id < (uint32_t)a.n_pages; };
-  auto tile_pages = [&](int v, TilePages<KT>& p) {
-    const int key0 = tile_key(v);
+  // the page of this wavefront's keys of a tile
+  auto tile_page = [&](int v) {
+    const int at = (tile_key(v) + 16 * wave) >> a.page_shift;
+    return table[at < a.max_pages ? at : a.max_pages - 1];
+  };
+  auto valid_keys = [&](int v, int id) { return page_ok(id) ? min(max(end - tile_key(v) - 16 * wave, 0), 16) : 0; };
+  auto k_rows = [&](int v, int id) {
+    return rows16(kbase, a.k_page * kElem, k_key, id, (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id));
+  };
+  auto v_rows = [&](int v, int id) {
+    return rows16(vbase, a.v_page * kElem, v_key, id, (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id));
+  };
+  // Through registers (e4m3, which is widened on the way, and sixteens that are not whole): fetch(), and put() some time later.
+  auto fetch = [&](__amdgpu_buffer_rsrc_t rows, uint32_t from, uint32_t key_stride, Raw (&r)[4]) {
 #pragma unroll
-    for (int h = 0; h < KT / 16; ++h) {
-      const int at = (key0 + 16 * h) >> a.page_shift;
-      p.id[h] = table[at < a.max_pages ? at : a.max_pages - 1];
+    for (int i = 0; i < 4; ++i) load_shared(rows, from + 4 * i * key_stride, r[i]);
+  };
+  auto put_k = [&](int buf, const Raw (&r)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u32x4 k;
+      if constexpr (ET == kFP8) k = e4m3_to_bf16(r[i]);
+      else k = r[i];
+      *reinterpret_cast<u32x4*>(&lds[buf][0][k_to + 1024 * i + (k_chunk ^ 64 * i)]) = k;
     }
   };
-  Raw kr[KT / 16], vr[KT / 16];
-  auto fetch = [&](int v, const TilePages<KT>& p) {
-    const int key0 = tile_key(v);
+  auto put_v = [&](int buf, const Raw (&r)[4], auto careful) {
 #pragma unroll
-    for (int h = 0; h < KT / 16; ++h) {
-      const int at = key0 + 16 * h, valid = page_ok(p.id[h]) ? min(max(end - at, 0), 16) : 0;
-      load_shared(rows16(kbase, a.k_page * kElem, k_key, p.id[h], at & page_mask, valid), k_from, kr[h]);
-      load_shared(rows16(vbase, a.v_page * kElem, v_key, p.id[h], at & page_mask, valid), v_from, vr[h]);
+    for (int i = 0; i < 4; ++i) {
+      u32x4 x;
+      if constexpr (ET == kFP8) x = e4m3_to_bf16(r[i]);
+      else x = r[i];
+      if constexpr (decltype(careful)::value) x = finite_part<false>(x);
+      *reinterpret_cast<u32x4*>(&lds[buf][1][v_to + 1024 * i]) = x;
     }
   };
-  auto put = [&](int buf, int key0, auto careful) {
+  // Straight into LDS: a load leaves its lanes' 16 bytes one behind the other, four rows, so a lane asks for the chunk that belongs
+  // in its place.
+  auto straight_k = [&](int buf, __amdgpu_buffer_rsrc_t rows) {
 #pragma unroll
-    for (int h = 0; h < KT / 16; ++h) {
-      u32x4 k, v;
-      if constexpr (ET == kFP8) { k = e4m3_to_bf16(kr[h]); v = e4m3_to_bf16(vr[h]); }
-      else { k = kr[h]; v = vr[h]; }
-      if constexpr (decltype(careful)::value) v = finite_part<false>(v);
-      const int key = key0 + 16 * h + srow;               // (keys before the window are in no row: their values are cleared)
-      if (key < any_lo && key >= a.n_sink) v = u32x4{0, 0, 0, 0};
-      *reinterpret_cast<u32x4*>(&lds[buf][0][4096 * h + k_to]) = k;
-      *reinterpret_cast<u32x4*>(&lds[buf][1][4096 * h + v_to]) = v;
+    for (int i = 0; i < 4; ++i)
+      load_to_lds(rows, srow * k_key + 4 * i * k_key + (k_chunk ^ 64 * i), &lds[buf][0][4096 * wave + 1024 * i]);
+  };
+  auto straight_v = [&](int buf, __amdgpu_buffer_rsrc_t rows) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_to_lds(rows, srow * v_key + 4 * i * v_key + ((chunk ^ srow << 2) << 4), &lds[buf][1][4096 * wave + 1024 * i]);
+  };
+  // A tile's sixteen keys of this wavefront: on their way (bring), and there (arrived, at the latest before the next barrier).
+  Raw kr[4], vr[4];
+  auto bring_k = [&](int buf, int v, int id) {
+    const auto rows = k_rows(v, id);
+    if constexpr (ET == kFP8) {
+      fetch(rows, k_from, k_key, kr);
+    } else if (valid_keys(v, id) == 16) {
+      straight_k(buf, rows);
+    } else {
+      Raw r[4];
+      fetch(rows, k_from, k_key, r);
+      put_k(buf, r);
     }
   };
+  auto bring_v = [&](int buf, int v, int id) {
+    const auto rows = v_rows(v, id);
+    if constexpr (ET == kFP8) {
+      fetch(rows, v_from, v_key, vr);
+    } else if (valid_keys(v, id) == 16) {
+      straight_v(buf, rows);
+    } else {
+      Raw r[4];
+      fetch(rows, v_from, v_key, r);
+      put_v(buf, r, std::false_type{});
+    }
+  };
+  auto arrived_k = [&](int buf) { if constexpr (ET == kFP8) put_k(buf, kr); };
+  auto arrived_v = [&](int buf) { if constexpr (ET == kFP8) put_v(buf, vr, std::false_type{}); };
 
   f32x16 o[4];
   float m, l;
+  bool bad_page = false;                                 // (as far as this wavefront knows; behind a barrier: of every tile brought in before)
   auto reset = [&]() {
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -132,89 +189,142 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
     m = -INFINITY;
     l = 0.f;
   };
-  // one tile from a buffer; s: its weights
-  auto attend = [&](int buf, int key0, const TilePages<KT>& pages, f32x16 (&s)[2]) {
+  // operands: elements 16 e .. 16 e + 15 of keys 32 kt .. 32 kt + 31; elements 32 d .. 32 d + 31 of keys 16 x .. 16 x + 15, transposed
+  auto key_operand = [&](int buf, int e, int kt) {
+    return *reinterpret_cast<const u32x4*>(&lds[buf][0][8192 * kt + k_at + (k_swap ^ 32 * e)]);
+  };
+  auto value_operand = [&](int buf, int x, int d) {
+    const char* from = &lds[buf][1][4096 * x + v_at + ((d ^ quad) << 6)];
+    const u32x2 v0 = read_transposed(from), v1 = read_transposed(from + 2048);
+    return u32x4{v0.x, v0.y, v1.x, v1.y};
+  };
+  auto score = [&](int buf, f32x16 (&s)[2]) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const u32x4 k = *reinterpret_cast<const u32x4*>(&lds[buf][0][8192 * kt + k_at + (k_swap ^ 32 * e)]);
-        s[kt] = mfma32(k, q[e], s[kt]);
+      for (int e = 0; e < 8; ++e) s[kt] = mfma32(key_operand(buf, e, kt), q[e], s[kt]);
+    }
+  };
+  // keys outside the row's set: key 32 kt + 8 (i / 4) + i % 4 of the tile, from this lane's first one on
+  auto mask = [&](int v, f32x16 (&s)[2]) {
+    const int key0 = tile_key(v);
+    if (!bad_page && key0 + KT - 1 <= min_hi && (key0 >= max_lo || key0 + KT <= a.n_sink)) return false;
+    const int at = key0 + 4 * u, to = hi - at, from = lo - at, sink = a.n_sink - at;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int page = (key0 + 16 * x) >> a.page_shift;
+      const bool ok = page_ok(table[page < a.max_pages ? page : a.max_pages - 1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = 8 * (x & 1) + j, key = 32 * (x >> 1) + 8 * (i >> 2) + (i & 3);
+        s[x >> 1][i] = ok && key <= to && (key >= from || key < sink) ? s[x >> 1][i] : -INFINITY;
       }
     }
-    bool good = true;
-#pragma unroll
-    for (int h = 0; h < KT / 16; ++h) good = good && page_ok(pages.id[h]);
-    if (!(good && key0 + KT - 1 <= min_hi && (key0 >= max_lo || key0 + KT <= a.n_sink))) {
-      // keys outside the row's set: key 32 kt + 8 (i / 4) + i % 4 of the tile, from this lane's first one on
-      const int at = key0 + 4 * u, to = hi - at, from = lo - at, sink = a.n_sink - at;
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * kt + 8 * (i >> 2) + (i & 3);
-          const bool ok = page_ok(pages.id[2 * kt + (i >> 3)]);
-          s[kt][i] = ok && key <= to && (key >= from || key < sink) ? s[kt][i] : -INFINITY;
-        }
-    }
+    return true;
+  };
+  auto largest = [&](const f32x16 (&s)[2]) {
     float top = s[0][0];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
-    top *= to_log2;
-    if (__any(top > m + 8.f)) {
-      const float m1 = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-      const float by = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
-      m = m1;
-      l *= by;
+    return top;
+  };
+  auto raise = [&](float top) {
+    if (!__any(top > m + 8.f)) return;
+    const float m1 = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+    const float by = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+    m = m1;
+    l *= by;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) o[d] *= by;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
-    u32x4 p[4];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[kt][i] = __builtin_amdgcn_exp2f(fmaf(s[kt][i], to_log2, -ref));
-        l += s[kt][i];
-        if (i & 1) p[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(s[kt][i - 1], s[kt][i]);
-      }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)                            // sixteen keys
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {                        // 32 elements
-        const char* from = &lds[buf][1][4096 * x + v_at + ((d ^ quad) << 6)];
-        const u32x2 v0 = read_transposed(from), v1 = read_transposed(from + 2048);
-        o[d] = mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[x], o[d]);
-      }
+    for (int d = 0; d < 4; ++d) o[d] *= by;
+  };
+  // weight n of the lane's 32
+  auto weigh = [&](int n, float ref, f32x16 (&s)[2], u32x4 (&p)[4]) {
+    const int kt = n >> 4, i = n & 15;
+    s[kt][i] = __builtin_amdgcn_exp2f(fmaf(s[kt][i], to_log2, -ref));
+    l += s[kt][i];
+    if (i & 1) p[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(s[kt][i - 1], s[kt][i]);
   };
 
+  // The tiles, two steps of a tile in flight: while the weights of tile v are worked out, the matrix unit forms the scores of
+  // tile v + 1.  Buffer v % 2 of the values holds tile v, buffer (v + 1) % 2 of the keys tile v + 1; tile v + 2's keys and
+  // tile v + 1's values are on their way.
   reset();
   if (t_begin < t_end) {
-    TilePages<KT> now, next;
-    tile_pages(t_begin, now);
-    fetch(t_begin, now);
-    if (t_begin + 1 < t_end) tile_pages(t_begin + 1, next);
-    put(0, tile_key(t_begin), std::false_type{});
+    // (tiles from wave_end on hold keys behind all of the wavefront's rows: it only helps to bring them in)
+    const int reach = wave_hi / KT, reach_v = reach < span.sink ? reach : max(reach - span.skip, span.sink - 1);
+    const int wave_end = wave_hi < 0 ? t_begin : min(max(reach_v + 1, t_begin), t_end);
+    const int id = tile_page(t_begin);
+    int id1 = t_begin + 1 < t_end ? tile_page(t_begin + 1) : 0;
+    if (!page_ok(id) || !page_ok(id1)) bad_pages = 1;
+    bring_k(t_begin & 1, t_begin, id);
+    bring_v(t_begin & 1, t_begin, id);
+    arrived_k(t_begin & 1);
+    arrived_v(t_begin & 1);
+    if (t_begin + 1 < t_end) {
+      bring_k((t_begin + 1) & 1, t_begin + 1, id1);
+      arrived_k((t_begin + 1) & 1);
+    }
+    stored();
     __syncthreads();
+    f32x16 s[2];
+    if (t_begin < wave_end) {
+      bad_page = bad_pages;
+      score(t_begin & 1, s);
+      mask(t_begin, s);
+      raise(largest(s) * to_log2);
+    }
+    __syncthreads();                                       // (the first tile's keys have been read: another's take their place)
 #pragma unroll 1
     for (int v = t_begin; v < t_end; ++v) {
-      const int buf = (v - t_begin) & 1, key0 = tile_key(v);
-      TilePages<KT> after = next;
-      if (v + 1 < t_end) fetch(v + 1, next);
-      if (v + 2 < t_end) tile_pages(v + 2, after);
-      if (key0 <= wave_hi) {
-        f32x16 s[2];
-        attend(buf, key0, now, s);
+      if (v + 1 < t_end) bring_v((v + 1) & 1, v + 1, id1);
+      if (v + 2 < t_end) {
+        id1 = tile_page(v + 2);
+        bring_k(v & 1, v + 2, id1);
+        if (!page_ok(id1)) bad_pages = 1;
       }
-      if (v + 1 < t_end) put(buf ^ 1, tile_key(v + 1), std::false_type{});
+      if (v < wave_end) {
+        // Step by step, in this order: a product, the operand of the one kAhead further on, and as much of the weights as the product
+        // takes.  Steps 0 .. 15 are the scores of tile v + 1 (behind the last tile those of an old one, unused), 16 .. 31 the output of tile v.
+        f32x16 next[2];
+        u32x4 p[4], operand[kAhead];
+        const float ref = m == -INFINITY ? 0.f : m;
+        float top = -INFINITY;
+        auto request = [&](auto at) {
+          constexpr int step = decltype(at)::value;
+          if constexpr (step < 16) operand[step % kAhead] = key_operand((v + 1) & 1, step >> 1, step & 1);
+          else if constexpr (step < 32) operand[step % kAhead] = value_operand(v & 1, (step - 16) >> 2, step & 3);
+        };
+        each<0, kAhead>(request);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { next[0][i] = 0.f; next[1][i] = 0.f; }
+        each<0, 32>([&](auto at) {
+          constexpr int step = decltype(at)::value;
+          if constexpr (step < 16) next[step & 1] = mfma32(operand[step % kAhead], q[step >> 1], next[step & 1]);
+          else o[step & 3] = mfma32(operand[step % kAhead], p[(step - 16) >> 2], o[step & 3]);
+          request(std::integral_constant<int, step + kAhead>{});
+          if constexpr (step < 24) {                       // of the 32 weights
+            each<step * 4 / 3, (step + 1) * 4 / 3>([&](auto n) { weigh(decltype(n)::value, ref, s, p); });
+          } else {
+            each<4 * (step - 24), 4 * (step - 23)>([&](auto n) { top = fmaxf(top, next[decltype(n)::value >> 4][decltype(n)::value & 15]); });
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if (v + 1 < wave_end) {
+          bad_page = bad_pages;
+          if (mask(v + 1, next)) top = largest(next);
+          raise(top * to_log2);
+        }
+        s[0] = next[0];
+        s[1] = next[1];
+      }
+      if (v + 1 < t_end) arrived_v((v + 1) & 1);
+      if (v + 2 < t_end) arrived_k(v & 1);
+      stored();
       __syncthreads();
-      now = next;
-      next = after;
     }
   }
   // An infinity or a NaN of V reaches rows that do not attend its key (a weight of 0 does not clear it) and leaves a NaN
@@ -230,15 +340,27 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
     float* weights = reinterpret_cast<float*>(&lds[1][0][0]) + (32 * wave + c) * KT;
 #pragma unroll 1
     for (int v = t_begin; v < t_end; ++v) {
-      const int key0 = tile_key(v);
-      TilePages<KT> now;
-      tile_pages(v, now);
-      fetch(v, now);
-      put(0, key0, std::true_type{});
+      const int key0 = tile_key(v), id0 = tile_page(v);
+      Raw r[4];
+      fetch(k_rows(v, id0), k_from, k_key, r);
+      put_k(0, r);
+      fetch(v_rows(v, id0), v_from, v_key, r);
+      put_v(0, r, std::true_type{});
       __syncthreads();
       if (key0 <= wave_hi) {
         f32x16 s[2];
-        attend(0, key0, now, s);
+        u32x4 p[4];
+        bad_page = true;
+        score(0, s);
+        mask(v, s);
+        raise(largest(s) * to_log2);
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int n = 0; n < 32; ++n) weigh(n, ref, s, p);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[d] = mfma32(value_operand(0, x, d), p[x], o[d]);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
