@@ -82,10 +82,18 @@ inline int hash_f32_keys(int K, int64_t groups32, int64_t groups64) {
   return K >= 5 && 7 * fullest(groups64) < 4 * fullest(groups32) ? 64 : 32;
 }
 
-// Whether one workgroup does a step's page plan (its prefix sums lie in LDS, its slots are filled in by 1024 threads) or
-// two launches do.
-constexpr int kPlanInOneRequests = 2048, kPlanInOneTokens = 8192;
-inline bool page_plan_in_one(int batch, int64_t max_tokens) { return batch <= kPlanInOneRequests && max_tokens <= kPlanInOneTokens; }
+// ---- page plan -----------------------------------------------------------------------------------------
+// Workgroups of a step's page plan in one launch, every one with all prefix sums in its LDS; 0: two launches, sums first.  Several
+// workgroups need inputs that are not written over.
+constexpr int kPlanInOneRequests = 2048, kPlanInOneTokens = 8192, kPlanMostWorkgroups = 128;
+inline int page_plan_workgroups(int batch, int64_t max_tokens, bool in_place) {
+  if (batch > kPlanInOneRequests) return 0;
+  if (in_place) return max_tokens <= kPlanInOneTokens ? 1 : 0;
+  const int64_t n = (max_tokens + 1023) / 1024;
+  return n <= 2 ? 1 : (int)(n < kPlanMostWorkgroups ? n : kPlanMostWorkgroups);
+}
+// Whether either kind of call may need the workspace.
+inline bool page_plan_needs_workspace(int batch, int64_t max_tokens) { return page_plan_workgroups(batch, max_tokens, true) == 0; }
 
 // ---- paged attention ------------------------------------------------------------------------------
 // rows: query rows (new tokens times the query heads of a KV head) that a workgroup takes at once; key_tile:

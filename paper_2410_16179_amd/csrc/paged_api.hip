@@ -64,7 +64,7 @@ constexpr size_t kCounterBytes = MAGICPIG_PAGED_COUNTER_BYTES;
 static_assert(kCounterBytes == mp::kPagedCounters * sizeof(unsigned), "");
 size_t ws_attention(const mp::PagedForm& f) { return kCounterBytes + align256((size_t)f.slots * f.rows * mp::kPartialStride * sizeof(float)); }
 size_t ws_plan(const Params* p) {
-  return mp::page_plan_in_one(p->batch, p->max_tokens) ? 0 : kCounterBytes + align256((size_t)3 * (p->batch + 1) * sizeof(int));
+  return !mp::page_plan_needs_workspace(p->batch, p->max_tokens) ? 0 : kCounterBytes + align256((size_t)3 * (p->batch + 1) * sizeof(int));
 }
 
 }  // namespace
