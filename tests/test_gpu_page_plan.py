@@ -192,8 +192,16 @@ def test_append_rounds_to_e4m3_as_defined():
     same(pools, want)
     # signs of zeros as well
     assert torch.equal(torch.signbit(pools[0].float()) & (pools[0].float() == 0), torch.signbit(want[0].float()) & (want[0].float() == 0))
-    scale = torch.full((1,), 0.37, device="cuda")
-    same(*append("fp8", n, 1, 64, "token", list(range(n)), (scale, scale), values=values))
+    # scales: ordinary ones, powers of two, the ends of what is taken from a reciprocal, below and above, zero, infinity, NaN, negative
+    scales = [0.37, 1.0 / 3.0, 0.0123456, 1.9999999, 2.0 ** -7, 3.0 * 2.0 ** -9, 2.0 ** -99, 2.0 ** -101, 1e-40, 2.0 ** 99, 3e38, 0.0, float("inf"),
+              float("nan"), -0.6]
+    for k, v in zip(scales, scales[1:] + scales[:1]):
+        one = [torch.full((1,), x, device="cuda") for x in (k, v)]
+        pools, want = append("fp8", n, 1, 64, "token", list(range(n)), one, values=values)
+        same(pools, want)
+        for got, w in zip(pools, want):
+            zero = (w.float() == 0)
+            assert torch.equal(torch.signbit(got.float()) & zero, torch.signbit(w.float()) & zero)
 
 
 def test_a_grid_s_worth_and_more():
