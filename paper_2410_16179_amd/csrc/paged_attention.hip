@@ -221,8 +221,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   }
   const int min_hi = len - tokens + first;               // what every row of the tile attends: [max_lo, min_hi]
   const int max_lo = a.n_local > 0 ? len - tokens + last - a.n_local + 1 : 0;
-  const int end = len - tokens + last + 1;               // what some row attends: [any_lo, end), and the keys below n_sink
-  const int any_lo = a.n_local > 0 ? len - tokens + first - a.n_local + 1 : 0;
+  const int end = len - tokens + last + 1;               // behind what some row attends
   const float to_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[g] : 1.f);
 
   const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)item.b * a.max_pages);
@@ -390,8 +389,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     }
   };
 
-  // Tiles whose keys every row attends, one after the other: the next one's K is requested when the scores have taken this
-  // one's, its V behind the products with this one's.
+  // whether every row attends all keys of a tile
   auto in_full = [&](int v) {
     const int key0 = tile_key(v);
     return key0 + KT - 1 <= min_hi && (key0 >= max_lo || key0 + KT <= a.n_sink);
@@ -403,7 +401,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     return ok;
   };
   bool bad_page = false;
-  // the first such tile from v on, its pages read
+  // the first such tile from v on with pages that are there; they are read
   auto find = [&](int v, TilePages<KT>& p) {
     for (; v < t_end; v += kPagedGroup) {
       if (!in_full(v)) continue;
@@ -413,9 +411,24 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     }
     return v;
   };
-  int all16[F::kHalves];
+  // rows of the tile's halves that are there
+  auto valid_rows = [&](int key0, const TilePages<KT>& p, int (&valid)[F::kHalves]) {
 #pragma unroll
-  for (int h = 0; h < F::kHalves; ++h) all16[h] = 16;
+    for (int h = 0; h < F::kHalves; ++h) valid[h] = page_ok(p.id[h]) ? min(max(end - key0 - 16 * h, 0), 16) : 0;
+  };
+  // keys outside the rows' sets get no weight
+  auto mask = [&](int key0, const int (&valid)[F::kHalves], float (&s)[NR][kScores]) {
+#pragma unroll
+    for (int h = 0; h < F::kHalves; ++h) {
+      const int at = key0 + 16 * h + 4 * u;               // key i of this lane is at + i
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const int to = valid[h] ? hi[n] - at : -1, from = lo[n] - at, sink = a.n_sink - at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][4 * h + i] = i <= to && (i >= from || i < sink) ? s[n][4 * h + i] : -INFINITY;
+      }
+    }
+  };
   TilePages<KT> now{}, next{}, after{};
   auto reset = [&]() {
 #pragma unroll
@@ -427,24 +440,50 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     }
   };
   reset();
-  int v = find(t_begin + wave, now), v1 = t_end;
-  if (v < t_end) {
-    request_k(tile_key(v), now, all16);
-    request_v(tile_key(v), now, all16);
-    v1 = find(v + kPagedGroup, next);
+  // The tiles, whole ones and then the others (the last ones, the borders of the window and of the sink): the next one's K is requested
+  // when the scores have taken this one's, its V behind the products with this one's.
+  auto other = [&](int v) {                               // the first of the others from v on
+    while (v < t_end && in_full(v)) v += kPagedGroup;
+    return v;
+  };
+  int w = t_begin + wave;
+  if (a.n_local == 0) {                                   // (only from the first key on that some row does not attend)
+    const int from = (min_hi + 1 > 0 ? min_hi + 1 : 0) / KT;
+    if (from > w) w += (from - w + kPagedGroup - 1) / kPagedGroup * kPagedGroup;
   }
+  w = other(w);
+  TilePages<KT> w_pages{};
+  if (w < t_end) tile_pages(w, w_pages);
+  int v = find(t_begin + wave, now), v1 = t_end;
+  int valid[F::kHalves];
+  {
+    const int first_tile = v < t_end ? v : w;
+    if (first_tile < t_end) {
+      const int key0 = tile_key(first_tile);
+      const TilePages<KT> p = v < t_end ? now : w_pages;
+      valid_rows(key0, p, valid);
+      request_k(key0, p, valid);
+      request_v(key0, p, valid);
+    }
+  }
+  if (v < t_end) v1 = find(v + kPagedGroup, next);
 #pragma unroll 1
   while (v < t_end) {
-    const int v2 = v1 + kPagedGroup;
+    const int v2 = v1 + kPagedGroup, ahead = v1 < t_end ? v1 : w;
     if (v2 < t_end) tile_pages(v2, after);
+    const int key1 = tile_key(ahead);
+    const TilePages<KT> p = v1 < t_end ? next : w_pages;
     float s[NR][kScores];
     scores(s);
-    if (v1 < t_end) request_k(tile_key(v1), next, all16);
+    if (ahead < t_end) {
+      valid_rows(key1, p, valid);
+      request_k(key1, p, valid);
+    }
     weigh(s);
     u32x4 vb[8];
     values(vb);
     add_values(s, vb);
-    if (v1 < t_end) request_v(tile_key(v1), next, all16);
+    if (ahead < t_end) request_v(key1, p, valid);
     v = v1;
     v1 = v2;
     next = after;
@@ -453,60 +492,60 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       v1 = find(v1 + kPagedGroup, next);
     }
   }
-
-  // The others: the last ones, the borders of the window and of the sink, tiles with a page that is none.
-  auto others = [&](auto all) {
-    constexpr bool CAREFUL = decltype(all)::value;
-    int v = t_begin + wave;
-    if (a.n_local == 0 && !bad_page && !CAREFUL) {   // only from the first key on that some row does not attend
-      const int from = (min_hi + 1 > 0 ? min_hi + 1 : 0) / KT;
-      if (from > v) v += (from - v + kPagedGroup - 1) / kPagedGroup * kPagedGroup;
-    }
 #pragma unroll 1
-    for (; v < t_end; v += kPagedGroup) {
-      const bool inside = in_full(v);
-      if (inside && !bad_page && !CAREFUL) continue;
-      tile_pages(v, now);
-      if (inside && !CAREFUL && pages_ok(now)) continue;
-      const int key0 = tile_key(v);
-      int valid[F::kHalves];
+  while (w < t_end) {
+    const int key0 = tile_key(w), w1 = other(w + kPagedGroup);
+    TilePages<KT> p{};
+    if (w1 < t_end) tile_pages(w1, p);
+    float s[NR][kScores];
+    scores(s);
+    mask(key0, valid, s);
+    if (w1 < t_end) {
+      valid_rows(tile_key(w1), p, valid);
+      request_k(tile_key(w1), p, valid);
+    }
+    weigh(s);
+    u32x4 vb[8];
+    values(vb);
+    add_values(s, vb);
+    if (w1 < t_end) request_v(tile_key(w1), p, valid);
+    w = w1;
+  }
+
+  // The products take every row of a tile with every key's V: an infinity or a NaN there reaches rows that do not attend the key
+  // (a weight of 0 does not clear it), and an infinity may come out as a NaN (the two parts of a weight differ in sign).
+  // Either leaves a NaN in the output, so a wavefront that ends with one goes over its tiles again, carefully: what is
+  // not finite is left out of the products and added afterwards to the rows that attend its key.  So does one that met a page that is none.
+  float sum = 0.f;                                       // NaN if one of them is, or if infinities meet
 #pragma unroll
-      for (int h = 0; h < F::kHalves; ++h) valid[h] = page_ok(now.id[h]) ? min(max(end - key0 - 16 * h, 0), 16) : 0;
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int t8 = 0; t8 < 8; ++t8) sum += (f.o[n][t8][0] + f.o[n][t8][1]) + (f.o[n][t8][2] + f.o[n][t8][3]);
+  if (bad_page || __any(sum != sum)) {
+    reset();
+#pragma unroll 1
+    for (int v = t_begin + wave; v < t_end; v += kPagedGroup) {
+      const int key0 = tile_key(v);
+      tile_pages(v, now);
+      valid_rows(key0, now, valid);
       request_k(key0, now, valid);
       request_v(key0, now, valid);
       float s[NR][kScores];
       scores(s);
-#pragma unroll
-      for (int h = 0; h < F::kHalves; ++h) {
-        const int at = key0 + 16 * h + 4 * u;               // key i of this lane is at + i
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-          const int to = valid[h] ? hi[n] - at : -1, from = lo[n] - at, sink = a.n_sink - at;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[n][4 * h + i] = i <= to && (i >= from || i < sink) ? s[n][4 * h + i] : -INFINITY;
-        }
-      }
+      mask(key0, valid, s);
       weigh(s);
       u32x4 vb[8];
       values(vb);
-      // V of the keys before the window is cleared (those behind the last one were read as zeros)
+      uint32_t cleared = 0;
 #pragma unroll
-      for (int h = 0; h < F::kHalves; ++h) {
-        const int at = key0 + 16 * h + 4 * u, from = any_lo - at, sink = a.n_sink - at;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t keep = i >= from || i < sink ? ~0u : 0u;
-#pragma unroll
-          for (int d = 0; d < (kF32 ? 2 : 1); ++d) vb[kF32 ? 2 * i + d : 4 * h + i] &= keep;
-        }
-      }
-      if (CAREFUL) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) vb[i] = finite_part<kF32>(vb[i]);
+      for (int i = 0; i < 8; ++i) {
+        const u32x4 x = finite_part<kF32>(vb[i]), d = x ^ vb[i];
+        cleared |= d.x | d.y | d.z | d.w;
+        vb[i] = x;
       }
       add_values(s, vb);
-      if (!CAREFUL) continue;
-      // what was cleared, added key by key to the rows that attend the key; the weights change lanes through LDS
+      if (!__any(cleared != 0)) continue;
+      // (the weights change lanes through LDS)
 #pragma unroll
       for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -538,21 +577,6 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
         }
       }
     }
-  };
-  others(std::false_type{});
-
-  // The products take every row of a tile with every key's V: an infinity or a NaN there reaches rows that do not attend the key
-  // (a weight of 0 does not clear it), and an infinity may come out as a NaN (the two parts of a weight differ in sign).
-  // Either leaves a NaN in the output, so a wavefront that ends with one goes over its tiles again, carefully: what is
-  // not finite is left out of the products and added afterwards to the rows that attend its key.
-  float sum = 0.f;                                       // NaN if one of them is, or if infinities meet
-#pragma unroll
-  for (int n = 0; n < NR; ++n)
-#pragma unroll
-    for (int t8 = 0; t8 < 8; ++t8) sum += (f.o[n][t8][0] + f.o[n][t8][1]) + (f.o[n][t8][2] + f.o[n][t8][3]);
-  if (__any(sum != sum)) {
-    reset();
-    others(std::true_type{});
   }
 
   // the wavefronts' parts, joined in LDS
