@@ -320,8 +320,10 @@ __device__ inline void paged_next(const PagedArgs& a, PagedShare& s) {
   s.pos = min(s.base + (k + 1) * groups, s.end);
   if (s.pos < s.end && s.pos == next) {
     s.base = next;
-    do s.r = paged_request(a, ++s.b);
-    while (s.r.tokens == 0);
+    do {
+      if (++s.b >= a.batch) { s.pos = s.end; return; }     // (not reached while the requests stay as they were counted)
+      s.r = paged_request(a, s.b);
+    } while (s.r.tokens == 0);
   }
 }
 

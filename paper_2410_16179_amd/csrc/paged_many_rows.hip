@@ -72,8 +72,9 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
   const int min_hi = len - tokens + first + t0, wave_hi = busy ? len - tokens + first + t1 : -1;
   const int max_lo = a.n_local > 0 ? wave_hi - a.n_local + 1 : 0;
   const int end = len - tokens + last + 1;
-  // a negative scale goes to the queries, so that the largest score is the largest product
-  const float signed_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f), to_log2 = fabsf(signed_log2);
+  // a negative scale goes to the queries, so that the largest score is the largest product; one of 0 becomes the smallest number
+  // there is, which leaves the -inf of a masked score what it is
+  const float signed_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f), to_log2 = signed_log2 == 0.f ? 1.17549435e-38f : fabsf(signed_log2);
   const uint32_t flip = signed_log2 < 0.f ? 0x80008000u : 0u;
 
   u32x4 q[8];

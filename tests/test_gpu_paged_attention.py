@@ -201,6 +201,79 @@ def test_logits_beyond_the_exponential_s_range():
         Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[300, 40], new=new, scale=-0.7, spread=3.0, seed=2).check()
 
 
+@pytest.mark.parametrize("kind,new", [("bf16", None), ("fp32", [3, 5]), ("fp8", None), ("bf16", [40, 40])])
+def test_infinite_keys(kind, new):
+    # a logit of +inf leaves NaN in its row, one of -inf takes the key out
+    p = Problem(kind=kind, heads=4, kv_heads=2, page=16, lengths=[90, 41], new=new, seed=21)
+    big = 448.0 if kind == "fp8" else float("inf")
+    p.k[int(p.table[0, 2]), 3, 0, 7] = big
+    p.k[int(p.table[1, 1]), 9, 1, 100] = -big
+    p.upload()
+    if kind == "fp8":
+        p.check()
+        return
+    out, lse = p.run()
+    want, want_lse, size, reach, count = p.reference()
+    nan = np.isnan(want).any(-1)
+    assert nan.any() and (~nan).any()
+    np.testing.assert_array_equal(np.isnan(out).any(-1), nan)
+    tol = ref.tolerance(want, size, np.where(np.isfinite(reach), reach, 40.0), count, kind, new == [40, 40])
+    assert (np.abs(out - want)[~nan] <= tol[~nan]).all()
+
+
+@pytest.mark.parametrize("new", [None, [3, 2, 1], [40, 9, 64]])
+def test_scales_of_zero_and_below(new):
+    p = Problem(kind="fp8", heads=6, kv_heads=3, page=16, lengths=[90, 12, 64], new=new, seed=22, spare_rows=1 if new else 0)
+    p.ks = torch.tensor([0.0, -0.02, 0.015])
+    p.vs = torch.tensor([0.02, 0.0, -0.03])
+    p.upload()
+    p.check()
+
+
+@pytest.mark.parametrize("how", [dict(kind="bf16", lengths=[30000, 700]), dict(kind="fp8", lengths=[9000, 9001, 40]), dict(kind="fp32", lengths=[7000]),
+                                 dict(kind="bf16", lengths=[6000, 900], new=[120, 64])])
+def test_the_same_bits_every_time(how):
+    # partials are joined in the order of the keys, whichever workgroup comes last
+    p = Problem(heads=8, kv_heads=2, page=32, seed=23, **how)
+    first = p.run()
+    for _ in range(5):
+        again = p.run()
+        np.testing.assert_array_equal(first[0], again[0])
+        np.testing.assert_array_equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_pools_beyond_4_gib(new):
+    heads, page, n = 2, 16, 700
+    n_pages = (5 << 30) // (page * 2 * D)                 # bf16, one KV head: 5 GiB a pool
+    g = torch.Generator(device="cuda").manual_seed(24)
+    k, v = (torch.empty(n_pages, page, 1, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    held = -(-n // page)
+    ids = torch.tensor([n_pages - 1 - 7 * j for j in range(held)], dtype=torch.int64, device="cuda")
+    for pool in (k, v):
+        pool[ids] = torch.randn(held, page, 1, D, generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.randn(new, heads, D, generator=g, device="cuda").to(torch.bfloat16)
+    out, lse = torch.zeros_like(q), torch.zeros(new, heads, device="cuda")
+    p = mp.make_paged_params(batch=1, n_q_heads=heads, n_kv_heads=1, dtype="bf16", page_size=page, max_pages=held, n_pages=n_pages, max_tokens=new,
+                             max_new=new)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    mp.magicpig_paged_attention(p, q, k, v, None, None, ids.to(torch.int32)[None].contiguous(), i32([n]), i32([0, new]), out, lse,
+                                mp.alloc_paged_workspace(p))
+    small = Problem(kind="bf16", heads=heads, kv_heads=1, page=page, lengths=[n], new=[new])
+    small.table = np.arange(held, dtype=np.int32)[None]
+    small.k, small.v, small.q = k[ids].cpu(), v[ids].cpu(), q.cpu()
+    small.single = False
+    want, want_lse, size, reach, count = small.reference()
+    tol = ref.tolerance(want, size, reach, count, "bf16", new * heads > 32)
+    assert (np.abs(out.cpu().double().numpy() - want) <= tol).all()
+    # and the append reaches the far end
+    rows = torch.randn(1, 1, D, generator=g, device="cuda").to(torch.bfloat16)
+    slot = (n_pages - 1) * page + page - 1
+    one = mp.make_paged_params(batch=1, n_q_heads=1, n_kv_heads=1, dtype="bf16", page_size=page, max_pages=1, n_pages=n_pages, max_tokens=1)
+    mp.magicpig_page_append(one, rows, rows, torch.tensor([slot], device="cuda"), None, None, k, v)
+    assert torch.equal(k[n_pages - 1, page - 1], rows[0]) and torch.equal(v[n_pages - 1, page - 1], rows[0])
+
+
 def test_strided_queries_and_either_form_of_single_tokens():
     p = Problem(kind="bf16", heads=8, kv_heads=2, page=16, lengths=[300, 40, 1], q_wide=4, seed=4)
     a, b = p.run(False), p.run(True)

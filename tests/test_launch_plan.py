@@ -1,5 +1,6 @@
 """The rules of csrc/launch_plan.h, compiled on their own."""
 import ctypes
+import math
 import os
 import subprocess
 
@@ -14,6 +15,13 @@ void gather(int units, int G, long nblk, long n_static, int tau, int* got) {
   got[0] = p.run_blocks; got[1] = p.runs; got[2] = p.static_runs; got[3] = p.static_keys; got[4] = p.full;
 }
 long head_limit(int tuned, int G) { return mp::head_per_workgroup_limit(tuned, G); }
+void paged(int batch, int kv, int group, int fp32, long max_tokens, int max_new, int starts, long max_len, int n_sink, int n_local, long* got) {
+  const mp::PagedForm f = mp::paged_form(batch, kv, group, fp32, max_tokens, max_new, starts, max_len, n_sink, n_local);
+  const long all[] = {f.rows, f.key_tile, f.tile_tokens, f.head_blocks, f.target, f.min_tiles, f.shares, f.min_share, f.group_shift, f.items, f.pieces,
+                      f.units, f.slots};
+  for (int i = 0; i < 13; ++i) got[i] = all[i];
+}
+int plan_workgroups(int batch, long max_tokens, int in_place) { return mp::page_plan_workgroups(batch, max_tokens, in_place); }
 int hash_f32(int K, long groups32, long groups64) { return mp::hash_f32_keys(K, groups32, groups64); }
 }
 """
@@ -89,3 +97,67 @@ def test_keys_of_a_float32_hashing_workgroup(plan, K, groups32, keys):
 def test_head_per_workgroup(plan, units, G, n, tuned, one):
     plan.head_limit.restype = ctypes.c_long
     assert (units * (-(-n // 256)) * G <= plan.head_limit(int(tuned), G)) == one
+
+
+_PAGED = ("rows", "key_tile", "tile_tokens", "head_blocks", "target", "min_tiles", "shares", "min_share", "group_shift", "items", "pieces", "units", "slots")
+
+
+def paged(plan, batch, kv, group, fp32=False, max_tokens=None, max_new=1, starts=False, max_len=4096, n_sink=0, n_local=0):
+    got = (ctypes.c_long * len(_PAGED))()
+    plan.paged(batch, kv, group, int(fp32), ctypes.c_long(batch if max_tokens is None else max_tokens), max_new, int(starts), ctypes.c_long(max_len),
+               n_sink, n_local, got)
+    return dict(zip(_PAGED, got))
+
+
+def test_rows_of_paged_attention_s_forms(plan):
+    assert [paged(plan, 1, 8, g, max_new=t)["rows"] for g, t in [(1, 1), (4, 4), (16, 1), (4, 5), (32, 1), (5, 6), (4, 9), (64, 1)]] == \
+        [16, 16, 16, 32, 32, 32, 128, 128]
+    assert all(paged(plan, 1, 8, g, fp32=True, max_new=t)["rows"] == 16 for g, t in [(1, 1), (4, 100), (64, 1)])
+    f = paged(plan, 1, 1, 20, fp32=True, max_new=3)          # a token's heads in two tiles
+    assert (f["tile_tokens"], f["head_blocks"], f["items"]) == (1, 2, 6)
+    assert paged(plan, 1, 8, 5, max_new=4)["tile_tokens"] == 6
+
+
+@pytest.mark.parametrize("batch,kv,group,fp32,max_new,max_len,n_local", [
+    (1, 8, 4, False, 1, 98304, 0), (1, 8, 4, False, 1, 16, 0), (48, 8, 8, False, 1, 32768, 0), (65536, 1, 1, False, 1, 1 << 30, 0), (3, 1024, 1, False, 1, 4096, 0),
+    (7, 300, 2, True, 1, 4096, 0), (512, 8, 4, True, 8192, 131072, 0), (24, 8, 5, False, 4, 20000, 4096), (2, 1, 64, True, 1 << 20, 1 << 20, 0)])
+def test_shares_of_few_rows(plan, batch, kv, group, fp32, max_new, max_len, n_local):
+    f = paged(plan, batch, kv, group, fp32, max_tokens=batch * max_new if batch * max_new < 1 << 24 else 1 << 24, max_new=max_new, starts=max_new > 1,
+              max_len=max_len, n_local=n_local)
+    assert f["rows"] <= 32
+    # a counter and two partials for every share of every KV head; about one workgroup per compute unit, or a share for every KV head
+    assert 1 <= f["shares"] and f["shares"] * kv <= 1024 and (f["shares"] == 1 or f["shares"] * kv <= f["target"])
+    assert f["slots"] == 2 * f["shares"] * kv and f["units"] == 0
+    # workgroup i: KV head (i / 8) % kv, share (i / 8) / kv * 8 + i % 8: every one of them is there
+    seen = {((i >> 3) % kv, (i >> 3) // kv * 8 + (i & 7)) for i in range(f["pieces"])}
+    assert {(g, j) for g in range(kv) for j in range(f["shares"])} <= seen
+    # the groups of all row tiles are counted in 31 bits, a group has a key tile for each of eight wavefronts
+    assert f["group_shift"] >= 3
+    row_tiles = batch * -(-max_new // f["tile_tokens"]) * f["head_blocks"]
+    charge = -(-max_len // f["key_tile"])
+    if n_local:
+        charge = min(charge, -(-0 // f["key_tile"]) + (n_local + f["tile_tokens"] - 2) // f["key_tile"] + 2)
+    assert row_tiles * -(-charge // (1 << f["group_shift"])) + f["shares"] < 1 << 31
+    assert f["group_shift"] == 3 or row_tiles * -(-charge // (1 << (f["group_shift"] - 1))) + 1024 >= (1 << 31) - 1
+
+
+@pytest.mark.parametrize("lengths,new,kv,group", [([4099, 2392, 1395, 3337], [4099, 2392, 1395, 3337], 8, 4), ([61440], [2048], 8, 4), ([100000] * 3, [40, 9, 300], 1, 8),
+                                                  ([64] * 200, [33] * 200, 2, 4), ([130000, 20], [64, 20], 5, 1), ([1 << 20], [33], 1, 1)])
+def test_pieces_of_many_rows_have_room(plan, lengths, new, kv, group):
+    f = paged(plan, len(lengths), kv, group, max_tokens=sum(new), max_new=max(new), starts=True, max_len=max(lengths))
+    assert f["rows"] == 128
+    # what the kernel does with the lengths it finds
+    tiles = [-(-t // f["tile_tokens"]) for t in new]
+    charge = [max(1, -(-n // f["key_tile"])) for n in lengths]
+    total = sum(t * kv * c for t, c in zip(tiles, charge))
+    piece = max(math.ceil(total * 1.0001 / f["target"]), f["min_tiles"])
+    pieces = [-(-c // piece) for c in charge]
+    assert sum(t * p for t, p in zip(tiles, pieces)) * kv <= f["pieces"]
+    assert sum(t * p for t, p in zip(tiles, pieces) if p > 1) * kv <= f["slots"]
+    assert sum(t for t, p in zip(tiles, pieces) if p > 1) * kv <= f["units"]
+
+
+def test_workgroups_of_the_page_plan(plan):
+    go = lambda batch, rows, in_place: plan.plan_workgroups(batch, ctypes.c_long(rows), int(in_place))
+    assert [go(64, 64, False), go(64, 64, True), go(512, 35840, False), go(512, 35840, True), go(2048, 8192, True), go(2049, 10, False), go(2049, 10, True),
+            go(5, 1 << 24, False)] == [1, 1, 35, 0, 1, 0, 0, 128]
