@@ -347,7 +347,8 @@ MAGICPIG_API int magicpig_page_append(const magicpig_paged_params* params, const
 
 /* Exact attention of the step's tokens.  Request b has lengths[b] keys, the new ones among them, and its
  * n_b = token_start[b + 1] - token_start[b] new tokens are rows token_start[b] .. of q; token i of them
- * stands at position lengths[b] - n_b + i.  token_start NULL: one token per request, row b.  For the
+ * stands at position lengths[b] - n_b + i.  token_start ascends, as magicpig_page_plan leaves it (where it does not, rows may be
+ * left out or taken twice).  token_start NULL: one token per request, row b.  For the
  * row of a token at position p and query head h with KV head g,
  *   A = { i <= p : n_local == 0 or i < n_sink or i > p - n_local },
  *   out = sum_A w_i v_i,  w = softmax_A(scale q.k_i),  lse = log sum_A exp(scale q.k_i),

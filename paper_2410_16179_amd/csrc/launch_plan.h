@@ -101,7 +101,7 @@ inline bool page_plan_needs_workspace(int batch, int64_t max_tokens) { return pa
 // min_tiles: key tiles of a piece at least.  items, pieces, units, slots: at most so many row
 // tiles of all KV heads, workgroups, row tiles that are cut, partials.
 struct PagedForm {
-  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles, shares, min_share, group_shift;
+  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles, shares, group_shift;
   int64_t items, pieces, units, slots;
 };
 
@@ -109,7 +109,6 @@ struct PagedForm {
 // keys among 128 rows through LDS.  float32: always 16.
 constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
 constexpr int kPagedGroupShift = 3, kPagedGroup = 1 << kPagedGroupShift;   // few rows: wavefronts of a workgroup
-constexpr int kPagedMinShare = 1;
 constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share of a KV head (at most 3 kNumCU, or a share for each)
 inline int paged_rows(bool fp32, int64_t rows) { return fp32 || rows <= 16 ? 16 : (rows <= 32 ? 32 : kPagedManyRows); }
 
@@ -131,7 +130,6 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
   f.target = many ? 2 * kNumCU : kNumCU;               // workgroups that are resident at once
   f.min_tiles = 512 / f.key_tile;
-  f.min_share = kPagedMinShare;
   int64_t tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens);
   if (starts && max_tokens / f.tile_tokens + batch < tiles) tiles = max_tokens / f.tile_tokens + batch;
   f.items = tiles * f.head_blocks * kv_heads;
@@ -154,7 +152,7 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
     f.group_shift = kPagedGroupShift;
     const int64_t row_tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens) * f.head_blocks;
     while (row_tiles * groups(f.group_shift) > INT32_MAX - kPagedCounters) ++f.group_shift;
-    const int64_t least = (groups(f.group_shift) * (f.items / kv_heads) + f.min_share - 1) / f.min_share;
+    const int64_t least = groups(f.group_shift) * (f.items / kv_heads);
     const int64_t shares = f.target / kv_heads > 1 ? f.target / kv_heads : 1;
     f.shares = (int)(shares < least ? shares : (least > 1 ? least : 1));
     f.pieces = (int64_t)(f.shares + 7) / 8 * 8 * kv_heads;   // (dealt to the eight XCDs in rounds of eight)

@@ -81,10 +81,10 @@ __device__ inline void join_parts(const PagedArgs& a, float* lds, int first_shar
 
 // Behind the wavefronts' parts in `joined`: the rows of the item they belong to are written, or, where other workgroups have keys of it
 // too, a partial; the last of these workgroups joins the partials.
-template <int KT, bool F32, int NR>
-__device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, float (&joined)[kPagedGroup][16 * NR][kPartialRow], int& last_one) {
+template <bool F32, int NR>
+__device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, const PagedItem& item,
+                                   float (&joined)[kPagedGroup][16 * NR][kPartialRow], int& last_one) {
   constexpr int R = 16 * NR;
-  const PagedItem item = paged_item<KT>(a, share);
   const int tt = item.tile / a.head_blocks, hb = item.tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, item.r.tokens) - 1;
   const int rows = a.head_blocks > 1 ? min(a.G - hb * R, R) : (last - first + 1) * a.G;
@@ -115,7 +115,7 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
       float* pp = a.partial + ((int64_t)slot * R + row) * kPartialRow;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) store_through(pp + e0 + e, o[e], o[e + 1]);
-      if (e0 == 0) store_through(pp + 128, m, l);
+      if (e0 == 0) store_through(pp + 128, paged_partial_max(m, l), l);
     }
   }
   if (whole) return;
@@ -603,8 +603,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     }
     if (u == 0) { to[128] = f.m[n]; to[129] = l; }
   }
+  const PagedItem done = paged_item<KT>(a, at_share);      // (read before the barrier: behind it the first thread goes on to the next item)
   __syncthreads();
-  finish_item<KT, kF32, NR>(a, at_share, joined, last_one);
+  finish_item<kF32, NR>(a, at_share, done, joined, last_one);
   if (threadIdx.x == 0) paged_next<KT>(a, at_share);
   __syncthreads();
   if (at_share.pos >= at_share.end) return;

@@ -44,7 +44,7 @@ struct PagedArgs {
   float per_piece;        // (1 + margin) / target pieces
   int min_tiles;          // of a piece
   int slots;              // partials that there is room for
-  int shares, min_share;  // few rows: shares of a KV head, and groups of group_tiles key tiles of one at least
+  int shares;             // few rows: shares of a KV head, counted in groups of group_tiles key tiles
   int group_tiles, group_shift;
   unsigned* arrived;      // few rows: partials of the cut item that begins in a share which are there (0 between calls)
   int64_t k_page, k_key, k_head, v_page, v_key, v_head, q_t, q_h;
@@ -274,7 +274,7 @@ __device__ inline bool paged_share(const PagedArgs& a, int index, PagedShare& ou
     if (b0 == 0) {
       total += sum;
       if (total == 0) return false;
-      out.each = max((int)(((uint32_t)total + (uint32_t)a.shares - 1u) / (uint32_t)a.shares), a.min_share);
+      out.each = (int)(((uint32_t)total + (uint32_t)a.shares - 1u) / (uint32_t)a.shares);
       const int64_t begin = (int64_t)out.each * out.j;
       if (begin >= total) return false;
       out.begin = out.pos = (int)begin;
@@ -326,6 +326,10 @@ __device__ inline void paged_next(const PagedArgs& a, PagedShare& s) {
     } while (s.r.tokens == 0);
   }
 }
+
+// A partial's maximum as it is stored: an empty partial has -inf, and the join leaves it out.  One whose scores are all NaN has found no
+// maximum either, but its sum is NaN.
+__device__ inline float paged_partial_max(float m, float l) { return m == -INFINITY && l != 0.f ? 0.f : m; }
 
 // Eight elements, e0 .. e0 + 7, of a finished row: o / l (times the values' scale), and with the first ones the row's lse.
 template <bool FP32>

@@ -400,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<f32x4*>(pp + 32 * d + 8 * i + 4 * u) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-    if (u == 0) { pp[128] = m; pp[129] = l; }
+    if (u == 0) { pp[128] = paged_partial_max(m, l); pp[129] = l; }
   } else {
     const int64_t to = (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + head;
     const float by = l == 0.f ? 0.f : (a.v_scale ? a.v_scale[pc.g] : 1.f) / l;

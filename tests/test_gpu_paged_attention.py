@@ -221,6 +221,22 @@ def test_infinite_keys(kind, new):
     assert (np.abs(out - want)[~nan] <= tol[~nan]).all()
 
 
+@pytest.mark.parametrize("kind,new", [("bf16", [1, 1]), ("fp32", [2, 1]), ("fp8", [5, 1]), ("bf16", [40, 33])])
+def test_a_query_that_is_nan_over_long_keys(kind, new):
+    # its keys are cut into parts in none of which a score is larger than another
+    p = Problem(kind=kind, heads=4, kv_heads=1, page=32, lengths=[6000, 300], new=new, seed=25)
+    p.q[0, 2] = float("nan")
+    p.upload()
+    out, lse = p.run()
+    want, want_lse, size, reach, count = p.reference()
+    nan = np.zeros(lse.shape, bool)
+    nan[0, 2] = True
+    np.testing.assert_array_equal(np.isnan(out).all(-1), nan)
+    np.testing.assert_array_equal(np.isnan(lse), nan)
+    tol = ref.tolerance(want, size, np.where(nan, 0, reach), count, kind, new == [40, 33])
+    assert (np.abs(out - want)[~nan] <= tol[~nan]).all()
+
+
 @pytest.mark.parametrize("new", [None, [3, 2, 1], [40, 9, 64]])
 def test_scales_of_zero_and_below(new):
     p = Problem(kind="fp8", heads=6, kv_heads=3, page=16, lengths=[90, 12, 64], new=new, seed=22, spare_rows=1 if new else 0)

@@ -17,9 +17,9 @@ void gather(int units, int G, long nblk, long n_static, int tau, int* got) {
 long head_limit(int tuned, int G) { return mp::head_per_workgroup_limit(tuned, G); }
 void paged(int batch, int kv, int group, int fp32, long max_tokens, int max_new, int starts, long max_len, int n_sink, int n_local, long* got) {
   const mp::PagedForm f = mp::paged_form(batch, kv, group, fp32, max_tokens, max_new, starts, max_len, n_sink, n_local);
-  const long all[] = {f.rows, f.key_tile, f.tile_tokens, f.head_blocks, f.target, f.min_tiles, f.shares, f.min_share, f.group_shift, f.items, f.pieces,
+  const long all[] = {f.rows, f.key_tile, f.tile_tokens, f.head_blocks, f.target, f.min_tiles, f.shares, f.group_shift, f.items, f.pieces,
                       f.units, f.slots};
-  for (int i = 0; i < 13; ++i) got[i] = all[i];
+  for (int i = 0; i < 12; ++i) got[i] = all[i];
 }
 int plan_workgroups(int batch, long max_tokens, int in_place) { return mp::page_plan_workgroups(batch, max_tokens, in_place); }
 int hash_f32(int K, long groups32, long groups64) { return mp::hash_f32_keys(K, groups32, groups64); }
@@ -99,7 +99,7 @@ def test_head_per_workgroup(plan, units, G, n, tuned, one):
     assert (units * (-(-n // 256)) * G <= plan.head_limit(int(tuned), G)) == one
 
 
-_PAGED = ("rows", "key_tile", "tile_tokens", "head_blocks", "target", "min_tiles", "shares", "min_share", "group_shift", "items", "pieces", "units", "slots")
+_PAGED = ("rows", "key_tile", "tile_tokens", "head_blocks", "target", "min_tiles", "shares", "group_shift", "items", "pieces", "units", "slots")
 
 
 def paged(plan, batch, kv, group, fp32=False, max_tokens=None, max_new=1, starts=False, max_len=4096, n_sink=0, n_local=0):
