@@ -312,7 +312,7 @@ typedef struct magicpig_paged_params {
  * aligned.  Its first MAGICPIG_PAGED_COUNTER_BYTES have to be zero before its first use; the calls leave them
  * zero again (they count, within magicpig_paged_attention, the parts of a row's sum that have arrived: a row whose count
  * starts elsewhere is left unwritten, or is written before all parts are there).  The rest need not be initialised or
- * preserved.  magicpig_page_plan needs a workspace for more than 2048 requests or 8192 token rows only. */
+ * preserved.  magicpig_page_plan needs a workspace for more than 2048 requests or 4096 token rows only. */
 #define MAGICPIG_PAGED_COUNTER_BYTES 4096u
 MAGICPIG_API size_t magicpig_paged_workspace_bytes(const magicpig_paged_params* params);
 

@@ -84,8 +84,11 @@ inline int hash_f32_keys(int K, int64_t groups32, int64_t groups64) {
 
 // ---- page plan -----------------------------------------------------------------------------------------
 // Workgroups of a step's page plan in one launch, every one with all prefix sums in its LDS; 0: two launches, sums first.  Several
-// workgroups need inputs that are not written over.
-constexpr int kPlanInOneRequests = 2048, kPlanInOneTokens = 8192, kPlanMostWorkgroups = 128;
+// workgroups need inputs that are not written over.  Measured, us a call in a graph, one launch | two: 64 requests of one token 3.2 | 4.9, 2000 of
+// one 6.2 | 13.8, 2000 of up to 100 (eight in ten of one) 8.8 | 16.6, 8 of up to 2048 4.1 | 6.2; 512 of up to 2048 (35840 rows) 5.8 | 9.5, in 8
+// workgroups for 35 13.1.  Written in place, one workgroup: 8 x 250 rows 3.9 | 5.4, 8 x 500 5.2 | 5.5, 64 x 64 6.0 | 5.9, 512 x 8 7.1 | 7.3,
+// 64 x 125 9.4 | 6.0.
+constexpr int kPlanInOneRequests = 2048, kPlanInOneTokens = 4096, kPlanMostWorkgroups = 128;
 inline int page_plan_workgroups(int batch, int64_t max_tokens, bool in_place) {
   if (batch > kPlanInOneRequests) return 0;
   if (in_place) return max_tokens <= kPlanInOneTokens ? 1 : 0;
@@ -106,7 +109,10 @@ struct PagedForm {
 };
 
 // Up to 32 rows are taken by the form that keeps keys in registers, 16 or 32 at a time; more (bf16) by the one that shares
-// keys among 128 rows through LDS.  float32: always 16.
+// keys among 128 rows through LDS.  float32: always 16.  Measured, us, requests x keys, 32 heads over 8: up to 16 rows taken 16 | 32 at a time: 1 x 2048
+// (4 rows) 12.5 | 14.3, 1 x 98304 79.0 | 81.5, 16 x 4096 (16 rows) 54.4 | 56.4; 17 to 32 rows 16 | 32 at a time | by the form for many: 20 rows 16 x 4096 94.7 | 56.5
+// | 62.9, 32 rows 1 x 65536 78.2 | 75.4 | 73.1, 64 x 1000 96.6 | 56.4 | 63.0; 36 rows 32 at a time | by the form for many: 16 x 4096 97 | 65.2, 64 x 300
+// 48.5 | 23.0, 1 x 65536 85.1 | 75.5, 1 x 2048 19.4 | 21.9; 64 rows 64 x 1000 102 | 65.6.
 constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
 constexpr int kPagedGroupShift = 3, kPagedGroup = 1 << kPagedGroupShift;   // few rows: wavefronts of a workgroup
 constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share of a KV head (at most 3 kNumCU, or a share for each)
@@ -128,7 +134,10 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : 32);
   f.tile_tokens = group <= f.rows ? f.rows / group : 1;
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
-  f.target = many ? 2 * kNumCU : kNumCU;               // workgroups that are resident at once
+  // target: workgroups that are resident at once.  Many rows, us with half as many | these | twice as many, 32 heads over 8: 64 rows over 65536 keys
+  // 90 | 87 | 121, 256 over 8192 34.5 | 34.7 | 35.7, 2048 tokens behind 59392 1893 | 1893 | 1935.  Pieces of at least 256 | 512 | 1024 keys: 256 rows
+  // over 8192 38.4 | 34.7 | 38.3, 30 x 300 tokens 147.5 | 147.4 | 142.
+  f.target = many ? 2 * kNumCU : kNumCU;
   f.min_tiles = 512 / f.key_tile;
   int64_t tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens);
   if (starts && max_tokens / f.tile_tokens + batch < tiles) tiles = max_tokens / f.tile_tokens + batch;

@@ -157,7 +157,7 @@ int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages
   a.tile_tokens = f.tile_tokens; a.head_blocks = f.head_blocks;
   a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * 1.4426950408889634f;
   a.per_piece = 1.0001f / (float)f.target;                  // (the margin keeps float32's rounding from making more pieces)
-  a.min_tiles = f.min_tiles; a.slots = (int)f.slots; a.shares = f.shares;
+  a.target = (float)f.target; a.min_tiles = f.min_tiles; a.slots = (int)f.slots; a.shares = f.shares;
   a.group_shift = f.group_shift; a.group_tiles = 1 << f.group_shift;
   a.k_page = p->k_stride_page; a.k_key = p->k_stride_key; a.k_head = p->k_stride_head;
   a.v_page = p->v_stride_page; a.v_key = p->v_stride_key; a.v_head = p->v_stride_head;

@@ -30,9 +30,9 @@ struct PageAppendArgs {
 // Few rows: the items of a KV head, one behind the other, are cut into `shares` equal shares; a workgroup takes a share, whole
 // items and parts of the first and the last.  A partial of either goes to the workspace (slots 2 w and 2 w + 1 of workgroup w), and the
 // workgroup that finds all others of the item there joins them.
-// Many rows: a long item is cut into pieces, one workgroup each, joined by a second kernel.  Pieces get at most
-// 1/target of the sum; a request that is cut has more than piece_tiles tiles per item, so cut items have at most twice
-// target pieces together.
+// Many rows: a long item is cut into pieces, one workgroup each, joined by a second kernel.  Pieces get 1/target of the sum or
+// somewhat more, so that there are no more than `target` of them where the items allow it; a request that is cut has more than
+// piece_tiles tiles per item, so cut items have at most twice target pieces together.
 struct PagedArgs {
   const void* q; const void* k; const void* v; const float* k_scale; const float* v_scale;
   const int* table; const int* lengths; const int* token_start;
@@ -42,7 +42,8 @@ struct PagedArgs {
   int tile_tokens, head_blocks;
   float scale_log2;       // logits scale * log2(e)
   float per_piece;        // (1 + margin) / target pieces
-  int min_tiles;          // of a piece
+  float target;           // pieces
+  int min_tiles;          // key tiles of one at least
   int slots;              // partials that there is room for
   int shares;             // few rows: shares of a KV head, counted in groups of group_tiles key tiles
   int group_tiles, group_shift;
@@ -68,6 +69,10 @@ __device__ inline PagedRequest paged_request(const PagedArgs& a, int b) {
     r.tokens = 1;
   }
   return r;
+}
+
+__device__ inline int paged_row_tiles(const PagedArgs& a, int tokens) {
+  return (tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
 }
 
 // Key tiles that a row tile of the request has at most (what its items are charged).
@@ -130,27 +135,50 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
   out.g = index % a.Hkv;
   index /= a.Hkv;
   float total = 0.f;
+  int longest = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
     float cost = 0.f;
     if (b < a.batch) {
       const PagedRequest r = paged_request(a, b);
-      const int tiles = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
-      cost = (float)tiles * (float)a.Hkv * (float)paged_charge<KT>(a, r.len);
+      const int charge = paged_charge<KT>(a, r.len);
+      cost = (float)paged_row_tiles(a, r.tokens) * (float)a.Hkv * (float)charge;
+      longest = max(longest, charge);
     }
     total += wave_sum(cost);
   }
   const float want = fminf(ceilf(total * a.per_piece), 1073741824.f);
-  const int piece_tiles = max((int)want, a.min_tiles);
-  if (WHAT == kPieces && a.batch <= 64) {
-    // Items with most keys first, over all requests: what is dealt out last is short.  An item's level is its tiles up to its last token's key
+  int piece_tiles = max((int)want, a.min_tiles);
+  const bool cut = __any(longest > piece_tiles);
+  if (cut && piece_tiles > a.min_tiles) {
+    // The smallest of eight lengths that makes no more than target pieces (counted in float32: about), or the first.  Prompt chunks of 128
+    // tokens behind 20000, three requests of 32 heads over 8 (96 row tiles): 221 us with the first always, 164; of 64, seven requests at 30000 390 | 293.
+    // It costs a workgroup 2 us: two of 512 tokens 345 | 349.
+    float count[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float by = __builtin_amdgcn_rcpf((float)piece_tiles);
+    for (int b = lane; b < a.batch; b += 64) {
+      const PagedRequest r = paged_request(a, b);
+      const float tiles = (float)paged_row_tiles(a, r.tokens) * (float)a.Hkv, charge = (float)paged_charge<KT>(a, r.len) * by;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) count[k] += tiles * ceilf(charge * (8.f / (8 + k)));
+    }
+    int fits = 0;
+#pragma unroll
+    for (int k = 7; k >= 0; --k)
+      if (wave_sum(count[k]) <= a.target) fits = k;
+    piece_tiles += (piece_tiles * (int64_t)fits + 7) / 8;
+  }
+  if (WHAT == kPieces && cut && a.batch <= 64) {
+    // Items with most keys first, over all requests: what is dealt out last is short.  Where items are cut there are few rounds, and the last one
+    // shows: 20 ragged chunks of 100 tokens behind up to 60000 635 us in the requests' order, 599 so; ten of 300 behind 30000 652 | 630.
+    // Where none is, the order by requests keeps what reads the same keys together: 60 prompts of up to 4096 tokens 1347 | 1392, 16 of up to 8192 1327 | 1342.  An item's level is its tiles up to its last token's key
     // (at most what the request is charged); at_least(x): a request's row tiles of level x or more, the last ones.  The level of the
     // item sought is found by halving.
     PagedRequest r{0, 0, 0};
     int tiles = 0, pieces = 1, top = -1;
     if (lane < a.batch) {
       r = paged_request(a, lane);
-      tiles = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
+      tiles = paged_row_tiles(a, r.tokens);
       const int charge = paged_charge<KT>(a, r.len);
       pieces = (charge + piece_tiles - 1) / piece_tiles;
       top = tiles ? min((r.len + KT - 1) / KT, charge) : -1;
@@ -170,7 +198,7 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
       else hi = mid;
     }
     const int many = at_least(lo), more = lo < top ? at_least(lo + 1) : 0, count = pieces * (many - more);
-    const int rank = index - before(lo + 1), upto = wave_prefix(count), cut = pieces > 1 ? tiles * pieces : 0, slots = wave_prefix(cut);
+    const int rank = index - before(lo + 1), upto = wave_prefix(count), partials = pieces > 1 ? tiles * pieces : 0, slots = wave_prefix(partials);
     const int f = __ffsll((unsigned long long)__ballot(upto > rank)) - 1;
     auto at = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
     const int i = rank - at(upto - count), here = at(many - more);
@@ -179,7 +207,7 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
     out.pieces = at(pieces);
     out.piece = i / here;
     out.tile = at(tiles - many) + i % here;
-    out.slot = (at(slots - cut) + out.tile * out.pieces) * a.Hkv + out.g * out.pieces;
+    out.slot = (at(slots - partials) + out.tile * out.pieces) * a.Hkv + out.g * out.pieces;
     return true;
   }
   int base = 0, slot_base = 0;
@@ -189,7 +217,7 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
     int tiles = 0, pieces = 1;
     if (b < a.batch) {
       r = paged_request(a, b);
-      tiles = (r.tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
+      tiles = paged_row_tiles(a, r.tokens);
       pieces = (paged_charge<KT>(a, r.len) + piece_tiles - 1) / piece_tiles;
     }
     const int cut = pieces > 1 ? tiles * pieces : 0;
@@ -237,9 +265,6 @@ struct PagedItem {
 template <int KT>
 __device__ inline int paged_groups(const PagedArgs& a, int len) {
   return (paged_charge<KT>(a, len) + a.group_tiles - 1) >> a.group_shift;
-}
-__device__ inline int paged_row_tiles(const PagedArgs& a, int tokens) {
-  return (tokens + a.tile_tokens - 1) / a.tile_tokens * a.head_blocks;
 }
 
 // The KV heads of a share follow one another on one XCD (workgroups go to the eight XCDs in turn): in pools that store keys token by
