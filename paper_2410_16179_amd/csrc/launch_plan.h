@@ -99,12 +99,15 @@ inline int page_plan_workgroups(int batch, int64_t max_tokens, bool in_place) {
 inline bool page_plan_needs_workspace(int batch, int64_t max_tokens) { return page_plan_workgroups(batch, max_tokens, true) == 0; }
 
 // ---- paged attention ------------------------------------------------------------------------------
+constexpr int kPagedGroupShift = 3, kPagedGroup = 1 << kPagedGroupShift;   // few rows: wavefronts of a workgroup
+// Few rows: near_shift, set_shift: KV heads that a workgroup may take at once (1 << each), for the two reasons that paged_share knows; group_shift: 1 <<
+// that many key tiles are a group, by which work is shared, for one KV head (of sets, as many fewer as heads more); shares: of a set of 1 << index KV heads.
 // rows: query rows (new tokens times the query heads of a KV head) that a workgroup takes at once; key_tile:
 // keys by which the work is counted.  tile_tokens, head_blocks: see PagedArgs.  target: pieces that the work is cut into;
 // min_tiles: key tiles of a piece at least.  items, pieces, units, slots: at most so many row
 // tiles of all KV heads, workgroups, row tiles that are cut, partials.
 struct PagedForm {
-  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles, shares, group_shift;
+  int rows, key_tile, tile_tokens, head_blocks, target, min_tiles, near_shift, set_shift, group_shift, shares[kPagedGroupShift + 1];
   int64_t items, pieces, units, slots;
 };
 
@@ -114,8 +117,8 @@ struct PagedForm {
 // | 62.9, 32 rows 1 x 65536 78.2 | 75.4 | 73.1, 64 x 1000 96.6 | 56.4 | 63.0; 36 rows 32 at a time | by the form for many: 16 x 4096 97 | 65.2, 64 x 300
 // 48.5 | 23.0, 1 x 65536 85.1 | 75.5, 1 x 2048 19.4 | 21.9; 64 rows 64 x 1000 102 | 65.6.
 constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
-constexpr int kPagedGroupShift = 3, kPagedGroup = 1 << kPagedGroupShift;   // few rows: wavefronts of a workgroup
-constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share of a KV head (at most 3 kNumCU, or a share for each)
+constexpr int kPagedNearParts = 16, kPagedNearTiles = 128;   // few rows: see paged_share
+constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share (at most kNumCU, or one for each KV head)
 inline int paged_rows(bool fp32, int64_t rows) { return fp32 || rows <= 16 ? 16 : (rows <= 32 ? 32 : kPagedManyRows); }
 
 // Row tiles of all KV heads and requests, whatever token counts (each at most max_new) the device memory holds.
@@ -125,9 +128,10 @@ inline int64_t paged_most_items(int batch, int kv_heads, int group, bool fp32, i
   return (int64_t)batch * ((max_new + tokens - 1) / tokens) * blocks * kv_heads;
 }
 
-// group: query heads per KV head.  starts: the requests' token counts differ (else one token each).
+// group: query heads per KV head.  starts: the requests' token counts differ (else one token each).  row_bytes: of a key's row, where the rows of a key's
+// heads lie one behind the other in both pools; else 0.
 inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64_t max_tokens, int max_new, bool starts, int64_t max_len,
-                            int n_sink, int n_local) {
+                            int n_sink, int n_local, int row_bytes) {
   PagedForm f{};
   f.rows = paged_rows(fp32, (int64_t)max_new * group);
   const bool many = f.rows == kPagedManyRows;
@@ -156,17 +160,28 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
     f.units = f.items < f.target ? f.items : f.target;
   }
   if (!many) {
-    // (a group has at least a key tile for each wavefront; the groups of all row tiles are counted in 31 bits)
+    // near_shift: sets of neighbouring rows, 512 bytes at most, of no more query rows than are joined at once; set_shift: sets that the kernel may
+    // choose, whatever the lengths
+    const int tokens = max_new < f.tile_tokens ? max_new : f.tile_tokens, used = group < f.rows ? group * tokens : f.rows;
+    while (row_bytes > 0 && row_bytes << f.near_shift < 512 && used << (f.near_shift + 1) <= 32) ++f.near_shift;
+    while (f.set_shift < kPagedGroupShift && kv_heads % (2 << f.set_shift) == 0 &&
+           f.target * (2 << f.set_shift) <= f.items * (f.set_shift < f.near_shift && f.items * charge >= kPagedNearTiles * f.target ? kPagedNearParts : 1))
+      ++f.set_shift;
+    // (a group has a key tile for each wavefront of a head; the groups of all row tiles are counted in 31 bits, in sets too)
     auto groups = [&](int shift) { return (charge + (1 << shift) - 1) >> shift; };
     f.group_shift = kPagedGroupShift;
     const int64_t row_tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens) * f.head_blocks;
-    while (row_tiles * groups(f.group_shift) > INT32_MAX - kPagedCounters) ++f.group_shift;
-    const int64_t least = groups(f.group_shift) * (f.items / kv_heads);
-    const int64_t shares = f.target / kv_heads > 1 ? f.target / kv_heads : 1;
-    f.shares = (int)(shares < least ? shares : (least > 1 ? least : 1));
-    f.pieces = (int64_t)(f.shares + 7) / 8 * 8 * kv_heads;   // (dealt to the eight XCDs in rounds of eight)
-    f.units = 0;
-    f.slots = 2 * (int64_t)f.shares * kv_heads;
+    while (row_tiles * groups(f.group_shift - f.set_shift) > INT32_MAX - kPagedCounters) ++f.group_shift;
+    f.pieces = f.slots = f.units = 0;
+    for (int shift = 0; shift <= f.set_shift; ++shift) {
+      const int sets = kv_heads >> shift;
+      const int64_t least = groups(f.group_shift - shift) * (f.items / kv_heads), most = f.target > sets ? f.target / sets : 1;
+      const int64_t shares = most < least ? most : (least > 1 ? least : 1);
+      const int64_t pieces = (shares + 7) / 8 * 8 * sets, slots = 2 * shares * kv_heads;   // (dealt to the eight XCDs in rounds of eight)
+      f.shares[shift] = (int)shares;
+      f.pieces = pieces > f.pieces ? pieces : f.pieces;
+      f.slots = slots > f.slots ? slots : f.slots;
+    }
   }
   return f;
 }

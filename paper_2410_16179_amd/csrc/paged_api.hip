@@ -57,7 +57,8 @@ int check_rows(int64_t token, int64_t head) {
 
 mp::PagedForm form_of(const Params* p, bool starts) {
   return mp::paged_form(p->batch, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->dtype == MAGICPIG_FP32, p->max_tokens, starts ? most_new(p) : 1,
-                        starts, (int64_t)p->max_pages * p->page_size, p->n_sink, p->n_local);
+                        starts, (int64_t)p->max_pages * p->page_size, p->n_sink, p->n_local,
+                        p->k_stride_head == mp::kHeadDim && p->v_stride_head == mp::kHeadDim ? mp::kHeadDim * element_bytes(p) : 0);
 }
 // The workspace: counters of arrived partials (zero between calls), then what a call keeps for itself.
 constexpr size_t kCounterBytes = MAGICPIG_PAGED_COUNTER_BYTES;
@@ -157,8 +158,9 @@ int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages
   a.tile_tokens = f.tile_tokens; a.head_blocks = f.head_blocks;
   a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * 1.4426950408889634f;
   a.per_piece = 1.0001f / (float)f.target;                  // (the margin keeps float32's rounding from making more pieces)
-  a.target = (float)f.target; a.min_tiles = f.min_tiles; a.slots = (int)f.slots; a.shares = f.shares;
-  a.group_shift = f.group_shift; a.group_tiles = 1 << f.group_shift;
+  a.target = f.target; a.min_tiles = f.min_tiles; a.slots = (int)f.slots;
+  a.near_shift = f.near_shift; a.set_shift = f.set_shift; a.group_shift = f.group_shift;
+  for (int i = 0; i <= f.set_shift; ++i) a.shares[i] = f.shares[i];
   a.k_page = p->k_stride_page; a.k_key = p->k_stride_key; a.k_head = p->k_stride_head;
   a.v_page = p->v_stride_page; a.v_key = p->v_stride_key; a.v_head = p->v_stride_head;
   a.q_t = p->q_stride_token; a.q_h = p->q_stride_head;

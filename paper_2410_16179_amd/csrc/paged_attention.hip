@@ -8,17 +8,18 @@ namespace {
 
 constexpr int kFewThreads = 64 * kPagedGroup;
 
-// Joins the partials of a cut item, by one workgroup: groups of sixteen threads take a row each, eight elements a thread, and where
-// there are few rows several groups share a row's partials; eight partials are requested at once.  lds: room for as many rows as there are groups.
-template <bool F32, int R, class OutRow>
-__device__ inline void join_parts(const PagedArgs& a, float* lds, int first_share, int parts, int g, int rows, float v_scale, OutRow out_row) {
-  constexpr int kAtOnce = 8;
+// Joins the partials of a cut item, by one workgroup: groups of sixteen threads take a row of a KV head each, eight elements a thread, and
+// where there are few rows several groups share a row's partials; eight partials are requested at once.  rows: of a head; all: of the set.  lds: room
+// for as many rows as there are groups.
+template <bool F32, int R, bool SETS, class Scale, class Finish>
+__device__ inline void join_parts(const PagedArgs& a, float* lds, int first_share, int parts, int g0, int rows, int all, Scale scale_of, Finish finish) {
+  constexpr int kAtOnce = 8, kLots = kFewThreads / 16;
   const int lot = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * 8;
-  constexpr int kLots = kFewThreads / 16;
-  const int per_row = rows < kLots ? kLots / rows : 1;
-  {
-    const int part = lot / rows, row = lot - part * rows;
-    const bool busy = part < per_row && row < rows;
+  const int per_row = all < kLots ? kLots / all : 1;
+  for (int base = 0; base == 0 || (SETS && base < all); base += kLots) {
+    const int part = lot / all, n = base + lot - part * all, head = SETS && rows < all ? n / rows : 0, row = n - head * rows;   // (part 0 where a group has a row of its own)
+    const bool busy = part < per_row && n < all;
+    const float v_scale = busy ? scale_of(head) : 1.f;
     float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
     if (busy) {
       for (int p = part; p < parts; p += kAtOnce * per_row) {
@@ -28,7 +29,7 @@ __device__ inline void join_parts(const PagedArgs& a, float* lds, int first_shar
           const int q = p + i * per_row;
           ml[i] = f32x2{-INFINITY, 0.f};
           if (q < parts) {
-            const float* from = a.partial + ((2 * ((int64_t)(first_share + q) * a.Hkv + g) + (q == 0 ? 1 : 0)) * R + row) * kPartialRow;
+            const float* from = a.partial + ((2 * ((int64_t)(first_share + q) * a.Hkv + g0 + head) + (q == 0 ? 1 : 0)) * R + row) * kPartialRow;
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[i][e] = load_through(from + e0 + 2 * e);
             ml[i] = load_through(from + 128);
@@ -64,7 +65,7 @@ __device__ inline void join_parts(const PagedArgs& a, float* lds, int first_shar
       __syncthreads();
       if (busy && part == 0) {
         for (int i = 1; i < per_row; ++i) {
-          const float* from = lds + (lot + i * rows) * kPartialRow;
+          const float* from = lds + (lot + i * all) * kPartialRow;
           const float m1 = from[128], top = fmaxf(m, m1);
           if (m1 == -INFINITY) continue;
           const float b0 = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), b1 = m1 == top ? 1.f : __builtin_amdgcn_exp2f(m1 - top);
@@ -75,43 +76,47 @@ __device__ inline void join_parts(const PagedArgs& a, float* lds, int first_shar
         }
       }
     }
-    if (busy && part == 0) paged_write_row<F32>(a, out_row(row), e0, o, m, l, v_scale);
+    if (busy && part == 0) finish(head, row, e0, o, m, l, v_scale);
   }
 }
 
 // Behind the wavefronts' parts in `joined`: the rows of the item they belong to are written, or, where other workgroups have keys of it
 // too, a partial; the last of these workgroups joins the partials.
-template <bool F32, int NR>
+template <bool F32, int NR, bool SETS>
 __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, const PagedItem& item,
                                    float (&joined)[kPagedGroup][16 * NR][kPartialRow], int& last_one) {
   constexpr int R = 16 * NR;
   const int tt = item.tile / a.head_blocks, hb = item.tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, item.r.tokens) - 1;
   const int rows = a.head_blocks > 1 ? min(a.G - hb * R, R) : (last - first + 1) * a.G;
-  auto out_row = [&](int row) {
-    const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G;
-    return (int64_t)(item.r.row + first + t) * a.Hq + item.g * a.G + h;
+  const int all = rows << item.shift, g0 = item.set << item.shift, waves = kPagedGroup >> item.shift;   // rows of the set; wavefronts of a KV head
+  auto scale_of = [&](int head) { return a.v_scale ? a.v_scale[g0 + head] : 1.f; };
+  auto finish = [&](int head, int row, int e0, const float (&o)[8], float m, float l, float v_scale) {
+    const int t = a.head_blocks > 1 ? 0 : row / a.G, h = a.head_blocks > 1 ? hb * R + row : row - t * a.G, g = g0 + head;
+    paged_write_row<F32>(a, (int64_t)(item.r.row + first + t) * a.Hq + g * a.G + h, e0, o, m, l, v_scale);
   };
   const bool whole = item.from == 0 && item.to == item.groups;
-  const int slot = 2 * (share.j * a.Hkv + item.g) + (item.from == 0 ? 1 : 0);
-  const float v_scale = a.v_scale ? a.v_scale[item.g] : 1.f;
   const int e0 = (threadIdx.x & 15) * 8;
-  for (int row = threadIdx.x >> 4; row < rows; row += kFewThreads / 16) {
-    float m = -INFINITY;
+  for (int n = threadIdx.x >> 4; n < all; n += kFewThreads / 16) {
+    const int head = SETS && item.shift ? n / rows : 0, row = n - head * rows;
+    const float v_scale = scale_of(head);
+    const float(*const part)[16 * NR][kPartialRow] = joined + head * waves;
+    float m = -INFINITY;                                   // (fewer than eight wavefronts: some are looked at again, without weight)
 #pragma unroll
-    for (int w = 0; w < kPagedGroup; ++w) m = fmaxf(m, joined[w][row][128]);
+    for (int w = 0; w < kPagedGroup; ++w) m = fmaxf(m, part[w & (waves - 1)][row][128]);
     float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll
     for (int w = 0; w < kPagedGroup; ++w) {
-      const float mw = joined[w][row][128];
-      const float by = mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
-      l += by * joined[w][row][129];
+      const float mw = part[w & (waves - 1)][row][128];
+      const float by = w >= waves || mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
+      l += by * part[w & (waves - 1)][row][129];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += by * joined[w][row][e0 + e];
+      for (int e = 0; e < 8; ++e) o[e] += by * part[w & (waves - 1)][row][e0 + e];
     }
     if (whole) {
-      paged_write_row<F32>(a, out_row(row), e0, o, m, l, v_scale);
+      finish(head, row, e0, o, m, l, v_scale);
     } else {
+      const int slot = 2 * (share.j * a.Hkv + g0 + head) + (item.from == 0 ? 1 : 0);
       float* pp = a.partial + ((int64_t)slot * R + row) * kPartialRow;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) store_through(pp + e0 + e, o[e], o[e + 1]);
@@ -121,7 +126,7 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
   if (whole) return;
   const int first_share = item.from == 0 ? share.j : item.begin / share.each;
   const int parts = (item.begin + item.groups - 1) / share.each - first_share + 1;
-  unsigned* const arrived = a.arrived + (int64_t)first_share * a.Hkv + item.g;
+  unsigned* const arrived = a.arrived + first_share * (a.Hkv >> item.shift) + item.set;
   stored();
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -131,7 +136,7 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
   }
   __syncthreads();
   if (!last_one) return;
-  join_parts<F32, R>(a, &joined[0][0][0], first_share, parts, item.g, rows, v_scale, out_row);
+  join_parts<F32, R, SETS>(a, &joined[0][0][0], first_share, parts, g0, rows, all, scale_of, finish);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------
@@ -164,7 +169,7 @@ struct FewRows {
   Raw vf[kFrags];
 };
 
-template <int ET, int NR>
+template <int ET, int NR, bool SETS>
 __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const PagedArgs a) {
   using F = FewRows<ET, NR>;
   constexpr bool kF32 = F::kF32;
@@ -177,7 +182,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   __shared__ PagedShare at_share;
   {
     PagedShare share;
-    if (!paged_share<KT>(a, blockIdx.x, share)) return;
+    if (!paged_share<KT, SETS>(a, blockIdx.x, share)) return;
     if (threadIdx.x == 0) at_share = share;
   }
   __syncthreads();
@@ -188,16 +193,18 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));
   const int lane = tid & 63, c = lane & 15, u = lane >> 4;
-  const PagedItem item = paged_item<KT>(a, at_share);
+  const PagedItem item = paged_item<KT, SETS>(a, at_share);
   const PagedRequest req = item.r;
-  const int tile = item.tile, g = item.g;
+  // the wavefront's KV head, and its place among the wavefronts that share the head's tiles
+  const int waves = kPagedGroup >> item.shift, place = wave & (waves - 1);
+  const int tile = item.tile, g = (item.set << item.shift) + (wave >> (kPagedGroupShift - item.shift));
   const int len = req.len, tokens = req.tokens;
   const int tt = tile / a.head_blocks, hb = tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, tokens) - 1;
   const int heads = min(a.G - hb * R, R);                // query heads of the tile: all G where a tile holds whole tokens
   const int rows = a.head_blocks > 1 ? heads : (last - first + 1) * a.G;
   const PagedSpan span = paged_span<KT>(a, len, tokens, first, last);
-  const int t_begin = item.from << a.group_shift, t_end = min(item.to << a.group_shift, span.count);
+  const int t_begin = item.from << item.group_shift, t_end = min(item.to << item.group_shift, span.count);
   // row of this lane's column: token and head
   int hi[NR], lo[NR];                                    // keys it attends: [lo, hi], and those below n_sink
   F f{};                                                 // (all of it: what an earlier item left would stay in registers)
@@ -403,7 +410,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   bool bad_page = false;
   // the first such tile from v on with pages that are there; they are read
   auto find = [&](int v, TilePages<KT>& p) {
-    for (; v < t_end; v += kPagedGroup) {
+    for (; v < t_end; v += waves) {
       if (!in_full(v)) continue;
       tile_pages(v, p);
       if (pages_ok(p)) break;
@@ -443,18 +450,18 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   // The tiles, whole ones and then the others (the last ones, the borders of the window and of the sink): the next one's K is requested
   // when the scores have taken this one's, its V behind the products with this one's.
   auto other = [&](int v) {                               // the first of the others from v on
-    while (v < t_end && in_full(v)) v += kPagedGroup;
+    while (v < t_end && in_full(v)) v += waves;
     return v;
   };
-  int w = t_begin + wave;
+  int w = t_begin + place;
   if (a.n_local == 0) {                                   // (only from the first key on that some row does not attend)
     const int from = (min_hi + 1 > 0 ? min_hi + 1 : 0) / KT;
-    if (from > w) w += (from - w + kPagedGroup - 1) / kPagedGroup * kPagedGroup;
+    if (from > w) w += (from - w + waves - 1) & ~(waves - 1);
   }
   w = other(w);
   TilePages<KT> w_pages{};
   if (w < t_end) tile_pages(w, w_pages);
-  int v = find(t_begin + wave, now), v1 = t_end;
+  int v = find(t_begin + place, now), v1 = t_end;
   int valid[F::kHalves];
   {
     const int first_tile = v < t_end ? v : w;
@@ -466,10 +473,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       request_v(key0, p, valid);
     }
   }
-  if (v < t_end) v1 = find(v + kPagedGroup, next);
+  if (v < t_end) v1 = find(v + waves, next);
 #pragma unroll 1
   while (v < t_end) {
-    const int v2 = v1 + kPagedGroup, ahead = v1 < t_end ? v1 : w;
+    const int v2 = v1 + waves, ahead = v1 < t_end ? v1 : w;
     if (v2 < t_end) tile_pages(v2, after);
     const int key1 = tile_key(ahead);
     const TilePages<KT> p = v1 < t_end ? next : w_pages;
@@ -489,12 +496,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     next = after;
     if (v1 < t_end && !(in_full(v1) && pages_ok(next))) {
       bad_page = bad_page || in_full(v1);
-      v1 = find(v1 + kPagedGroup, next);
+      v1 = find(v1 + waves, next);
     }
   }
 #pragma unroll 1
   while (w < t_end) {
-    const int key0 = tile_key(w), w1 = other(w + kPagedGroup);
+    const int key0 = tile_key(w), w1 = other(w + waves);
     TilePages<KT> p{};
     if (w1 < t_end) tile_pages(w1, p);
     float s[NR][kScores];
@@ -524,7 +531,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   if (bad_page || __any(sum != sum)) {
     reset();
 #pragma unroll 1
-    for (int v = t_begin + wave; v < t_end; v += kPagedGroup) {
+    for (int v = t_begin + place; v < t_end; v += waves) {
       const int key0 = tile_key(v);
       tile_pages(v, now);
       valid_rows(key0, now, valid);
@@ -603,10 +610,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     }
     if (u == 0) { to[128] = f.m[n]; to[129] = l; }
   }
-  const PagedItem done = paged_item<KT>(a, at_share);      // (read before the barrier: behind it the first thread goes on to the next item)
+  const PagedItem done = paged_item<KT, SETS>(a, at_share);      // (read before the barrier: behind it the first thread goes on to the next item)
   __syncthreads();
-  finish_item<kF32, NR>(a, at_share, done, joined, last_one);
-  if (threadIdx.x == 0) paged_next<KT>(a, at_share);
+  finish_item<kF32, NR, SETS>(a, at_share, done, joined, last_one);
+  if (threadIdx.x == 0) paged_next<KT, SETS>(a, at_share);
   __syncthreads();
   if (at_share.pos >= at_share.end) return;
   }
@@ -665,7 +672,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const PagedArg
 
 template <int ET, int NR>
 hipError_t launch_few_rows(const PagedArgs& a, const PagedForm& form, hipStream_t s) {
-  paged_few_rows_kernel<ET, NR><<<(unsigned)form.pieces, kFewThreads, 0, s>>>(a);
+  if (form.set_shift > 0) paged_few_rows_kernel<ET, NR, true><<<(unsigned)form.pieces, kFewThreads, 0, s>>>(a);
+  else paged_few_rows_kernel<ET, NR, false><<<(unsigned)form.pieces, kFewThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

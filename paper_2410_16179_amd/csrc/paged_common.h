@@ -27,8 +27,9 @@ struct PageAppendArgs {
 // head_blocks tiles per token).  An item is a row tile of one request and KV head; its keys are counted
 // in tiles.  Lengths are known on the device alone, so every workgroup works out by itself what it takes; a request is
 // charged its keys as if all its row tiles reached the last one.
-// Few rows: the items of a KV head, one behind the other, are cut into `shares` equal shares; a workgroup takes a share, whole
-// items and parts of the first and the last.  A partial of either goes to the workspace (slots 2 w and 2 w + 1 of workgroup w), and the
+// Few rows: the items of a KV head, one behind the other, are cut into equal shares; a workgroup takes a share, whole
+// items and parts of the first and the last, of a set of one, two, four or eight KV heads at once, by different ones of its eight
+// wavefronts.  A partial of either goes to the workspace (slots 2 i and 2 i + 1 of share and KV head i), and the
 // workgroup that finds all others of the item there joins them.
 // Many rows: a long item is cut into pieces, one workgroup each, joined by a second kernel.  Pieces get 1/target of the sum or
 // somewhat more, so that there are no more than `target` of them where the items allow it; a request that is cut has more than
@@ -42,11 +43,10 @@ struct PagedArgs {
   int tile_tokens, head_blocks;
   float scale_log2;       // logits scale * log2(e)
   float per_piece;        // (1 + margin) / target pieces
-  float target;           // pieces
+  int target;             // pieces, or shares of all sets
   int min_tiles;          // key tiles of one at least
   int slots;              // partials that there is room for
-  int shares;             // few rows: shares of a KV head, counted in groups of group_tiles key tiles
-  int group_tiles, group_shift;
+  int near_shift, set_shift, group_shift, shares[kPagedGroupShift + 1];   // few rows: see PagedForm
   unsigned* arrived;      // few rows: partials of the cut item that begins in a share which are there (0 between calls)
   int64_t k_page, k_key, k_head, v_page, v_key, v_head, q_t, q_h;
 };
@@ -165,7 +165,7 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
     int fits = 0;
 #pragma unroll
     for (int k = 7; k >= 0; --k)
-      if (wave_sum(count[k]) <= a.target) fits = k;
+      if (wave_sum(count[k]) <= (float)a.target) fits = k;
     piece_tiles += (piece_tiles * (int64_t)fits + 7) / 8;
   }
   if (WHAT == kPieces && cut && a.batch <= 64) {
@@ -249,57 +249,84 @@ __device__ inline void paged_piece_range(int count, int piece, int pieces, int& 
   end = begin + each + (piece < more ? 1 : 0);
 }
 
-// Few rows: a workgroup's share of a KV head's items, in groups of key tiles: [begin, end) of all, which starts inside request b,
-// whose items begin at `base`; pos: where the workgroup is.
+// Few rows: a workgroup's share of the items of a set of 1 << shift KV heads, in groups of key tiles: [begin, end) of all, which starts
+// inside request b, whose items begin at `base`; pos: where the workgroup is.
 struct PagedShare {
-  int g, j, b, base, pos, begin, end, each;
+  int set, shift, j, b, base, pos, begin, end, each;
   PagedRequest r;
 };
 // The item that `pos` lies in: its first group, and the groups [from, to) of its `groups` that the share has.
 struct PagedItem {
-  int g, b, tile, begin, from, to, groups;
+  int set, shift, group_shift, b, tile, begin, from, to, groups;
   PagedRequest r;
 };
 
-// (the host chooses group_tiles so that the groups of all row tiles stay below 2^31)
+// (the host chooses group_shift so that the groups of all row tiles stay below 2^31)
 template <int KT>
-__device__ inline int paged_groups(const PagedArgs& a, int len) {
-  return (paged_charge<KT>(a, len) + a.group_tiles - 1) >> a.group_shift;
+__device__ inline int paged_groups(const PagedArgs& a, int len, int group_shift) {
+  return (paged_charge<KT>(a, len) + (1 << group_shift) - 1) >> group_shift;
 }
 
-// The KV heads of a share follow one another on one XCD (workgroups go to the eight XCDs in turn): in pools that store keys token by
-// token their rows are neighbours.
-template <int KT>
+// How many KV heads a workgroup takes at once, by different wavefronts, follows from the parts that the longest item is cut into: a set's parts are
+// joined by one workgroup.  Measured, us, a head at a time | in sets, 4 query heads a KV head if not said otherwise:
+//   Where a token's rows of several heads lie one behind the other, wavefronts that read them at about the same time read longer runs of memory
+//   (e4m3 rows of 128 bytes, eight heads, plain reads: 5.5 TB/s by one head, 6.3 by two, 6.7 by four, whether a wavefront takes all of them or each its
+//   own).  So up to 512 bytes, at up to 16 parts, if there are 16 key tiles or more for each wavefront: e4m3, 8 KV heads, 48 requests of up to 30011
+//   keys and 8 query heads 111 | 103, 16 x 8192 60.5 | 55.7; 32 KV heads, 4 x 20000 136 | 117, 64 x 2000 220 | 168; bf16, 64 x 4000 179 | 170.  At 32
+//   parts and more the join costs more: 1 x 65536 38 | 42 in twos, 68 in fours; at four tiles a wavefront it does too: 32 KV heads, 1 x 8192 22.5 | 24.3.
+//   Query rows of a set beyond the 32 that are joined at once: 16 x 4096, 32 rows 39.9 | 69.
+//   Where items are short, at most a share, sets of any heads save the way from item to item: 8 KV heads, 256 x 300 e4m3 62 | 36, bf16 77 | 58, stored
+//   head by head 59 | 35, 1000 x 50 171 | 52, 32 rows 256 x 300 84 | 51.
+// The sets of a share follow one another on one XCD (workgroups go to the eight XCDs in turn).
+// SETS: whether it may be more than one (the way there costs a small call 0.5 us, of 12).
+template <int KT, bool SETS>
 __device__ inline bool paged_share(const PagedArgs& a, int index, PagedShare& out) {
-  const int lane = threadIdx.x & 63, i = index >> 3;
-  out.g = i % a.Hkv;
-  out.j = i / a.Hkv * 8 + (index & 7);
-  if (out.j >= a.shares) return false;
+  const int lane = threadIdx.x & 63;
+  PagedRequest r0{0, 0, 0};                                 // (the first 64 requests are read once)
+  if (lane < a.batch) r0 = paged_request(a, lane);
+  int shift = 0, shares = a.shares[0];
+  if constexpr (SETS) {
+    float sum = 0.f, longest = 0.f;
+    for (int b = lane; b < a.batch; b += 64) {
+      const PagedRequest r = b < 64 ? r0 : paged_request(a, b);
+      const float charge = r.tokens > 0 ? (float)paged_charge<KT>(a, r.len) : 0.f;
+      sum += charge * (float)paged_row_tiles(a, r.tokens);
+      longest = fmaxf(longest, charge);
+    }
+    sum = wave_sum(sum) * (float)a.Hkv;
+    longest = wave_max(longest) * (float)a.target;
+    const float near = sum * (sum >= (float)(kPagedNearTiles * a.target) ? (float)kPagedNearParts : 1.f);
+    while (shift < a.set_shift && longest * (float)(2 << shift) <= (shift < a.near_shift ? near : sum)) ++shift;
+    shift = __builtin_amdgcn_readfirstlane(shift);
+#pragma unroll
+    for (int x = 1; x <= kPagedGroupShift; ++x) shares = shift == x ? a.shares[x] : shares;
+  }
+  out.shift = shift;
+  const int group_shift = a.group_shift - shift;
+  const int sets = a.Hkv >> shift, i = index >> 3;
+  out.set = i % sets;
+  out.j = i / sets * 8 + (index & 7);
+  if (out.j >= shares) return false;
+  auto groups_of = [&](const PagedRequest& r) { return paged_row_tiles(a, r.tokens) * paged_groups<KT>(a, r.len, group_shift); };
   int total = 0;
   for (int b0 = 64; b0 < a.batch; b0 += 64) {             // (the first 64 requests are counted below, once)
     const int b = b0 + lane;
-    int v = 0;
-    if (b < a.batch) {
-      const PagedRequest r = paged_request(a, b);
-      v = paged_row_tiles(a, r.tokens) * paged_groups<KT>(a, r.len);
-    }
-    total += __builtin_amdgcn_readlane(wave_prefix(v), 63);
+    total += __builtin_amdgcn_readlane(wave_prefix(b < a.batch ? groups_of(paged_request(a, b)) : 0), 63);
   }
   int base = 0;
   out.each = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
-    PagedRequest r{0, 0, 0};
-    int v = 0;
-    if (b < a.batch) {
-      r = paged_request(a, b);
-      v = paged_row_tiles(a, r.tokens) * paged_groups<KT>(a, r.len);
+    PagedRequest r = r0;
+    if (b0 > 0) {
+      r = PagedRequest{0, 0, 0};
+      if (b < a.batch) r = paged_request(a, b);
     }
-    const int upto = wave_prefix(v), sum = __builtin_amdgcn_readlane(upto, 63);
+    const int v = groups_of(r), upto = wave_prefix(v), all = __builtin_amdgcn_readlane(upto, 63);
     if (b0 == 0) {
-      total += sum;
+      total += all;
       if (total == 0) return false;
-      out.each = (int)(((uint32_t)total + (uint32_t)a.shares - 1u) / (uint32_t)a.shares);
+      out.each = (int)(((uint32_t)total + (uint32_t)shares - 1u) / (uint32_t)shares);
       const int64_t begin = (int64_t)out.each * out.j;
       if (begin >= total) return false;
       out.begin = out.pos = (int)begin;
@@ -315,21 +342,23 @@ __device__ inline bool paged_share(const PagedArgs& a, int index, PagedShare& ou
       out.base = base + __builtin_amdgcn_readlane(upto - v, f);
       return true;
     }
-    base += sum;
+    base += all;
   }
   return false;
 }
 
 // (the share lies in LDS: the same for all lanes)
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-template <int KT>
+template <int KT, bool SETS>
 __device__ inline PagedItem paged_item(const PagedArgs& a, const PagedShare& s) {
   PagedItem i;
-  i.g = uniform(s.g);
+  i.set = uniform(s.set);
+  i.shift = SETS ? uniform(s.shift) : 0;
+  i.group_shift = a.group_shift - i.shift;
   i.b = uniform(s.b);
   i.r.len = uniform(s.r.len); i.r.tokens = uniform(s.r.tokens); i.r.row = uniform(s.r.row);
   const int tiles = paged_row_tiles(a, i.r.tokens), pos = uniform(s.pos), base = uniform(s.base), end = uniform(s.end);
-  i.groups = paged_groups<KT>(a, i.r.len);
+  i.groups = paged_groups<KT>(a, i.r.len, i.group_shift);
   const int k = tiles > 1 ? (pos - base) / i.groups : 0;
   i.begin = base + k * i.groups;
   i.from = pos - i.begin;
@@ -338,9 +367,9 @@ __device__ inline PagedItem paged_item(const PagedArgs& a, const PagedShare& s) 
   return i;
 }
 // Behind the item, by one thread: the next request that has rows, if the share goes on there.
-template <int KT>
+template <int KT, bool SETS>
 __device__ inline void paged_next(const PagedArgs& a, PagedShare& s) {
-  const int tiles = paged_row_tiles(a, s.r.tokens), groups = paged_groups<KT>(a, s.r.len);
+  const int tiles = paged_row_tiles(a, s.r.tokens), groups = paged_groups<KT>(a, s.r.len, a.group_shift - (SETS ? s.shift : 0));
   const int next = s.base + tiles * groups, k = tiles > 1 ? (s.pos - s.base) / groups : 0;
   s.pos = min(s.base + (k + 1) * groups, s.end);
   if (s.pos < s.end && s.pos == next) {

@@ -237,6 +237,29 @@ def test_a_query_that_is_nan_over_long_keys(kind, new):
     assert (np.abs(out - want)[~nan] <= tol[~nan]).all()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("layout", ["token", "head"])
+@pytest.mark.parametrize("heads,kv_heads,batch,longest", [(32, 32, 70, 60), (16, 8, 300, 40), (24, 12, 200, 90), (64, 32, 140, 600)])
+def test_many_short_requests(kind, layout, heads, kv_heads, batch, longest):
+    # workgroups take two, four or eight KV heads at once
+    lengths = np.random.default_rng(batch).integers(0, longest, batch).tolist()
+    new = None if heads > 24 else [1 + i % 4 for i in range(batch)]
+    Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=16, lengths=lengths, new=new, layout=layout, seed=batch).check()
+
+
+@pytest.mark.parametrize("kind,heads,kv_heads,new,shortest", [("fp8", 32, 8, 1, 7000), ("bf16", 16, 8, 1, 7000), ("fp32", 8, 8, 1, 7000), ("fp8", 32, 8, 4, 6000),
+                                                              ("fp8", 48, 12, 1, 1)])
+def test_long_requests_over_neighbouring_heads(kind, heads, kv_heads, new, shortest):
+    # items that are cut, in sets of KV heads whose rows are neighbours; all requests share the longest one's pages
+    batch, longest = (20, 8000) if shortest > 1 else (90, 9000)
+    lengths = [longest] + np.random.default_rng(26).integers(shortest, longest, batch - 1).tolist()
+    p = Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=64, lengths=[longest] + [0] * (batch - 1), new=[new] * batch, seed=26)
+    p.lengths = lengths
+    p.table[1:] = p.table[0]
+    p.upload()
+    p.check()
+
+
 @pytest.mark.parametrize("new", [None, [3, 2, 1], [40, 9, 64]])
 def test_scales_of_zero_and_below(new):
     p = Problem(kind="fp8", heads=6, kv_heads=3, page=16, lengths=[90, 12, 64], new=new, seed=22, spare_rows=1 if new else 0)

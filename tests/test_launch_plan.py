@@ -15,11 +15,11 @@ void gather(int units, int G, long nblk, long n_static, int tau, int* got) {
   got[0] = p.run_blocks; got[1] = p.runs; got[2] = p.static_runs; got[3] = p.static_keys; got[4] = p.full;
 }
 long head_limit(int tuned, int G) { return mp::head_per_workgroup_limit(tuned, G); }
-void paged(int batch, int kv, int group, int fp32, long max_tokens, int max_new, int starts, long max_len, int n_sink, int n_local, long* got) {
-  const mp::PagedForm f = mp::paged_form(batch, kv, group, fp32, max_tokens, max_new, starts, max_len, n_sink, n_local);
-  const long all[] = {f.rows, f.key_tile, f.tile_tokens, f.head_blocks, f.target, f.min_tiles, f.shares, f.group_shift, f.items, f.pieces,
+void paged(int batch, int kv, int group, int fp32, long max_tokens, int max_new, int starts, long max_len, int n_sink, int n_local, int row_bytes, long* got) {
+  const mp::PagedForm f = mp::paged_form(batch, kv, group, fp32, max_tokens, max_new, starts, max_len, n_sink, n_local, row_bytes);
+  const long all[] = {f.rows, f.key_tile, f.tile_tokens, f.head_blocks, f.target, f.min_tiles, f.near_shift, f.set_shift, f.group_shift, f.shares[0], f.shares[1], f.shares[2], f.shares[3], f.items, f.pieces,
                       f.units, f.slots};
-  for (int i = 0; i < 12; ++i) got[i] = all[i];
+  for (int i = 0; i < 17; ++i) got[i] = all[i];
 }
 int plan_workgroups(int batch, long max_tokens, int in_place) { return mp::page_plan_workgroups(batch, max_tokens, in_place); }
 int hash_f32(int K, long groups32, long groups64) { return mp::hash_f32_keys(K, groups32, groups64); }
@@ -99,13 +99,13 @@ def test_head_per_workgroup(plan, units, G, n, tuned, one):
     assert (units * (-(-n // 256)) * G <= plan.head_limit(int(tuned), G)) == one
 
 
-_PAGED = ("rows", "key_tile", "tile_tokens", "head_blocks", "target", "min_tiles", "shares", "group_shift", "items", "pieces", "units", "slots")
+_PAGED = ("rows", "key_tile", "tile_tokens", "head_blocks", "target", "min_tiles", "near_shift", "set_shift", "group_shift", "shares0", "shares1", "shares2", "shares3", "items", "pieces", "units", "slots")
 
 
-def paged(plan, batch, kv, group, fp32=False, max_tokens=None, max_new=1, starts=False, max_len=4096, n_sink=0, n_local=0):
+def paged(plan, batch, kv, group, fp32=False, max_tokens=None, max_new=1, starts=False, max_len=4096, n_sink=0, n_local=0, row_bytes=0):
     got = (ctypes.c_long * len(_PAGED))()
     plan.paged(batch, kv, group, int(fp32), ctypes.c_long(batch if max_tokens is None else max_tokens), max_new, int(starts), ctypes.c_long(max_len),
-               n_sink, n_local, got)
+               n_sink, n_local, row_bytes, got)
     return dict(zip(_PAGED, got))
 
 
@@ -118,27 +118,32 @@ def test_rows_of_paged_attention_s_forms(plan):
     assert paged(plan, 1, 8, 5, max_new=4)["tile_tokens"] == 6
 
 
+@pytest.mark.parametrize("row_bytes", [0, 128, 256, 512])
 @pytest.mark.parametrize("batch,kv,group,fp32,max_new,max_len,n_local", [
     (1, 8, 4, False, 1, 98304, 0), (1, 8, 4, False, 1, 16, 0), (48, 8, 8, False, 1, 32768, 0), (65536, 1, 1, False, 1, 1 << 30, 0), (3, 1024, 1, False, 1, 4096, 0),
     (7, 300, 2, True, 1, 4096, 0), (512, 8, 4, True, 8192, 131072, 0), (24, 8, 5, False, 4, 20000, 4096), (2, 1, 64, True, 1 << 20, 1 << 20, 0)])
-def test_shares_of_few_rows(plan, batch, kv, group, fp32, max_new, max_len, n_local):
+def test_shares_of_few_rows(plan, batch, kv, group, fp32, max_new, max_len, n_local, row_bytes):
     f = paged(plan, batch, kv, group, fp32, max_tokens=batch * max_new if batch * max_new < 1 << 24 else 1 << 24, max_new=max_new, starts=max_new > 1,
-              max_len=max_len, n_local=n_local)
+              max_len=max_len, n_local=n_local, row_bytes=row_bytes)
     assert f["rows"] <= 32
-    # a counter and two partials for every share of every KV head; about one workgroup per compute unit, or a share for every KV head
-    assert 1 <= f["shares"] and f["shares"] * kv <= 1024 and (f["shares"] == 1 or f["shares"] * kv <= f["target"])
-    assert f["slots"] == 2 * f["shares"] * kv and f["units"] == 0
-    # workgroup i: KV head (i / 8) % kv, share (i / 8) / kv * 8 + i % 8: every one of them is there
-    seen = {((i >> 3) % kv, (i >> 3) // kv * 8 + (i & 7)) for i in range(f["pieces"])}
-    assert {(g, j) for g in range(kv) for j in range(f["shares"])} <= seen
-    # the groups of all row tiles are counted in 31 bits, a group has a key tile for each of eight wavefronts
-    assert f["group_shift"] >= 3
+    assert 0 <= f["near_shift"] <= 2 and f["set_shift"] <= 3 and kv % (1 << f["set_shift"]) == 0 and f["units"] == 0
+    assert f["near_shift"] == 0 or (row_bytes << f["near_shift"] <= 512 and min(group * min(max_new, f["tile_tokens"]), f["rows"]) << f["near_shift"] <= 32)
     row_tiles = batch * -(-max_new // f["tile_tokens"]) * f["head_blocks"]
     charge = -(-max_len // f["key_tile"])
     if n_local:
-        charge = min(charge, -(-0 // f["key_tile"]) + (n_local + f["tile_tokens"] - 2) // f["key_tile"] + 2)
-    assert row_tiles * -(-charge // (1 << f["group_shift"])) + f["shares"] < 1 << 31
-    assert f["group_shift"] == 3 or row_tiles * -(-charge // (1 << (f["group_shift"] - 1))) + 1024 >= (1 << 31) - 1
+        charge = min(charge, (n_local + f["tile_tokens"] - 2) // f["key_tile"] + 2)
+    # a set only where its parts (of the longest item, if all were as long) can be few enough
+    assert f["set_shift"] == 0 or f["target"] << f["set_shift"] <= f["items"] * (16 if f["set_shift"] <= f["near_shift"] and f["items"] * charge >= 128 * f["target"] else 1)
+    groups = lambda shift: row_tiles * -(-charge // (1 << (f["group_shift"] - shift)))
+    for shift in range(f["set_shift"] + 1):                 # whichever the kernel takes
+        sets, most = kv >> shift, f["shares%d" % shift]
+        # a counter for every share of a set, a workgroup per compute unit at most, or one for every set
+        assert most >= 1 and most * sets <= 1024 and (most == 1 or most * sets <= f["target"])
+        # groups of all row tiles are counted in 31 bits; a group has at least a key tile for each of a head's wavefronts
+        assert f["group_shift"] >= 3 and groups(shift) + most < 1 << 31
+        # the grid and the workspace have room for every share (workgroup i: set (i / 8) % sets, share (i / 8) / sets * 8 + i % 8)
+        assert min(f["pieces"] // 8 // sets * 8, f["slots"] // (2 * kv)) >= most
+    assert f["group_shift"] == 3 or row_tiles * -(-charge // (1 << (f["group_shift"] - 1 - f["set_shift"]))) + 1024 >= (1 << 31) - 1
 
 
 @pytest.mark.parametrize("lengths,new,kv,group", [([4099, 2392, 1395, 3337], [4099, 2392, 1395, 3337], 8, 4), ([61440], [2048], 8, 4), ([100000] * 3, [40, 9, 300], 1, 8),
