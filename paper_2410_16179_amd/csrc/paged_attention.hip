@@ -625,8 +625,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
 constexpr int kJoinThreads = 16 * kPagedManyRows / 2;
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const PagedArgs a) {
   constexpr int KT = kPagedManyKeys, R = kPagedManyRows;
-  PagedPiece pc;
-  if (!paged_locate<KT, kCutItems>(a, blockIdx.x, pc)) return;
+  __shared__ PagedPiece cut;
+  __shared__ bool found;
+  if (threadIdx.x < 64) {                                  // (one wavefront looks for all sixteen)
+    PagedPiece pc;
+    const bool there = paged_locate<KT, kCutItems>(a, blockIdx.x, pc);
+    if (threadIdx.x == 0) { cut = pc; found = there; }
+  }
+  __syncthreads();
+  if (!found) return;
+  const PagedPiece pc = cut;
   const int row = blockIdx.y * (R / 2) + (threadIdx.x >> 4), e0 = (threadIdx.x & 15) * 8;
   const int tt = pc.tile / a.head_blocks, hb = pc.tile - tt * a.head_blocks;
   const int first = tt * a.tile_tokens, last = min(first + a.tile_tokens, pc.r.tokens) - 1;
