@@ -357,7 +357,9 @@ MAGICPIG_API int magicpig_page_append(const magicpig_paged_params* params, const
  * the row; keys of a page whose table entry lies outside [0, n_pages) count as outside A.  Lengths are clamped to [0, max_pages *
  * page_size], token counts to [0, max_new], rows to [0, max_tokens).  out [max_tokens, n_q_heads, 128] of
  * `dtype`; lse [max_tokens, n_q_heads] float32 or NULL (two attentions over disjoint keys are joined by
- * it); rows that are no request's token are left as they are. */
+ * it); rows that are no request's token are left as they are.  The kernels are chosen by max_new: where
+ * prompts and single tokens meet in a step, the single ones are faster in a call of their own (of
+ * token_start NULL or a small max_new). */
 MAGICPIG_API int magicpig_paged_attention(const magicpig_paged_params* params, const void* q, const void* k_pages,
                                           const void* v_pages, const float* k_scale, const float* v_scale,
                                           const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,

@@ -618,7 +618,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   const PagedItem done = paged_item<KT, SETS>(a, at_share);      // (read before the barrier: behind it the first thread goes on to the next item)
   __syncthreads();
   finish_item<kF32, NR, SETS>(a, at_share, done, joined, last_one);
-  if (threadIdx.x == 0) paged_next<KT, SETS>(a, at_share);
+  if (wave == 0) paged_next<KT, SETS>(a, at_share);
   __syncthreads();
   if (at_share.pos >= at_share.end) return;
   }

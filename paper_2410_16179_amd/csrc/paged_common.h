@@ -366,19 +366,36 @@ __device__ inline PagedItem paged_item(const PagedArgs& a, const PagedShare& s) 
   i.tile = k & 1 ? tiles - 1 - k / 2 : k / 2;              // (from both ends in turn: later tokens have more keys)
   return i;
 }
-// Behind the item, by one thread: the next request that has rows, if the share goes on there.
+// Behind the item, by one whole wavefront: the next request that has rows, if the share goes on there (requests without rows, idle places of a
+// batch, are passed by 64 at a time).
 template <int KT, bool SETS>
 __device__ inline void paged_next(const PagedArgs& a, PagedShare& s) {
-  const int tiles = paged_row_tiles(a, s.r.tokens), groups = paged_groups<KT>(a, s.r.len, a.group_shift - (SETS ? s.shift : 0));
-  const int next = s.base + tiles * groups, k = tiles > 1 ? (s.pos - s.base) / groups : 0;
-  s.pos = min(s.base + (k + 1) * groups, s.end);
-  if (s.pos < s.end && s.pos == next) {
-    s.base = next;
-    do {
-      if (++s.b >= a.batch) { s.pos = s.end; return; }     // (not reached while the requests stay as they were counted)
-      s.r = paged_request(a, s.b);
-    } while (s.r.tokens == 0);
+  const int lane = threadIdx.x & 63;
+  bool idle = false;
+  if (lane == 0) {
+    const int tiles = paged_row_tiles(a, s.r.tokens), groups = paged_groups<KT>(a, s.r.len, a.group_shift - (SETS ? s.shift : 0));
+    const int next = s.base + tiles * groups, k = tiles > 1 ? (s.pos - s.base) / groups : 0;
+    s.pos = min(s.base + (k + 1) * groups, s.end);
+    if (s.pos < s.end && s.pos == next) {
+      s.base = next;
+      if (++s.b < a.batch) {
+        s.r = paged_request(a, s.b);
+        idle = s.r.tokens == 0;
+      } else {
+        s.pos = s.end;                                     // (not reached while the requests stay as they were counted)
+      }
+    }
   }
+  if (!__any(idle)) return;
+  for (int b0 = uniform(s.b) + 1; b0 < a.batch; b0 += 64) {
+    PagedRequest x{0, 0, 0};
+    if (b0 + lane < a.batch) x = paged_request(a, b0 + lane);
+    const uint64_t found = __ballot(x.tokens > 0);
+    if (!found) continue;
+    if (lane == __ffsll((unsigned long long)found) - 1) { s.b = b0 + lane; s.r = x; }
+    return;
+  }
+  if (lane == 0) s.pos = s.end;
 }
 
 // A partial's maximum as it is stored: an empty partial has -inf, and the join leaves it out.  One whose scores are all NaN has found no

@@ -328,6 +328,14 @@ def test_many_requests():
             new=[int(x) for x in rng.integers(0, 12, 150)], seed=1).check()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_idle_places_between_requests(kind):
+    lengths, new = [0] * 700, [0] * 700
+    for b, n, t in [(0, 40, 1), (63, 5, 2), (64, 900, 1), (300, 3, 3), (301, 17, 1), (690, 2000, 4)]:
+        lengths[b], new[b] = n, t
+    Problem(kind=kind, heads=8, kv_heads=2, page=16, lengths=lengths, new=new, seed=27, spare_rows=2).check()
+
+
 def test_token_counts_are_bounded_by_the_parameters():
     # token_start promises more than max_new: the first max_new rows are taken, at the positions of the last ones
     Problem(kind="bf16", heads=4, kv_heads=2, page=16, lengths=[50, 60], new=[9, 3], max_new=4, seed=8).check()
