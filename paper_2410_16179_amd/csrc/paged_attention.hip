@@ -101,17 +101,18 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
     const int head = SETS && item.shift ? n / rows : 0, row = n - head * rows;
     const float v_scale = scale_of(head);
     const float(*const part)[16 * NR][kPartialRow] = joined + head * waves;
-    float m = -INFINITY;                                   // (fewer than eight wavefronts: some are looked at again, without weight)
+    float m = -INFINITY;                                   // (of fewer than eight wavefronts some are looked at again: the same maximum)
 #pragma unroll
     for (int w = 0; w < kPagedGroup; ++w) m = fmaxf(m, part[w & (waves - 1)][row][128]);
     float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll
     for (int w = 0; w < kPagedGroup; ++w) {
-      const float mw = part[w & (waves - 1)][row][128];
-      const float by = w >= waves || mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
-      l += by * part[w & (waves - 1)][row][129];
+      if (SETS && w >= waves) break;                       // (not taken again with a weight of 0: an output may be infinite)
+      const float mw = part[w][row][128];
+      const float by = mw == -INFINITY ? 0.f : (mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m));
+      l += by * part[w][row][129];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += by * part[w & (waves - 1)][row][e0 + e];
+      for (int e = 0; e < 8; ++e) o[e] += by * part[w][row][e0 + e];
     }
     if (whole) {
       finish(head, row, e0, o, m, l, v_scale);

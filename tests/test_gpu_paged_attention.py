@@ -355,3 +355,16 @@ def test_lse_joins_attentions_over_disjoint_keys():
     joined = sum(o * np.exp(x - top)[..., None] for o, x in parts)
     np.testing.assert_allclose(top, lse, atol=2e-6)
     np.testing.assert_allclose(joined, whole, atol=1e-5)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,batch,shortest,longest,new", [(16, 8, 300, 280, 300, None), (4, 2, 600, 280, 300, None), (12, 4, 400, 270, 300, [2, 1]),
+                                                                       (16, 8, 70, 300, 300, None)])
+def test_infinities_reach_their_rows_where_a_workgroup_takes_several_kv_heads(kind, heads, kv_heads, batch, shortest, longest, new):
+    lengths = np.random.default_rng(batch).integers(shortest, longest + 1, batch).tolist()
+    p = Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=16, lengths=lengths, new=None if new is None else new * (batch // len(new)), seed=31)
+    for b in range(0, batch, 7):
+        for g, pos, e, value in [(b, lengths[b] - 1 - b % 40, 0, "inf"), (b + 1, b % 200, 1, "-inf"), (b + 1, 5, 2, "nan")]:
+            p.v[int(p.table[b, pos // 16]), pos % 16, g % kv_heads, (3 * b + e) % D] = float(value)
+    p.upload()
+    p.check()
