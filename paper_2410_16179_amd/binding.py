@@ -53,10 +53,6 @@ class magicpig_paged_params(ctypes.Structure):
         ("v_new_stride_token", ctypes.c_int64), ("v_new_stride_head", ctypes.c_int64),
     ]
 
-    def __setattr__(self, name, value):
-        self.__dict__.pop("sizes", None)                     # (what _paged_sizes worked out from the fields)
-        super().__setattr__(name, value)
-
 
 EXPORTS = (
     "magicpig_code_words_per_key", "magicpig_code_words_per_query", "magicpig_key_code_bytes",
@@ -337,14 +333,15 @@ class _PagedSizes:
         self.v_new = reach((p.v_new_stride_token, p.max_tokens), (p.v_new_stride_head, p.n_kv_heads))
         self.lse = p.max_tokens * p.n_q_heads
         self.out = self.lse * p.head_dim
-        self.params = ctypes.byref(p)
 
 
 def _paged_sizes(p) -> _PagedSizes:
-    s = p.__dict__.get("sizes")                              # (dropped when a field is set)
-    if s is None:
-        s = p.__dict__["sizes"] = _PagedSizes(p)
-    return s
+    """Worked out once per block and kept with it, next to the bytes they stand for: a block that was changed, in whatever way, or a copy
+    that was, gets its own.  Nothing in them refers to the block."""
+    fields, kept = bytes(p), p.__dict__.get("sizes")
+    if kept is None or kept[0] != fields:
+        kept = p.__dict__["sizes"] = fields, _PagedSizes(p)
+    return kept[1]
 
 
 def _dense(t, device, dtype, elements) -> bool:
@@ -418,7 +415,7 @@ def magicpig_page_plan(params, new_tokens, lengths, block_table, free_pages, n_f
         _refuse(device, new_tokens=of(new_tokens, n), lengths=of(lengths, n), block_table=of(block_table, s.table),
                 free_pages=of(free_pages, s.n_pages), n_free=of(n_free, 1), lengths_out=of(lengths_out, n), n_free_out=of(n_free_out, 1),
                 token_start=of(token_start, n + 1), slots=(slots, (torch.int64,), s.tokens, True, False), status=of(status, 1))
-    _paged_call(device, lib().magicpig_page_plan, s.params, new_tokens.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
+    _paged_call(device, lib().magicpig_page_plan, ctypes.byref(params), new_tokens.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
                 free_pages.data_ptr(), n_free.data_ptr(), lengths_out.data_ptr(), n_free_out.data_ptr(), token_start.data_ptr(),
                 slots.data_ptr(), status.data_ptr(), _ptr(workspace), _nbytes(workspace))
 
@@ -437,7 +434,7 @@ def magicpig_page_append(params, k_new, v_new, slots, k_scale, v_scale, k_pages,
                 slots=(slots, (torch.int64,), s.tokens, True, False), k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False),
                 v_pages=(v_pages, s.pool_dtype, s.v_pages, False, False), k_scale=(k_scale, (f32,), s.heads, True, True),
                 v_scale=(v_scale, (f32,), s.heads, True, True))
-    _paged_call(device, lib().magicpig_page_append, s.params, k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), _ptr(k_scale),
+    _paged_call(device, lib().magicpig_page_append, ctypes.byref(params), k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), _ptr(k_scale),
                 _ptr(v_scale), k_pages.data_ptr(), v_pages.data_ptr())
 
 
@@ -458,7 +455,7 @@ def magicpig_paged_attention(params, q, k_pages, v_pages, k_scale, v_scale, bloc
                 v_scale=(v_scale, (f32,), s.heads, True, True), block_table=(block_table, (i32,), s.table, True, False),
                 lengths=(lengths, (i32,), s.batch, True, False), token_start=(token_start, (i32,), s.batch + 1, True, True),
                 out=(out, (s.dtype,), s.out, True, False), lse=(lse, (f32,), s.lse, True, True))
-    _paged_call(device, lib().magicpig_paged_attention, s.params, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale),
+    _paged_call(device, lib().magicpig_paged_attention, ctypes.byref(params), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale),
                 _ptr(v_scale), block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start), out.data_ptr(), _ptr(lse), _ptr(workspace),
                 _nbytes(workspace))
 

@@ -1,7 +1,9 @@
 """The paged calls' host side, without a GPU: sizes, refusals of parameters and arguments, the binding's own checks,
 and the rules by which the work of paged attention is cut."""
+import copy
 import ctypes
 import math
+import pickle
 
 import numpy as np
 import pytest
@@ -182,3 +184,48 @@ def test_binding_refuses_tensors_that_do_not_fit(name, change, says):
     with pytest.raises(mp.MagicpigError, match="n_free_out"):
         mp.magicpig_page_plan(p, posing(3), posing(3), posing(3, 40), posing(100), posing(1), posing(3), posing(0), posing(4),
                               posing(12, dtype=torch.int64), posing(1))
+
+
+# ---- parameter blocks that are copied, changed and kept ----------------------------------------------------
+@pytest.fixture
+def made(monkeypatch):
+    """The calls that the binding makes of the library, instead of making them: (device, function, block's address, ..)."""
+    calls = []
+    monkeypatch.setattr(mp, "_paged_call", lambda *a: calls.append(a))
+    return calls
+
+
+def call_each(p):
+    mp.magicpig_page_plan(p, posing(p.batch), posing(p.batch), posing(p.batch, p.max_pages), posing(p.n_pages), posing(1), posing(p.batch), posing(1),
+                          posing(p.batch + 1), posing(p.max_tokens, dtype=torch.int64), posing(1))
+    got = attention_arguments(p)
+    new = posing(p.max_tokens, 2, 128, dtype=torch.bfloat16)
+    mp.magicpig_page_append(p, new, new, posing(p.max_tokens, dtype=torch.int64), None, None, got["k_pages"], got["v_pages"])
+    mp.magicpig_paged_attention(p, **got)
+
+
+@pytest.mark.parametrize("how", ["copy", "deepcopy", "pickle"])
+def test_a_copied_block_is_the_one_that_is_passed_on(made, how):
+    p = params()
+    call_each(p)
+    c = {"copy": copy.copy, "deepcopy": copy.deepcopy, "pickle": lambda x: pickle.loads(pickle.dumps(x))}[how](p)
+    assert bytes(c) == bytes(p)
+    p.max_tokens, p.n_pages, p.max_pages = 5000, 7000, 80
+    del made[:]
+    call_each(c)
+    assert len(made) == 3 and all(a[2]._obj is c for a in made)
+    with pytest.raises(mp.MagicpigError, match="elements"):        # the original's tensors have to be larger now
+        mp.magicpig_paged_attention(p, **attention_arguments(c))
+    call_each(p)
+    assert len(made) == 6 and all(a[2]._obj is p for a in made[3:])
+
+
+def test_a_block_changed_past_its_fields_is_read_anew(made):
+    p, other = params(), params(max_tokens=600, max_pages=41)
+    call_each(p)
+    ctypes.memmove(ctypes.addressof(p), ctypes.addressof(other), ctypes.sizeof(p))
+    with pytest.raises(mp.MagicpigError):
+        mp.magicpig_paged_attention(p, **attention_arguments(params()))
+    assert len(made) == 3
+    call_each(p)
+    assert len(made) == 6
