@@ -113,9 +113,9 @@ struct PagedForm {
 
 // Up to 32 rows are taken by the form that keeps keys in registers, 16 or 32 at a time; more (bf16) by the one that shares
 // keys among 128 rows through LDS.  float32: always 16.  Measured, us, requests x keys, 32 heads over 8: up to 16 rows taken 16 | 32 at a time: 1 x 2048
-// (4 rows) 12.5 | 14.3, 1 x 98304 79.0 | 81.5, 16 x 4096 (16 rows) 54.4 | 56.4; 17 to 32 rows 16 | 32 at a time | by the form for many: 20 rows 16 x 4096 94.7 | 56.5
-// | 62.9, 32 rows 1 x 65536 78.2 | 75.4 | 73.1, 64 x 1000 96.6 | 56.4 | 63.0; 36 rows 32 at a time | by the form for many: 16 x 4096 97 | 65.2, 64 x 300
-// 48.5 | 23.0, 1 x 65536 85.1 | 75.5, 1 x 2048 19.4 | 21.9; 64 rows 64 x 1000 102 | 65.6.
+// (4 rows) 12.5 | 14.3, 1 x 98304 79.0 | 81.5, 16 x 4096 (16 rows) 54.4 | 56.4; 17 to 32 rows 16 | 32 at a time | by the form for many: 20 rows 16 x 4096 94.7 | 57.2
+// | 67.1, 32 rows 1 x 65536 78.2 | 76.9 | 76.6, 64 x 1000 96.6 | 54.0 | 62.7; 36 rows 32 at a time | by the form for many: 16 x 4096 97 | 70.7, 64 x 300
+// 37.5 | 24.4, 1 x 65536 85.5 | 80.9, 1 x 2048 19.8 | 24.5; 64 rows 64 x 1000 91.5 | 66.5, 1 x 65536 86.9 | 92.1.
 constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
 constexpr int kPagedNearParts = 16, kPagedNearTiles = 128;   // few rows: see paged_share
 constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share (at most kNumCU, or one for each KV head)
@@ -139,8 +139,8 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   f.tile_tokens = group <= f.rows ? f.rows / group : 1;
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
   // target: workgroups that are resident at once.  Many rows, us with half as many | these | twice as many, 32 heads over 8: 64 rows over 65536 keys
-  // 90 | 87 | 121, 256 over 8192 34.5 | 34.7 | 35.7, 2048 tokens behind 59392 1893 | 1893 | 1935.  Pieces of at least 256 | 512 | 1024 keys: 256 rows
-  // over 8192 38.4 | 34.7 | 38.3, 30 x 300 tokens 147.5 | 147.4 | 142.
+  // 102 | 94 | 128, 256 over 8192 40.3 | 38.5 | 39.0, 2048 tokens behind 59392 2706 | 2708 | 2725.  Pieces of at least 256 | 512 | 1024 keys: 256 rows
+  // over 8192 43.9 | 38.5 | 43.7, 30 x 300 tokens behind 300 162 | 160 | 157.
   f.target = many ? 2 * kNumCU : kNumCU;
   f.min_tiles = 512 / f.key_tile;
   int64_t tiles = (int64_t)batch * ((max_new + f.tile_tokens - 1) / f.tile_tokens);

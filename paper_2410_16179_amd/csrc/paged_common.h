@@ -152,8 +152,8 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
   const bool cut = __any(longest > piece_tiles);
   if (cut && piece_tiles > a.min_tiles) {
     // The smallest of eight lengths that makes no more than target pieces (counted in float32: about), or the first.  Prompt chunks of 128
-    // tokens behind 20000, three requests of 32 heads over 8 (96 row tiles): 221 us with the first always, 164; of 64, seven requests at 30000 390 | 293.
-    // It costs a workgroup 2 us: two of 512 tokens 345 | 349.
+    // tokens behind 20000, three requests of 32 heads over 8 (96 row tiles): 256 us with the first always, 209; of 64, seven requests at 30000 470 | 376.
+    // It costs a workgroup 2 us: two of 512 tokens behind 20000 478 | 478.
     float count[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const float by = __builtin_amdgcn_rcpf((float)piece_tiles);
     for (int b = lane; b < a.batch; b += 64) {
@@ -170,8 +170,8 @@ __device__ inline bool paged_locate(const PagedArgs& a, int index, PagedPiece& o
   }
   if (WHAT == kPieces && cut && a.batch <= 64) {
     // Items with most keys first, over all requests: what is dealt out last is short.  Where items are cut there are few rounds, and the last one
-    // shows: 20 ragged chunks of 100 tokens behind up to 60000 635 us in the requests' order, 599 so; ten of 300 behind 30000 652 | 630.
-    // Where none is, the order by requests keeps what reads the same keys together: 60 prompts of up to 4096 tokens 1347 | 1392, 16 of up to 8192 1327 | 1342.  An item's level is its tiles up to its last token's key
+    // shows: 20 ragged chunks of 100 tokens behind up to 60000 962 us in the requests' order, 750 so; ten of 300 behind 30000 766 | 674.
+    // Where none is, the order by requests keeps what reads the same keys together: 60 prompts of up to 4096 tokens 1300 | 1342, 16 of up to 8192 1745 | 1754.  An item's level is its tiles up to its last token's key
     // (at most what the request is charged); at_least(x): a request's row tiles of level x or more, the last ones.  The level of the
     // item sought is found by halving.
     PagedRequest r{0, 0, 0};

@@ -38,11 +38,12 @@ __device__ inline void each(F&& f) {
 // A operands come from LDS: K rows by 16-byte reads, V^T by the transposing read, four keys of a column at a
 // time.  16-byte chunks of a row are stored at places that depend on the key (chunk ^ key % 16 of K, and
 // chunk ^ 4 (key % 4) of V), so that the lanes of a read meet different banks.
-// Bound by the matrix unit, 52 % busy, and the vector instructions of the weights beside it: 2048 tokens behind 59392 keys, 32 heads over 8, take 1922
-// us, 1055 TFLOP/s (a library product of 8192^3 1204 on this card); four prompts of up to 4099 tokens 344 us, 850 TFLOP/s of what they need (the tiles on the
-// diagonal are formed whole).  Weights after the scores instead of beside the next tile's, and staging through registers: 2364 us.
-// Weights are rounded to bf16 (half a step is 2^-8 of a weight): a second product with what the rounding left
-// would cost half as much matrix work again, and the output is rounded to bf16 anyway.
+// A weight is taken as the sum of two bf16 (off by 2^-16 of it at most), as in the form for few rows, so a token's precision does not depend on how many
+// come with it: two products, with one operand read.  One bf16 alone (2^-8) leaves a third more error in outputs whose values' mean is 0 (4096 keys); it
+// takes 2037 us of the first case below for 2780, and 350 of the second for 450.
+// Bound by the matrix unit: 2048 tokens behind 59392 keys, 32 heads over 8, take 2.71 to 2.80 ms (cards and runs differ), 725 to 750 TFLOP/s of the
+// attention's operations, 1.09 to 1.12 PFLOP/s with the second products (a library product of 8192^3 reaches 1.20 on this card); four prompts of up to 4099
+// tokens 450 us, 650 TFLOP/s. The weights are spread over the products that they wait for; worked out in the first 24 of the 32 steps: 2797 us for 2780.
 template <int ET>
 __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs a) {
   constexpr int kElem = ET == kFP8 ? 1 : 2;
@@ -245,12 +246,17 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
 #pragma unroll
     for (int d = 0; d < 4; ++d) o[d] *= by;
   };
-  // weight n of the lane's 32
-  auto weigh = [&](int n, float ref, f32x16 (&s)[2], u32x4 (&p)[4]) {
+  // weight n of the lane's 32, as the sum of two bf16
+  auto weigh = [&](int n, float ref, f32x16 (&s)[2], u32x4 (&p)[4], u32x4 (&rest)[4]) {
     const int kt = n >> 4, i = n & 15;
     s[kt][i] = __builtin_amdgcn_exp2f(fmaf(s[kt][i], to_log2, -ref));
     l += s[kt][i];
-    if (i & 1) p[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(s[kt][i - 1], s[kt][i]);
+    if (i & 1) {
+      const int x = 2 * kt + (i >> 3), at = (i & 7) >> 1;
+      const uint32_t both = pack_bf16(s[kt][i - 1], s[kt][i]);
+      p[x][at] = both;
+      rest[x][at] = pack_bf16(s[kt][i - 1] - __uint_as_float(both << 16), s[kt][i] - __uint_as_float(both & 0xffff0000u));
+    }
   };
 
   // The tiles, two steps of a tile in flight: while the weights of tile v are worked out, the matrix unit forms the scores of
@@ -294,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
         // Step by step, in this order: a product, the operand of the one kAhead further on, and as much of the weights as the product
         // takes.  Steps 0 .. 15 are the scores of tile v + 1 (behind the last tile those of an old one, unused), 16 .. 31 the output of tile v.
         f32x16 next[2];
-        u32x4 p[4], operand[kAhead];
+        u32x4 p[4], rest[4], operand[kAhead];
         const float ref = m == -INFINITY ? 0.f : m;
         float top = -INFINITY;
         auto request = [&](auto at) {
@@ -308,12 +314,15 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
         each<0, 32>([&](auto at) {
           constexpr int step = decltype(at)::value;
           if constexpr (step < 16) next[step & 1] = mfma32(operand[step % kAhead], q[step >> 1], next[step & 1]);
-          else o[step & 3] = mfma32(operand[step % kAhead], p[(step - 16) >> 2], o[step & 3]);
+          else o[step & 3] = mfma32(operand[step % kAhead], rest[(step - 16) >> 2], mfma32(operand[step % kAhead], p[(step - 16) >> 2], o[step & 3]));
           request(std::integral_constant<int, step + kAhead>{});
-          if constexpr (step < 24) {                       // of the 32 weights
-            each<step * 4 / 3, (step + 1) * 4 / 3>([&](auto n) { weigh(decltype(n)::value, ref, s, p); });
+          // (of the 32 weights twelve beside the sixteen products of the scores, the others beside the first 24 of the output's)
+          if constexpr (step < 16) {
+            each<step * 3 / 4, (step + 1) * 3 / 4>([&](auto n) { weigh(decltype(n)::value, ref, s, p, rest); });
+          } else if constexpr (step < 28) {
+            each<12 + (step - 16) * 5 / 3, 12 + (step - 15) * 5 / 3>([&](auto n) { weigh(decltype(n)::value, ref, s, p, rest); });
           } else {
-            each<4 * (step - 24), 4 * (step - 23)>([&](auto n) { top = fmaxf(top, next[decltype(n)::value >> 4][decltype(n)::value & 15]); });
+            each<8 * (step - 28), 8 * (step - 27)>([&](auto n) { top = fmaxf(top, next[decltype(n)::value >> 4][decltype(n)::value & 15]); });
           }
           __builtin_amdgcn_sched_barrier(0);
         });
@@ -353,18 +362,21 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
       __syncthreads();
       if (key0 <= wave_hi) {
         f32x16 s[2];
-        u32x4 p[4];
+        u32x4 p[4], rest[4];
         bad_page = true;
         score(0, s);
         mask(v, s);
         raise(largest(s) * to_log2);
         const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-        for (int n = 0; n < 32; ++n) weigh(n, ref, s, p);
+        for (int n = 0; n < 32; ++n) weigh(n, ref, s, p, rest);
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) o[d] = mfma32(value_operand(0, x, d), p[x], o[d]);
+          for (int d = 0; d < 4; ++d) {
+            const u32x4 v = value_operand(0, x, d);
+            o[d] = mfma32(v, rest[x], mfma32(v, p[x], o[d]));
+          }
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll

@@ -368,3 +368,19 @@ def test_infinities_reach_their_rows_where_a_workgroup_takes_several_kv_heads(ki
             p.v[int(p.table[b, pos // 16]), pos % 16, g % kv_heads, (3 * b + e) % D] = float(value)
     p.upload()
     p.check()
+
+
+@pytest.mark.parametrize("kind,layout", [("bf16", "token"), ("bf16", "head"), ("fp8", "token")])
+@pytest.mark.parametrize("lengths,new,n_local", [([300, 90], [90, 40], 0), ([1500], [64], 0), ([700, 90], [90, 40], 100), ([6000], [33], 0)])
+@pytest.mark.parametrize("spread", [0.05, 0.3])
+def test_weights_of_many_rows_keep_sixteen_bits(kind, layout, lengths, new, n_local, spread):
+    # values of mean 0: where they cancel, what a weight has lost shows next to what the output's own rounding leaves
+    p = Problem(kind=kind, heads=4, kv_heads=1, page=16, layout=layout, lengths=lengths, new=new, n_local=n_local, spread=spread, seed=34)
+    rng = np.random.default_rng(35)
+    held = torch.from_numpy(p._held(p.v.shape[0]))
+    p.v[held] = torch.from_numpy((40.0 if kind == "fp8" else 1.0) * rng.standard_normal((int(held.sum()), 1, D))).float().to(p.v.dtype)
+    p.upload()
+    out, _ = p.run()
+    want, _, size, reach, count = p.reference()
+    tol = ref.tolerance(want, size, reach, count, kind, False)
+    assert (np.abs(out - want) <= tol).all(), np.max(np.abs(out - want) / tol)
