@@ -359,7 +359,9 @@ MAGICPIG_API int magicpig_page_append(const magicpig_paged_params* params, const
  * `dtype`; lse [max_tokens, n_q_heads] float32 or NULL (two attentions over disjoint keys are joined by
  * it); rows that are no request's token are left as they are.  The kernels are chosen by max_new: where
  * prompts and single tokens meet in a step, the single ones are faster in a call of their own (of
- * token_start NULL or a small max_new). */
+ * token_start NULL or a small max_new).  MAGICPIG_UNSUPPORTED where max_new and max_tokens allow
+ * more row tiles than a grid holds: 2^24, of 128 rows of a KV head each, up to (max_tokens / (128 / G) + batch) * n_kv_heads of them
+ * with G = n_q_heads / n_kv_heads (the other two calls take such parameters, and so does the workspace's size). */
 MAGICPIG_API int magicpig_paged_attention(const magicpig_paged_params* params, const void* q, const void* k_pages,
                                           const void* v_pages, const float* k_scale, const float* v_scale,
                                           const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,

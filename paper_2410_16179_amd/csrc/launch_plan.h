@@ -186,4 +186,8 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   return f;
 }
 
+// Whether the form's workgroups make a grid: its threads are counted in 32 bits (those of few rows are a thousand workgroups or a few).
+constexpr int kPagedManyThreads = 256;
+inline bool paged_grid_fits(const PagedForm& f) { return f.rows != kPagedManyRows || f.pieces * kPagedManyThreads < (int64_t)1 << 32; }
+
 }  // namespace mp

@@ -76,7 +76,8 @@ size_t magicpig_paged_workspace_bytes(const Params* p) {
   if (check(p) != MAGICPIG_OK) return 0;
   size_t m = ws_plan(p);
   for (const bool starts : {false, true}) {
-    const size_t a = ws_attention(form_of(p, starts));
+    const mp::PagedForm f = form_of(p, starts);
+    const size_t a = mp::paged_grid_fits(f) ? ws_attention(f) : 0;   // (attention refuses the others)
     if (a > m) m = a;
   }
   return m < 256 ? 256 : m;
@@ -142,6 +143,7 @@ int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages
       !aligned(lengths, 4) || !aligned(token_start, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(workspace))
     return MAGICPIG_INVALID_ARG;
   const mp::PagedForm f = form_of(p, token_start != nullptr);
+  if (!mp::paged_grid_fits(f)) return MAGICPIG_UNSUPPORTED;
   const size_t need = ws_attention(f);
   if (!workspace || workspace_bytes < need) return MAGICPIG_WORKSPACE_TOO_SMALL;
   if (p->batch == 0) return MAGICPIG_OK;

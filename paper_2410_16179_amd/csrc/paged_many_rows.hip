@@ -45,7 +45,7 @@ __device__ inline void each(F&& f) {
 // attention's operations, 1.09 to 1.12 PFLOP/s with the second products (a library product of 8192^3 reaches 1.20 on this card); four prompts of up to 4099
 // tokens 450 us, 650 TFLOP/s. The weights are spread over the products that they wait for; worked out in the first 24 of the 32 steps: 2797 us for 2780.
 template <int ET>
-__global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(const PagedArgs a) {
   constexpr int kElem = ET == kFP8 ? 1 : 2;
   typedef typename std::conditional<ET == kFP8, u32x2, u32x4>::type Raw;
   __shared__ __align__(16) char lds[2][2][kTileBytes];     // [buffer][keys, values]
@@ -433,8 +433,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_rows_kernel(const PagedArgs
 }  // namespace
 
 void launch_paged_many_rows(const PagedArgs& a, bool fp8, const PagedForm& form, hipStream_t s) {
-  if (fp8) paged_many_rows_kernel<kFP8><<<(unsigned)form.pieces, 256, 0, s>>>(a);
-  else paged_many_rows_kernel<kBF16><<<(unsigned)form.pieces, 256, 0, s>>>(a);
+  if (fp8) paged_many_rows_kernel<kFP8><<<(unsigned)form.pieces, kPagedManyThreads, 0, s>>>(a);
+  else paged_many_rows_kernel<kBF16><<<(unsigned)form.pieces, kPagedManyThreads, 0, s>>>(a);
 }
 
 }  // namespace mp

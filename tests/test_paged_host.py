@@ -229,3 +229,20 @@ def test_a_block_changed_past_its_fields_is_read_anew(made):
     assert len(made) == 3
     call_each(p)
     assert len(made) == 6
+
+
+@accepted
+def test_row_tiles_up_to_what_a_grid_holds():
+    # sixteen heads a KV head: eight tokens a tile; 64 KV heads; keys that are not cut.  2^18 tiles a head make 2^24 workgroups of 256 threads
+    def p(tokens, **kw):
+        return params(**{**dict(batch=1, n_q_heads=1024, n_kv_heads=64, max_pages=32, max_tokens=tokens, max_new=tokens), **kw})
+    assert attend(p((1 << 21) - 8)) == LAUNCH
+    assert attend(p((1 << 21) - 7)) == attend(p(1 << 21)) == attend(p(1 << 24)) == UNSUPPORTED
+    assert attend(params(batch=64, n_q_heads=1024, n_kv_heads=64, max_tokens=1 << 24, max_new=1 << 18)) == UNSUPPORTED
+    # one token a request, and few rows, are no such grid; neither are the other calls
+    assert attend(p(1 << 24), token_start=None) == attend(p(1 << 24, max_new=2)) == LAUNCH
+    assert attend(p(1 << 24, n_q_heads=64, dtype="fp32")) == LAUNCH
+    big = p(1 << 24)
+    assert append(big) == plan(big, bytes=mp.magicpig_paged_workspace_bytes(big)) == LAUNCH
+    assert attend(big, token_start=None, bytes=mp.magicpig_paged_workspace_bytes(big)) == LAUNCH
+    assert mp.magicpig_paged_workspace_bytes(big) < 1 << 26
