@@ -77,9 +77,11 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
   const int max_lo = a.n_local > 0 ? wave_hi - a.n_local + 1 : 0;
   const int end = len - tokens + last + 1;
   // a negative scale goes to the queries, so that the largest score is the largest product; one of 0 becomes the smallest number
-  // there is, which leaves the -inf of a masked score what it is
-  const float signed_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f), to_log2 = signed_log2 == 0.f ? 1.17549435e-38f : fabsf(signed_log2);
-  const uint32_t flip = signed_log2 < 0.f ? 0x80008000u : 0u;
+  // there is, which leaves the -inf of a masked score what it is; one that is a NaN goes to the queries too, for the same reason
+  const float signed_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[pc.g] : 1.f);
+  const bool no_scale = signed_log2 != signed_log2;
+  const float to_log2 = no_scale ? 1.f : (signed_log2 == 0.f ? 1.17549435e-38f : fabsf(signed_log2));
+  const uint32_t flip = signed_log2 < 0.f ? 0x80008000u : 0u, nan = no_scale ? 0x7fff7fffu : 0u;
 
   u32x4 q[8];
   {
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       q[s] = u32x4{0, 0, 0, 0};
-      if (real) q[s] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + at + 16 * s) ^ flip;
+      if (real) q[s] = (*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + at + 16 * s) ^ flip) | nan;
     }
   }
 

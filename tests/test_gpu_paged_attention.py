@@ -384,3 +384,11 @@ def test_weights_of_many_rows_keep_sixteen_bits(kind, layout, lengths, new, n_lo
     want, _, size, reach, count = p.reference()
     tol = ref.tolerance(want, size, reach, count, kind, False)
     assert (np.abs(out - want) <= tol).all(), np.max(np.abs(out - want) / tol)
+
+
+@pytest.mark.parametrize("new", [None, [4, 2, 3], [30, 9, 64]])
+def test_a_scale_that_is_nan_leaves_rows_without_keys_alone(new):
+    p = Problem(kind="fp8", heads=12, kv_heads=2, page=16, lengths=[0, 12, 70] if new is None else [2, 0, 70], new=new, seed=32)
+    p.ks = torch.tensor([float("nan"), 0.015])
+    p.upload()
+    p.check()
