@@ -402,22 +402,27 @@ __device__ inline void paged_next(const PagedArgs& a, PagedShare& s) {
 // maximum either, but its sum is NaN.
 __device__ inline float paged_partial_max(float m, float l) { return m == -INFINITY && l != 0.f ? 0.f : m; }
 
-// Eight elements, e0 .. e0 + 7, of a finished row: o / l (times the values' scale), and with the first ones the row's lse.
+// Eight elements, e0 .. e0 + 7, of a finished row: o / l (times the values' scale), and with the first ones the row's lse.  A row that no key has
+// a weight in is zeros, whatever is in o: logits of -inf at keys whose values are infinite leave a NaN there.
 template <bool FP32>
 __device__ inline void paged_write_row(const PagedArgs& a, int64_t row, int e0, const float (&o)[8], float m, float l, float v_scale) {
-  const float by = l == 0.f ? 0.f : v_scale / l;           // (a NaN stays one)
+  const bool none = l == 0.f;                              // (a NaN is not)
+  const float by = v_scale / l;
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = none ? 0.f : o[e] * by;
   if constexpr (FP32) {
     float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + row * kHeadDim + e0);
-    to[0] = make_float4(o[0] * by, o[1] * by, o[2] * by, o[3] * by);
-    to[1] = make_float4(o[4] * by, o[5] * by, o[6] * by, o[7] * by);
+    to[0] = make_float4(x[0], x[1], x[2], x[3]);
+    to[1] = make_float4(x[4], x[5], x[6], x[7]);
   } else {
     typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
     bf16x8 v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (__bf16)(o[e] * by);
+    for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
     *reinterpret_cast<bf16x8*>(reinterpret_cast<uint16_t*>(a.out) + row * kHeadDim + e0) = v;
   }
-  if (a.lse && e0 == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  if (a.lse && e0 == 0) a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s);

@@ -420,15 +420,16 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
     if (u == 0) { pp[128] = paged_partial_max(m, l); pp[129] = l; }
   } else {
     const int64_t to = (int64_t)(pc.r.row + first + t) * a.Hq + pc.g * a.G + head;
-    const float by = l == 0.f ? 0.f : (a.v_scale ? a.v_scale[pc.g] : 1.f) / l;
+    const bool none = l == 0.f;                          // (as paged_write_row has it)
+    const float by = (a.v_scale ? a.v_scale[pc.g] : 1.f) / l;
+    auto done = [&](int d, int i) { return none ? 0.f : o[d][i] * by; };
     uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + to * kHeadDim + 4 * u;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<u32x2*>(out + 32 * d + 8 * i) = u32x2{pack_bf16(o[d][4 * i] * by, o[d][4 * i + 1] * by),
-                                                               pack_bf16(o[d][4 * i + 2] * by, o[d][4 * i + 3] * by)};
-    if (a.lse && u == 0) a.lse[to] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+        *reinterpret_cast<u32x2*>(out + 32 * d + 8 * i) = u32x2{pack_bf16(done(d, 4 * i), done(d, 4 * i + 1)), pack_bf16(done(d, 4 * i + 2), done(d, 4 * i + 3))};
+    if (a.lse && u == 0) a.lse[to] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
   }
 }
 

@@ -392,3 +392,23 @@ def test_a_scale_that_is_nan_leaves_rows_without_keys_alone(new):
     p.ks = torch.tensor([float("nan"), 0.015])
     p.upload()
     p.check()
+
+
+@pytest.mark.parametrize("kind,new,keys", [("bf16", [1, 1], 70), ("fp32", [2, 1], 70), ("bf16", [5, 1], 70), ("bf16", [40, 1], 70), ("bf16", [1, 1], 6000),
+                                           ("bf16", [40, 1], 6000)])
+@pytest.mark.parametrize("value", ["inf", "nan"])
+def test_a_row_whose_logits_are_all_minus_infinity_gives_zeros_whatever_the_values_are(kind, new, keys, value):
+    p = Problem(kind=kind, heads=4, kv_heads=1, page=16, lengths=[keys, 33], new=new, seed=33)
+    k = p.k[..., 0]
+    k[~torch.isnan(k)] = 1.0
+    p.q[0, 2, 0] = float("-inf")
+    p.v[int(p.table[0, 1]), 3, 0, 7] = float(value)        # (the other rows of the request attend it and take it)
+    p.upload()
+    out, lse = p.run()
+    np.testing.assert_array_equal(out[0, 2], 0.0)
+    assert lse[0, 2] == -np.inf
+    others = np.delete(np.arange(4), 2)
+    np.testing.assert_array_equal(out[0, others, 7], float(value))
+    rest = np.ones(D, bool)
+    rest[7] = False
+    assert np.isfinite(out[0][:, rest]).all() and np.isfinite(lse[0, others]).all()
