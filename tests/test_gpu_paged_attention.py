@@ -412,3 +412,82 @@ def test_a_row_whose_logits_are_all_minus_infinity_gives_zeros_whatever_the_valu
     rest = np.ones(D, bool)
     rest[7] = False
     assert np.isfinite(out[0][:, rest]).all() and np.isfinite(lse[0, others]).all()
+
+
+def counts_problem(**how):
+    """All logits 0, so every weight is 1 exactly: the sum of the weights is the number of keys attended, and with V an indicator (element
+    e of KV head g is 1 in the keys i with (i + 29 g) % 128 == e, else 0) an output times that sum is how many of these are attended."""
+    p = Problem(spread=0.0, seed=36, **how)
+    for b, n in enumerate(p.lengths):
+        i = np.arange(n)
+        for g in range(p.kv_heads):
+            rows = np.zeros((n, D), np.float32)
+            rows[i, (i + 29 * g) % D] = 1.0
+            p.v[torch.from_numpy(p.table[b, i // p.page].astype(np.int64)), torch.from_numpy(i % p.page), g] = torch.from_numpy(rows).to(p.v.dtype)
+    if p.vs is not None:
+        p.vs = torch.full_like(p.vs, 0.5)
+    p.upload()
+    return p
+
+
+def check_counts(p):
+    # lse: a logarithm to half a unit of float32 or so, times ln 2 in float32 and rounded: 2^-22 of it; one key of n makes 1 / n.
+    # out: 1 / sum, the product and the output's rounding: 2^-22, and 2^-8 in bf16; less than half a key of up to 120 there
+    out, lse = p.run()
+    group, scale = p.heads // p.kv_heads, 1.0 if p.vs is None else 0.5
+    for b, n in enumerate(p.lengths):
+        new = int(p.start[b + 1] - p.start[b])
+        for t in range(new):
+            i = np.arange(max(n - new + t + 1, 0))
+            if p.n_local:
+                i = i[(i < p.n_sink) | (i > n - new + t - p.n_local)]
+            for g in range(p.kv_heads):
+                got, got_lse = out[p.start[b] + t, g * group:(g + 1) * group], lse[p.start[b] + t, g * group:(g + 1) * group]
+                if len(i) == 0:
+                    assert (got == 0).all() and (got_lse == -np.inf).all()
+                    continue
+                most = 2.0 ** -22 * np.log(len(i))
+                assert 1.0 / (len(i) + 1) > 2 * most
+                assert (np.abs(got_lse - np.log(len(i))) <= most).all(), (b, t, g, len(i), np.exp(got_lse))
+                there = np.bincount((i + 29 * g) % D, minlength=D)
+                assert there.max() <= 120
+                assert (np.abs(got / scale * len(i) - there) < 0.5).all(), (b, t, g, len(i), np.argwhere(np.abs(got / scale * len(i) - there) >= 0.5)[:4])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads,page,layout", [(8, 2, 64, "token"), (20, 1, 16, "head"), (4, 4, 128, "token")])
+@pytest.mark.parametrize("lengths", [[15011], [8192], [4097, 3, 8191, 0, 513, 512, 511, 15000]])
+def test_every_key_counts_once_for_single_tokens(kind, heads, kv_heads, page, layout, lengths):
+    # one request cut into shares; requests cut at any place, at tile and page borders
+    check_counts(counts_problem(kind=kind, heads=heads, kv_heads=kv_heads, page=page, layout=layout, lengths=lengths))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads,new", [(8, 2, [4, 1, 3, 2, 4]), (10, 2, [6, 6, 2, 5, 1]), (8, 2, [64, 33, 1, 70, 129]), (32, 1, [1, 40, 5, 9, 3]),
+                                                (1, 1, [33, 400, 2, 129, 128])])
+@pytest.mark.parametrize("n_sink,n_local", [(0, 0), (4, 500), (70, 33), (0, 4096), (1, 1)])
+def test_every_key_counts_once_for_new_tokens(kind, heads, kv_heads, new, n_sink, n_local):
+    check_counts(counts_problem(kind=kind, heads=heads, kv_heads=kv_heads, page=32, lengths=[9001, 300, 2, 70, 15104], new=new, n_sink=n_sink, n_local=n_local))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads,batch,shortest,longest", [(32, 32, 70, 0, 60), (16, 8, 300, 250, 300), (24, 12, 200, 60, 90), (8, 8, 20, 6000, 8000)])
+def test_every_key_counts_once_where_a_workgroup_takes_several_kv_heads(kind, heads, kv_heads, batch, shortest, longest):
+    lengths = np.random.default_rng(batch).integers(shortest, longest + 1, batch).tolist()
+    check_counts(counts_problem(kind=kind, heads=heads, kv_heads=kv_heads, page=16, lengths=lengths))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("lengths,new", [([6000, 300, 1030], [150, 40, 129]), ([15104], [129]), ([15000], [33]), ([515, 64, 65, 63], [515, 64, 65, 63]),
+                                         ([12000, 4000, 700, 15000], [40, 50, 33, 64])])
+@pytest.mark.parametrize("n_local", [0, 700])
+def test_every_key_counts_once_for_prompts(kind, lengths, new, n_local):
+    check_counts(counts_problem(kind=kind, heads=4, kv_heads=1, page=64, lengths=lengths, new=new, n_local=n_local, n_sink=3 if n_local else 0))
+
+
+def test_every_key_counts_once_for_many_requests_some_of_them_cut():
+    lengths, new = [100] * 70, [1] * 70
+    for b, n, t in [(0, 15000, 33), (64, 15104, 129), (65, 9000, 40), (69, 12345, 70)]:
+        lengths[b], new[b] = n, t
+    for most in (129, 8):                                 # 128 rows at a time, and 16
+        check_counts(counts_problem(kind="bf16", heads=2, kv_heads=1, page=16, lengths=lengths, new=[min(t, most) for t in new]))
