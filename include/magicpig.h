@@ -276,12 +276,16 @@ MAGICPIG_API int magicpig_sampled_attention_tables(const magicpig_params* params
  * through element strides (page, key, head).  A request's cache is a row of the block table
  * [batch, max_pages] int32: entry j is the page that holds its keys [j page_size, (j + 1) page_size).
  * A slot, page * page_size + offset, names one key's place in the pool.
+ * A dense cache [batch, n_kv_heads, n_cap, 128] of the sampled calls is a pool too, if page_size divides n_cap: strides page_size * 128,
+ * 128 and n_cap * 128, n_pages = ((batch - 1) n_kv_heads + 1) n_cap / page_size, entry j of request b is page
+ * b n_kv_heads n_cap / page_size + j.
  *
  * magicpig_page_plan hands out pages and makes the slot map of a step, magicpig_page_append stores the
  * step's keys and values in their slots, magicpig_paged_attention attends the step's tokens.  All
  * three read what varies from step to step (lengths, token counts, tables) from device memory when
  * their kernels run: one captured graph serves every step; the parameters are bounds.  Two calls that
  * share a workspace or an output must be ordered.  Pool rows that no slot names are left as they are.
+ * Outputs overlap neither inputs nor each other but where it is said that they may.
  * Table entries and slots are checked by the kernels: one outside the pool is never followed. */
 typedef struct magicpig_paged_params {
   int32_t batch;        /* requests (rows of the block table), 0 .. 65536                        */

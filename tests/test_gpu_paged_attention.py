@@ -491,3 +491,38 @@ def test_every_key_counts_once_for_many_requests_some_of_them_cut():
         lengths[b], new[b] = n, t
     for most in (129, 8):                                 # 128 rows at a time, and 16
         check_counts(counts_problem(kind="bf16", heads=2, kv_heads=1, page=16, lengths=lengths, new=[min(t, most) for t in new]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("new", [None, [3, 1, 2], [40, 9, 33]])
+def test_a_dense_cache_is_a_pool(kind, new):
+    # [batch, kv heads, n_cap, 128], as the sampled calls take it, through strides and a table that counts on
+    cap, page, kv_heads = 640, 64, 2
+    p = Problem(kind=kind, heads=8, kv_heads=kv_heads, page=page, lengths=[640, 77, 500], new=new, layout="head", seed=37)
+    want = p.run()
+    batch, per = len(p.lengths), cap // page
+    dense = [torch.full((batch, kv_heads, cap, D), float("nan")).to(x.dtype) for x in (p.k, p.v)]
+    for x, pool in zip(dense, (p.k, p.v)):
+        for b, n in enumerate(p.lengths):
+            i = np.arange(n)
+            x[b, :, :n] = pool[torch.from_numpy(p.table[b, i // page].astype(np.int64)), torch.from_numpy(i % page)].transpose(0, 1)
+    dk, dv = (x.cuda() for x in dense)
+    table = (torch.arange(batch, dtype=torch.int32)[:, None] * kv_heads * per + torch.arange(per, dtype=torch.int32)).cuda()
+    strides = (page * D, D, cap * D)
+    params = p.params(max_pages=per, n_pages=((batch - 1) * kv_heads + 1) * per, k_strides=strides, v_strides=strides)
+    out, lse = torch.full(p.dq.shape, 7.0, dtype=p.dq.dtype, device="cuda"), torch.full(p.dq.shape[:2], 7.0, device="cuda")
+    mp.magicpig_paged_attention(params, p.dq, dk, dv, p.dks, p.dvs, table, p.dlen, None if p.single else p.dstart, out, lse,
+                                mp.alloc_paged_workspace(params))
+    np.testing.assert_array_equal(out.cpu().double().numpy(), want[0])
+    np.testing.assert_array_equal(lse.cpu().double().numpy(), want[1])
+    # a new key of each request that has room
+    rows = torch.randn(batch, kv_heads, D, device="cuda").to(p.dq.dtype)
+    slots = torch.tensor([-1] + [b * kv_heads * cap + p.lengths[b] for b in range(1, batch)], device="cuda")
+    one = mp.make_paged_params(batch=batch, n_q_heads=8, n_kv_heads=kv_heads, dtype=params.dtype, kv_dtype=params.kv_dtype, page_size=page, max_pages=per,
+                               n_pages=params.n_pages, k_strides=strides, v_strides=strides)
+    for b in range(1, batch):
+        dense[0][b, :, p.lengths[b]] = rows[b].cpu().to(dk.dtype)
+        dense[1][b, :, p.lengths[b]] = rows[b].cpu().to(dk.dtype)
+    mp.magicpig_page_append(one, rows, rows, slots, None, None, dk, dv)
+    for got, x in zip((dk, dv), dense):
+        np.testing.assert_array_equal(got.cpu().float().numpy(), x.float().numpy())
