@@ -112,7 +112,8 @@ struct PagedForm {
 };
 
 // Up to 32 rows are taken by the form that keeps keys in registers, 16 or 32 at a time; more (bf16) by the one that shares
-// keys among 128 rows through LDS.  float32: always 16.  Measured, us, requests x keys, 32 heads over 8: up to 16 rows taken 16 | 32 at a time: 1 x 2048
+// keys among 128 rows through LDS.  float32: always 16, for which prompts pay: every sixteen rows read the keys again (four prompts of up to 4099 tokens 5.4 ms,
+// 54 TFLOP/s, 512 tokens behind 8000 708 us, 98 TFLOP/s, of the 153 of a library product).  Measured, us, requests x keys, 32 heads over 8: up to 16 rows taken 16 | 32 at a time: 1 x 2048
 // (4 rows) 12.5 | 14.3, 1 x 98304 79.0 | 81.5, 16 x 4096 (16 rows) 54.4 | 56.4; 17 to 32 rows 16 | 32 at a time | by the form for many: 20 rows 16 x 4096 94.7 | 57.2
 // | 67.1, 32 rows 1 x 65536 78.2 | 76.9 | 76.6, 64 x 1000 96.6 | 54.0 | 62.7; 36 rows 32 at a time | by the form for many: 16 x 4096 97 | 70.7, 64 x 300
 // 37.5 | 24.4, 1 x 65536 85.5 | 80.9, 1 x 2048 19.8 | 24.5; 64 rows 64 x 1000 91.5 | 66.5, 1 x 65536 86.9 | 92.1.

@@ -7,8 +7,9 @@ namespace mp {
 namespace {
 
 // Sixteen lanes take a row of 128 elements, eight a lane, of the keys and of the values: each lane reads its 16
-// bytes (bf16) of both and stores what they become.  Bound by memory: 2 rows in, 2 rows out.  16384 tokens of eight heads
-// into e4m3 pools (101 MB) 21.4 us, 4.7 TB/s, the rate of a large copy; 64 tokens 2.6 us, a launch.
+// bytes (bf16) of both and stores what they become.  Bound by memory: 2 rows in, 2 rows out.  16384 tokens of eight heads, 15360 of them with a slot,
+// in graph replay: into e4m3 pools (94.5 MB) 23 us, 4.1 TB/s, bf16 (126 MB) 24, 5.2 TB/s, float32 (252 MB) 59, 4.3 TB/s (a large copy 4.9); called one
+// behind the other e4m3 takes 21.5.  Rows without a slot are read all the same: their loads are requested beside the slot's.  64 tokens 2.5 us, a launch.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int ET>
@@ -28,7 +29,7 @@ __device__ inline float to_e4m3_range(float x) {          // (comparisons are fa
 // x / scale as correctly rounded as a division gives it, from the reciprocal: the product's remainder is exact (a fused
 // multiply-add), and what it lacks is added.  Beyond 512 the product stands (it is clamped, an infinity and a NaN among them); the sign is the
 // product's (a zero's would be lost).  A quarter of a division's instructions, which were what e4m3 pools waited for:
-// 16384 tokens of eight heads, graph replay, 28.3 -> 24.2 us (3.5 -> 4.2 TB/s; bf16 pools 23.4, 5.7 TB/s).
+// that case, graph replay, 28.3 us with divisions, 24.2 so (then with ordinary stores).
 __device__ inline float quotient(float x, float scale, float inverse) {
   const float q = x * inverse;
   const float r = __builtin_copysignf(fmaf(fmaf(-q, scale, x), inverse, q), q);

@@ -627,7 +627,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
 
 // ---- joining the pieces of an item (many rows) --------------------------------------------------------
 // A workgroup takes half of the rows of a cut item, sixteen lanes a row, eight elements a lane, four partials requested at once.
-// (A workgroup per row, most of them without work, took 35 us of a prompt's 450; two per item take 4.8 where nothing is cut.)
+// (A workgroup per row, most of them without work, took 35 us of four prompts; two per item take 4.8 where nothing is cut.)
 constexpr int kJoinThreads = 16 * kPagedManyRows / 2;
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const PagedArgs a) {
   constexpr int KT = kPagedManyKeys, R = kPagedManyRows;

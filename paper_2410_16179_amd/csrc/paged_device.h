@@ -32,7 +32,8 @@ __device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Loads through a buffer descriptor, not kept in the caches (nt): a step reads a row once.
+// Loads through a buffer descriptor, not kept in the caches (nt): a decoding step reads a row once.  Where a request has several row tiles (more new tokens
+// than 16 or 32 rows hold: float32 prompts above all) each of them reads the rows again, in this way too.
 constexpr int kBufferWord3 = 0x00020000;
 constexpr int kNonTemporal = 2;
 __device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
