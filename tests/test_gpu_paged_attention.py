@@ -526,3 +526,48 @@ def test_a_dense_cache_is_a_pool(kind, new):
     mp.magicpig_page_append(one, rows, rows, slots, None, None, dk, dv)
     for got, x in zip((dk, dv), dense):
         np.testing.assert_array_equal(got.cpu().float().numpy(), x.float().numpy())
+
+
+@pytest.mark.parametrize("kind,heads,kv_heads,page,lengths,new", [
+    ("bf16", 2, 1, 16, [b % 4 for b in range(5000)], None), ("bf16", 2, 1, 16, [b % 5 for b in range(3000)], [b % 3 for b in range(3000)]),
+    ("bf16", 4, 1, 1024, [1023, 1024, 1025, 9000], [9, 33, 1, 70]), ("fp8", 4, 2, 1024, [1023, 1024, 1025, 15000], None), ("fp32", 4, 1, 1024, [1025, 9000], [3, 70]),
+    ("bf16", 300, 300, 16, [700, 40], None), ("fp32", 513, 513, 16, [70, 3], [2, 1]), ("bf16", 300, 300, 16, [700, 40], [33, 5])])
+def test_every_key_counts_once_for_many_requests_large_pages_and_many_heads(kind, heads, kv_heads, page, lengths, new):
+    check_counts(counts_problem(kind=kind, heads=heads, kv_heads=kv_heads, page=page, lengths=lengths, new=new))
+
+
+@pytest.mark.parametrize("new", [None, [40, 5]])
+def test_what_may_be_left_out(new):
+    # no lse, one scale without the other, pools as bytes: the same bits as with them
+    p = Problem(kind="fp8", heads=8, kv_heads=2, page=32, lengths=[5000, 77], new=new, seed=38)
+    one = torch.ones(2, device="cuda")
+
+    def go(k, v, ks, vs, lse):
+        out = torch.zeros_like(p.dq)
+        mp.magicpig_paged_attention(p.params(), p.dq, k, v, ks, vs, p.dtable, p.dlen, None if p.single else p.dstart, out, lse, mp.alloc_paged_workspace(p.params()))
+        return out
+    lse = torch.zeros(p.dq.shape[:2], device="cuda")
+    for ks, vs in ((p.dks, None), (None, p.dvs), (None, None)):
+        full = go(p.dk, p.dv, one if ks is None else ks, one if vs is None else vs, lse)
+        assert torch.isfinite(full).all() and full.abs().max() > 0
+        assert torch.equal(go(p.dk, p.dv, ks, vs, None), full)
+        assert torch.equal(go(p.dk.view(torch.uint8), p.dv.view(torch.uint8), ks, vs, None), full)
+
+
+def test_calls_under_way_together_on_two_streams():
+    # nothing but the arguments and the workspaces is theirs: each gives the bits that it gives alone
+    problems = [Problem(kind="bf16", heads=8, kv_heads=2, page=32, lengths=[30000, 700], seed=39), Problem(kind="fp8", heads=8, kv_heads=8, page=32, lengths=[9000, 4], seed=40),
+                Problem(kind="bf16", heads=8, kv_heads=2, page=32, lengths=[6000, 900], new=[120, 64], seed=41)]
+    alone = [p.run() for p in problems]
+    streams = [torch.cuda.Stream() for _ in problems]
+    work = [(p, p.params(), torch.full_like(p.dq, 7.0), torch.full(p.dq.shape[:2], 7.0, device="cuda"), mp.alloc_paged_workspace(p.params())) for p in problems]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for (p, params, out, lse, ws), s in zip(work, streams):
+            with torch.cuda.stream(s):
+                mp.magicpig_paged_attention(params, p.dq, p.dk, p.dv, p.dks, p.dvs, p.dtable, p.dlen, None if p.single else p.dstart, out, lse, ws)
+    torch.cuda.synchronize()
+    for (p, params, out, lse, ws), want in zip(work, alone):
+        np.testing.assert_array_equal(out.cpu().double().numpy(), want[0])
+        np.testing.assert_array_equal(lse.cpu().double().numpy(), want[1])
+        assert not ws[:4096].any()
