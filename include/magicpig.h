@@ -299,7 +299,7 @@ typedef struct magicpig_paged_params {
   int32_t max_new;      /* new tokens of one request at most, 1 .. 2^24                          */
   int32_t n_sink, n_local;   /* n_local 0: a token attends every key up to its own.  Otherwise the
                            first n_sink keys and the n_local up to its own.  Each 0 .. 2^30      */
-  float scale;          /* of the logits q.k; 0 stands for 1/sqrt(128)                           */
+  float scale;          /* of the logits q.k; 0 stands for 1/sqrt(128); up to 2^127 either way   */
   int64_t n_pages;      /* pages in the pools, 1 .. 2^31 - 1                                     */
   int64_t max_tokens;   /* rows of the token arrays (q, out, lse, new keys and values, slots),
                            1 .. 2^24: the new tokens of all requests at most                     */

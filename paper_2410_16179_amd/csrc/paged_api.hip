@@ -12,6 +12,8 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 bool aligned16(const void* p) { return aligned(p, 16); }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 // new tokens of a request that the token arrays have rows for
 int most_new(const Params* p) { return p->max_new < p->max_tokens ? p->max_new : (int)p->max_tokens; }
 
@@ -21,7 +23,7 @@ int check(const Params* p) {
   if (p->batch < 0 || p->n_q_heads <= 0 || p->n_kv_heads <= 0 || p->n_q_heads % p->n_kv_heads != 0) return MAGICPIG_INVALID_ARG;
   if (p->max_pages < 1 || p->n_pages < 1 || p->max_tokens < 1 || p->max_new < 1) return MAGICPIG_INVALID_ARG;
   if (p->n_sink < 0 || p->n_local < 0 || p->n_sink > (1 << 30) || p->n_local > (1 << 30)) return MAGICPIG_INVALID_ARG;
-  if (!std::isfinite(p->scale)) return MAGICPIG_INVALID_ARG;
+  if (!std::isfinite(p->scale * kLog2e)) return MAGICPIG_INVALID_ARG;
   if (p->head_dim != mp::kHeadDim) return MAGICPIG_UNSUPPORTED;
   if (p->dtype != MAGICPIG_BF16 && p->dtype != MAGICPIG_FP32) return MAGICPIG_UNSUPPORTED;
   if (p->kv_dtype != MAGICPIG_KV_SAME && p->kv_dtype != MAGICPIG_KV_FP8_E4M3) return MAGICPIG_UNSUPPORTED;
@@ -158,7 +160,7 @@ int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages
   a.n_sink = p->n_sink; a.n_local = p->n_local;
   a.max_len = p->max_pages * p->page_size; a.max_tokens = (int)p->max_tokens; a.n_pages = (int)p->n_pages;
   a.tile_tokens = f.tile_tokens; a.head_blocks = f.head_blocks;
-  a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * 1.4426950408889634f;
+  a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * kLog2e;
   a.per_piece = 1.0001f / (float)f.target;                  // (the margin keeps float32's rounding from making more pieces)
   a.target = f.target; a.min_tiles = f.min_tiles; a.slots = (int)f.slots;
   a.near_shift = f.near_shift; a.set_shift = f.set_shift; a.group_shift = f.group_shift;

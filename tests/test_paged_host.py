@@ -246,3 +246,12 @@ def test_row_tiles_up_to_what_a_grid_holds():
     assert append(big) == plan(big, bytes=mp.magicpig_paged_workspace_bytes(big)) == LAUNCH
     assert attend(big, token_start=None, bytes=mp.magicpig_paged_workspace_bytes(big)) == LAUNCH
     assert mp.magicpig_paged_workspace_bytes(big) < 1 << 26
+
+
+@accepted
+def test_a_scale_whose_exponent_of_two_overflows_is_refused():
+    # (an infinite factor would make a NaN of a product that is 0)
+    for value in (2.0 ** 127 * 1.5, -3e38, 2.4e38):
+        p = params(scale=value)
+        assert plan(p) == append(p) == attend(p) == INVALID
+    assert attend(params(scale=2.0 ** 127)) == attend(params(scale=-2.0 ** 127)) == LAUNCH
