@@ -41,10 +41,10 @@ __device__ inline void each(F&& f) {
 // A weight is taken as the sum of two bf16 (off by 2^-16 of it at most), as in the form for few rows, so a token's precision does not depend on how many
 // come with it: two products, with one operand read.  One bf16 alone (2^-8) leaves a third more error in outputs whose values' mean is 0 (4096 keys); it
 // takes 2037 us of the first case below for 2780, and 350 of the second for 450.
-// 2048 tokens behind 59392 keys, 32 heads over 8, take 2.71 to 2.80 ms (cards and runs differ), 725 to 750 TFLOP/s of the attention's operations, 1.09 to
-// 1.12 PFLOP/s with the second products (a library product of 8192^3 reaches 1.20 on this card).  At 1.82 GHz the matrix unit is busy for 58 % of
+// 2048 tokens behind 59392 keys, 32 heads over 8, take 2.65 to 2.80 ms (cards and runs differ), 725 to 765 TFLOP/s of the attention's operations, 1.09 to
+// 1.15 PFLOP/s with the second products (a library product of 8192^3 reaches 1.20 on this card).  At 1.82 GHz the matrix unit is busy for 58 % of
 // the cycles, the vector instructions, those of the weights above all, take 55 %, LDS 49 % (39 for reads, 10 for bringing tiles in): two
-// wavefronts a SIMD, whose products and weights overlap, leave little between them.  Four prompts of up to 4099 tokens 445 to 460 us, 640 TFLOP/s, matrix unit 49 %: the
+// wavefronts a SIMD, whose products and weights overlap, leave little between them.  Four prompts of up to 4099 tokens 435 to 460 us, 635 to 670 TFLOP/s, matrix unit 49 %: the
 // starts and ends of 5.5 rounds of workgroups are not covered (tiles on the diagonal, formed whole, are 4 % of its cycles).  e4m3, widened on the way to LDS: 2.79 ms, 460 us.
 // The weights are spread over the products that they wait for; worked out in the first 24 of the 32 steps: 2797 us for 2780.  With one bf16, weights
 // after the scores instead of beside the next tile's, and staging through registers, took 2364 us for 1922.
