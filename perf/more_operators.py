@@ -538,11 +538,11 @@ def run(s):
                 "evict": _plain_evict}[s["op"]](s)
     from paper_2410_16179_amd import binding as mp
     if s["op"] == "append":
-        mp.magicpig_page_append_mxfp4(s["params"], s["k_new"], s["v_new"], s["slots"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"])
-        mp.magicpig_page_read_mxfp4(s["back_params"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"], s["slots"], s["k_out"], s["v_out"])
+        mp.magicpig_page_append_mxfp(s["params"], s["k_new"], s["v_new"], s["slots"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"])
+        mp.magicpig_page_read_mxfp(s["back_params"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"], s["slots"], s["k_out"], s["v_out"])
         return {"k": s["k_out"], "v": s["v_out"]}
     if s["op"] == "attention":
-        mp.magicpig_paged_attention_mxfp4(s["params"], s["q"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"], s["table"],
+        mp.magicpig_paged_attention_mxfp(s["params"], s["q"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"], s["table"],
                                           s["lengths"], s["token_start"], s["out"], s["lse"], s["ws"])
         return {"out": s["out"], "lse": s["lse"]}
     if s["op"] == "weights":
@@ -558,7 +558,7 @@ def run(s):
     got = {"weights": s["weights"], "free": s["free"], "n_free": s["n_free_out"], "status": s["status"]}
     if s["k_block"] is None:
         return {**got, "k_pages": s["k_pages"], "v_pages": s["v_pages"]}
-    mp.magicpig_page_read_mxfp4(s["params"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"], s["slots"], s["k_out"], s["v_out"])
+    mp.magicpig_page_read_mxfp(s["params"], s["k_pages"], s["v_pages"], s["k_block"], s["v_block"], s["slots"], s["k_out"], s["v_out"])
     return {**got, "k": s["k_out"], "v": s["v_out"]}
 
 
