@@ -47,9 +47,12 @@ extern "C" {
 enum { MAGICPIG_BF16 = 0, MAGICPIG_FP32 = 1 };
 /* storage type of the K / V cache (magicpig_params.kv_dtype) */
 enum { MAGICPIG_KV_SAME = 0,        /* the caches hold `dtype` elements                          */
-       MAGICPIG_KV_FP8_E4M3 = 1 };  /* the caches hold OCP e4m3 bytes (quantised K / V, the
+       MAGICPIG_KV_FP8_E4M3 = 1,    /* the caches hold OCP e4m3 bytes (quantised K / V, the
                                        paper's App. "Limitations and future work"); needs dtype
                                        BF16 for q and W                                          */
+       MAGICPIG_KV_MXFP4 = 4 };     /* paged pools only: microscaled 4-bit floating point (OCP MXFP4),
+                                       two elements a byte and a power of two for each 32 elements;
+                                       needs dtype BF16; see "pools in four bits"                */
 
 enum {
   MAGICPIG_OK = 0,
@@ -293,7 +296,8 @@ typedef struct magicpig_paged_params {
                            64 query heads per KV head, 1024 KV heads                             */
   int32_t head_dim;     /* must be 128 */
   int32_t dtype;        /* MAGICPIG_BF16 | MAGICPIG_FP32: q, new keys and values, out            */
-  int32_t kv_dtype;     /* MAGICPIG_KV_SAME | MAGICPIG_KV_FP8_E4M3 (needs dtype BF16): the pools */
+  int32_t kv_dtype;     /* MAGICPIG_KV_SAME | MAGICPIG_KV_FP8_E4M3 | MAGICPIG_KV_MXFP4 (both need
+                           dtype BF16): the pools                                                */
   int32_t page_size;    /* keys per page: 16, 32, 64, .. 1024 (a power of two)                   */
   int32_t max_pages;    /* entries in a row of the block table; max_pages * page_size <= 2^30    */
   int32_t max_new;      /* new tokens of one request at most, 1 .. 2^24                          */
@@ -303,8 +307,8 @@ typedef struct magicpig_paged_params {
   int64_t n_pages;      /* pages in the pools, 1 .. 2^31 - 1                                     */
   int64_t max_tokens;   /* rows of the token arrays (q, out, lse, new keys and values, slots),
                            1 .. 2^24: the new tokens of all requests at most                     */
-  /* element strides, multiples of 8 (of the pools: of 16 when they hold e4m3), innermost dimension
-   * contiguous; a pool's key stride * page_size stays below 2^31 bytes */
+  /* element strides, multiples of 8 (of the pools: of 16 when they hold e4m3, of 128 when they hold MXFP4),
+   * innermost dimension contiguous; a pool's key stride * page_size stays below 2^31 bytes */
   int64_t k_stride_page, k_stride_key, k_stride_head;     /* pools */
   int64_t v_stride_page, v_stride_key, v_stride_head;
   int64_t q_stride_token, q_stride_head;                  /* q [max_tokens, n_q_heads, 128] */
@@ -370,6 +374,35 @@ MAGICPIG_API int magicpig_paged_attention(const magicpig_paged_params* params, c
                                           const void* v_pages, const float* k_scale, const float* v_scale,
                                           const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,
                                           void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- pools in four bits --------------------------------------------------------------------------
+ * With kv_dtype MAGICPIG_KV_MXFP4 a key's row of 128 elements is 64 bytes of its pool: element d in byte d / 2, an even one in the
+ * low half; bit 3 of a half is the sign, bits 0 .. 2 stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1).  Beside the pool lies one of block scales,
+ * four bytes a row: byte s of elements 32 j .. 32 j + 31 makes them element * 2^(s - 127) (e8m0); 255 makes them NaN.  The strides of the
+ * parameters count elements: byte strides of a pool are half of them, those of its block scales a 32nd.  A row takes 68 bytes for
+ * 256 in bf16.  magicpig_page_plan hands out pages as for other pools; magicpig_page_append and magicpig_paged_attention refuse such
+ * parameters (MAGICPIG_UNSUPPORTED), as these calls do others.
+ *
+ * magicpig_page_append_mxfp stores rows k_new[t], v_new[t] in slot slots[t], as magicpig_page_append does.  A block's scale is the
+ * least power of two, 2^-127 at least, that leaves no element above 6; elements are rounded to the nearest value, of two as near to the
+ * one of even code.  Magnitudes above 3 * 2^126 count as that.  A block with an infinity or a NaN becomes NaN.
+ *
+ * magicpig_page_read_mxfp is the way back: rows of slots slots[t], every t < max_tokens whose slot lies in the pool, as bf16
+ * (exact, but that values of 2^128 and more become infinities) to k_out[t], v_out[t], [max_tokens, n_kv_heads, 128] with the strides of
+ * new keys and values; other rows are left as they are.  The key hashing, a swap to host memory or a dense cache take them from there.
+ *
+ * magicpig_paged_attention_mxfp is magicpig_paged_attention over such pools: same arguments, workspace and result, keys and values being
+ * those that magicpig_page_read_mxfp gives. */
+MAGICPIG_API int magicpig_page_append_mxfp(const magicpig_paged_params* params, const void* k_new, const void* v_new, const int64_t* slots,
+                                            void* k_pages, void* v_pages, uint8_t* k_block_scales, uint8_t* v_block_scales,
+                                            void* hip_stream);
+MAGICPIG_API int magicpig_page_read_mxfp(const magicpig_paged_params* params, const void* k_pages, const void* v_pages,
+                                          const uint8_t* k_block_scales, const uint8_t* v_block_scales, const int64_t* slots, void* k_out,
+                                          void* v_out, void* hip_stream);
+MAGICPIG_API int magicpig_paged_attention_mxfp(const magicpig_paged_params* params, const void* q, const void* k_pages,
+                                                const void* v_pages, const uint8_t* k_block_scales, const uint8_t* v_block_scales,
+                                                const int32_t* block_table, const int32_t* lengths, const int32_t* token_start, void* out,
+                                                float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Profiling aid, and the only setting the library keeps: a per-thread (thread_local) list of
  * events, empty unless this function was called on the calling host thread; production callers

@@ -18,7 +18,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("MAGICPIG_LIB") or os.path.join(_PKG, "libmagicpig.so")
 
 MAGICPIG_BF16, MAGICPIG_FP32 = 0, 1
-MAGICPIG_KV_SAME, MAGICPIG_KV_FP8_E4M3 = 0, 1
+MAGICPIG_KV_SAME, MAGICPIG_KV_FP8_E4M3, MAGICPIG_KV_MXFP4 = 0, 1, 4
 
 
 class MagicpigError(RuntimeError):
@@ -66,6 +66,7 @@ EXPORTS = (
     "magicpig_prepared_projector_bytes", "magicpig_prepare_projector", "magicpig_centering_bytes",
     "magicpig_prepare_centering", "magicpig_hash_query_prepared", "magicpig_hash_decode_step_prepared",
     "magicpig_paged_workspace_bytes", "magicpig_page_plan", "magicpig_page_append", "magicpig_paged_attention",
+    "magicpig_page_append_mxfp", "magicpig_page_read_mxfp", "magicpig_paged_attention_mxfp",
 )
 
 _lib = None
@@ -120,6 +121,12 @@ def lib() -> ctypes.CDLL:
     L.magicpig_page_append.argtypes = [PP] + [vp] * 8
     L.magicpig_paged_attention.restype = ctypes.c_int
     L.magicpig_paged_attention.argtypes = [PP] + [vp] * 11 + [sz, vp]
+    L.magicpig_page_append_mxfp.restype = ctypes.c_int
+    L.magicpig_page_append_mxfp.argtypes = [PP] + [vp] * 8
+    L.magicpig_page_read_mxfp.restype = ctypes.c_int
+    L.magicpig_page_read_mxfp.argtypes = [PP] + [vp] * 8
+    L.magicpig_paged_attention_mxfp.restype = ctypes.c_int
+    L.magicpig_paged_attention_mxfp.argtypes = [PP] + [vp] * 11 + [sz, vp]
     L.magicpig_status_string.restype, L.magicpig_status_string.argtypes = ctypes.c_char_p, [ctypes.c_int]
     L.magicpig_last_hip_error.restype, L.magicpig_last_hip_error.argtypes = ctypes.c_char_p, []
     L.magicpig_profile_stage_events.restype = None
@@ -301,8 +308,9 @@ def make_paged_params(*, batch, n_q_heads, n_kv_heads, dtype, page_size, max_pag
                       q_strides=None, k_new_strides=None, v_new_strides=None) -> magicpig_paged_params:
     """Parameter block of the paged calls.  Element strides default to contiguous pools
     [n_pages, page_size, n_kv_heads, 128] and contiguous token arrays [max_tokens, heads, 128]; pool strides
-    are (page, key, head), those of token arrays (token, head).  max_tokens defaults to batch."""
-    kv_dtype = {"fp8": MAGICPIG_KV_FP8_E4M3, "": 0, None: 0}.get(kv_dtype, kv_dtype)
+    are (page, key, head), those of token arrays (token, head).  max_tokens defaults to batch.  kv_dtype: "" (pools hold
+    `dtype`), "fp8" or "mxfp4"; strides of pools in four bits count elements, two of which are a byte of the tensor."""
+    kv_dtype = {"fp8": MAGICPIG_KV_FP8_E4M3, "mxfp4": MAGICPIG_KV_MXFP4, "": 0, None: 0}.get(kv_dtype, kv_dtype)
     code = {"bf16": MAGICPIG_BF16, "fp32": MAGICPIG_FP32, torch.bfloat16: MAGICPIG_BF16,
             torch.float32: MAGICPIG_FP32}.get(dtype, dtype)
     row = n_kv_heads * head_dim
@@ -324,10 +332,15 @@ class _PagedSizes:
     def __init__(self, p):
         reach = lambda *dims: p.head_dim + sum(stride * (size - 1) for stride, size in dims)
         self.dtype = _DTYPES.get(p.dtype)
-        self.pool_dtype = (torch.float8_e4m3fn, torch.uint8) if p.kv_dtype == MAGICPIG_KV_FP8_E4M3 else (self.dtype,)
+        self.four = p.kv_dtype == MAGICPIG_KV_MXFP4
+        self.pool_dtype = {MAGICPIG_KV_FP8_E4M3: (torch.float8_e4m3fn, torch.uint8),
+                           MAGICPIG_KV_MXFP4: (torch.uint8, torch.float4_e2m1fn_x2)}.get(p.kv_dtype, (self.dtype,))
         self.batch, self.heads, self.n_pages, self.tokens, self.table = p.batch, p.n_kv_heads, p.n_pages, p.max_tokens, p.batch * p.max_pages
         self.k_pages = reach((p.k_stride_page, p.n_pages), (p.k_stride_key, p.page_size), (p.k_stride_head, p.n_kv_heads))
         self.v_pages = reach((p.v_stride_page, p.n_pages), (p.v_stride_key, p.page_size), (p.v_stride_head, p.n_kv_heads))
+        if self.four:                                        # (entries of the tensors: two elements, and a block's scale)
+            self.k_block, self.v_block = self.k_pages // 32, self.v_pages // 32
+            self.k_pages, self.v_pages = self.k_pages // 2, self.v_pages // 2
         self.q = reach((p.q_stride_token, p.max_tokens), (p.q_stride_head, p.n_q_heads))
         self.k_new = reach((p.k_new_stride_token, p.max_tokens), (p.k_new_stride_head, p.n_kv_heads))
         self.v_new = reach((p.v_new_stride_token, p.max_tokens), (p.v_new_stride_head, p.n_kv_heads))
@@ -458,6 +471,68 @@ def magicpig_paged_attention(params, q, k_pages, v_pages, k_scale, v_scale, bloc
     _paged_call(device, lib().magicpig_paged_attention, ctypes.byref(params), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale),
                 _ptr(v_scale), block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start), out.data_ptr(), _ptr(lse), _ptr(workspace),
                 _nbytes(workspace))
+
+
+_SCALES = (torch.uint8, torch.float8_e8m0fnu)
+
+
+def _four_bit_sizes(params) -> _PagedSizes:
+    s = _paged_sizes(params)
+    if not s.four:
+        raise MagicpigError("the parameters' kv_dtype is not MAGICPIG_KV_MXFP4")
+    return s
+
+
+def _rows_mxfp4(params, k_rows, v_rows, slots, k_pages, v_pages, k_block_scales, v_block_scales, names) -> int:
+    """The device of a call between rows and pools in four bits, when everything fits."""
+    s, device = _four_bit_sizes(params), _paged_device(k_pages)
+    try:
+        fits = (_strided(k_rows, device, (s.dtype,), s.k_new) and _strided(v_rows, device, (s.dtype,), s.v_new)
+                and _dense(slots, device, torch.int64, s.tokens) and _strided(k_pages, device, s.pool_dtype, s.k_pages)
+                and _strided(v_pages, device, s.pool_dtype, s.v_pages) and _strided(k_block_scales, device, _SCALES, s.k_block)
+                and _strided(v_block_scales, device, _SCALES, s.v_block))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(device, **{names[0]: (k_rows, (s.dtype,), s.k_new, False, False), names[1]: (v_rows, (s.dtype,), s.v_new, False, False)},
+                slots=(slots, (torch.int64,), s.tokens, True, False), k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False),
+                v_pages=(v_pages, s.pool_dtype, s.v_pages, False, False), k_block_scales=(k_block_scales, _SCALES, s.k_block, False, False),
+                v_block_scales=(v_block_scales, _SCALES, s.v_block, False, False))
+    return device
+
+
+def magicpig_page_append_mxfp(params, k_new, v_new, slots, k_pages, v_pages, k_block_scales, v_block_scales) -> None:
+    device = _rows_mxfp4(params, k_new, v_new, slots, k_pages, v_pages, k_block_scales, v_block_scales, ("k_new", "v_new"))
+    _paged_call(device, lib().magicpig_page_append_mxfp, ctypes.byref(params), k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(),
+                k_pages.data_ptr(), v_pages.data_ptr(), k_block_scales.data_ptr(), v_block_scales.data_ptr())
+
+
+def magicpig_page_read_mxfp(params, k_pages, v_pages, k_block_scales, v_block_scales, slots, k_out, v_out) -> None:
+    device = _rows_mxfp4(params, k_out, v_out, slots, k_pages, v_pages, k_block_scales, v_block_scales, ("k_out", "v_out"))
+    _paged_call(device, lib().magicpig_page_read_mxfp, ctypes.byref(params), k_pages.data_ptr(), v_pages.data_ptr(), k_block_scales.data_ptr(),
+                v_block_scales.data_ptr(), slots.data_ptr(), k_out.data_ptr(), v_out.data_ptr())
+
+
+def magicpig_paged_attention_mxfp(params, q, k_pages, v_pages, k_block_scales, v_block_scales, block_table, lengths, token_start, out,
+                                   lse=None, workspace=None) -> None:
+    s, device, i32, f32 = _four_bit_sizes(params), _paged_device(q, workspace), torch.int32, torch.float32
+    try:
+        fits = (_strided(q, device, (s.dtype,), s.q) and _strided(k_pages, device, s.pool_dtype, s.k_pages)
+                and _strided(v_pages, device, s.pool_dtype, s.v_pages) and _strided(k_block_scales, device, _SCALES, s.k_block)
+                and _strided(v_block_scales, device, _SCALES, s.v_block) and _dense(block_table, device, i32, s.table)
+                and _dense(lengths, device, i32, s.batch) and (token_start is None or _dense(token_start, device, i32, s.batch + 1))
+                and _dense(out, device, s.dtype, s.out) and (lse is None or _dense(lse, device, f32, s.lse)))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(device, q=(q, (s.dtype,), s.q, False, False), k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False),
+                v_pages=(v_pages, s.pool_dtype, s.v_pages, False, False), k_block_scales=(k_block_scales, _SCALES, s.k_block, False, False),
+                v_block_scales=(v_block_scales, _SCALES, s.v_block, False, False), block_table=(block_table, (i32,), s.table, True, False),
+                lengths=(lengths, (i32,), s.batch, True, False), token_start=(token_start, (i32,), s.batch + 1, True, True),
+                out=(out, (s.dtype,), s.out, True, False), lse=(lse, (f32,), s.lse, True, True))
+    _paged_call(device, lib().magicpig_paged_attention_mxfp, ctypes.byref(params), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                k_block_scales.data_ptr(), v_block_scales.data_ptr(), block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start),
+                out.data_ptr(), _ptr(lse), _ptr(workspace), _nbytes(workspace))
 
 
 # ---- buffer helpers (allocation and layout only) ---------------------------------------------

@@ -8,8 +8,9 @@ namespace mp {
 
 // Element types of the tensors.  The helpers below take one as template argument; a `bool FP32`
 // converts to kBF16 / kFP32.  kFP8: OCP e4m3 bytes (value = the decoded byte, no scale), a storage
-// type of the K / V cache only; every e4m3 value is a bf16 value.
-enum : int { kBF16 = 0, kFP32 = 1, kFP8 = 2 };
+// type of the K / V cache only; every e4m3 value is a bf16 value.  kFP4: microscaled e2m1, two elements a byte and beside them an
+// e8m0 byte for each 32, a storage type of paged pools only (not one that the helpers below take).
+enum : int { kBF16 = 0, kFP32 = 1, kFP8 = 2, kFP4 = 3 };
 
 typedef float mp_f32x2 __attribute__((ext_vector_type(2)));
 // eight e4m3 bytes -> eight floats (v_cvt_pk_f32_fp8: two per instruction)

@@ -131,12 +131,13 @@ inline int64_t paged_most_items(int batch, int kv_heads, int group, bool fp32, i
 
 // group: query heads per KV head.  starts: the requests' token counts differ (else one token each).  row_bytes: of a key's row, where the rows of a key's
 // heads lie one behind the other in both pools; else 0.
+// four: pools in four bits, of which a wavefront takes 64 keys at once.
 inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64_t max_tokens, int max_new, bool starts, int64_t max_len,
-                            int n_sink, int n_local, int row_bytes) {
+                            int n_sink, int n_local, int row_bytes, bool four = false) {
   PagedForm f{};
   f.rows = paged_rows(fp32, (int64_t)max_new * group);
   const bool many = f.rows == kPagedManyRows;
-  f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : 32);
+  f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : (four ? 64 : 32));
   f.tile_tokens = group <= f.rows ? f.rows / group : 1;
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
   // target: workgroups that are resident at once.  Many rows, us with half as many | these | twice as many, 32 heads over 8: 64 rows over 65536 keys

@@ -26,8 +26,8 @@ int check(const Params* p) {
   if (!std::isfinite(p->scale * kLog2e)) return MAGICPIG_INVALID_ARG;
   if (p->head_dim != mp::kHeadDim) return MAGICPIG_UNSUPPORTED;
   if (p->dtype != MAGICPIG_BF16 && p->dtype != MAGICPIG_FP32) return MAGICPIG_UNSUPPORTED;
-  if (p->kv_dtype != MAGICPIG_KV_SAME && p->kv_dtype != MAGICPIG_KV_FP8_E4M3) return MAGICPIG_UNSUPPORTED;
-  if (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 && p->dtype != MAGICPIG_BF16) return MAGICPIG_UNSUPPORTED;
+  if (p->kv_dtype != MAGICPIG_KV_SAME && p->kv_dtype != MAGICPIG_KV_FP8_E4M3 && p->kv_dtype != MAGICPIG_KV_MXFP4) return MAGICPIG_UNSUPPORTED;
+  if (p->kv_dtype != MAGICPIG_KV_SAME && p->dtype != MAGICPIG_BF16) return MAGICPIG_UNSUPPORTED;
   if (p->batch > 65536 || p->n_kv_heads > 1024 || p->n_q_heads / p->n_kv_heads > 64) return MAGICPIG_UNSUPPORTED;
   if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)) != 0) return MAGICPIG_UNSUPPORTED;
   if ((int64_t)p->max_pages * p->page_size > ((int64_t)1 << 30)) return MAGICPIG_UNSUPPORTED;
@@ -38,14 +38,17 @@ int check(const Params* p) {
   return MAGICPIG_OK;
 }
 
-int element_bytes(const Params* p) { return p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? 1 : (p->dtype == MAGICPIG_FP32 ? 4 : 2); }
+bool four(const Params* p) { return p->kv_dtype == MAGICPIG_KV_MXFP4; }
+int64_t row_bytes(const Params* p, int64_t elements) {
+  return four(p) ? elements / 2 : elements * (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? 1 : (p->dtype == MAGICPIG_FP32 ? 4 : 2));
+}
 
 int check_pool(const Params* p, int64_t page, int64_t key, int64_t head) {
   if (page < 0 || key < mp::kHeadDim || head < 0) return MAGICPIG_INVALID_ARG;
-  const int64_t unit = p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? 16 : 8;
+  const int64_t unit = four(p) ? mp::kHeadDim : (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? 16 : 8);   // (four bits: a row's scales are a word)
   if (page % unit || key % unit || head % unit) return MAGICPIG_UNSUPPORTED;
   // rows inside a page are addressed by 32-bit byte offsets
-  if (key > ((int64_t)1 << 31) || key * p->page_size * element_bytes(p) >= ((int64_t)1 << 31)) return MAGICPIG_UNSUPPORTED;
+  if (key > ((int64_t)1 << 31) || row_bytes(p, key * p->page_size) >= ((int64_t)1 << 31)) return MAGICPIG_UNSUPPORTED;
   return MAGICPIG_OK;
 }
 int check_pools(const Params* p) {
@@ -60,7 +63,7 @@ int check_rows(int64_t token, int64_t head) {
 mp::PagedForm form_of(const Params* p, bool starts) {
   return mp::paged_form(p->batch, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->dtype == MAGICPIG_FP32, p->max_tokens, starts ? most_new(p) : 1,
                         starts, (int64_t)p->max_pages * p->page_size, p->n_sink, p->n_local,
-                        p->k_stride_head == mp::kHeadDim && p->v_stride_head == mp::kHeadDim ? mp::kHeadDim * element_bytes(p) : 0);
+                        p->k_stride_head == mp::kHeadDim && p->v_stride_head == mp::kHeadDim ? (int)row_bytes(p, mp::kHeadDim) : 0, four(p));
 }
 // The workspace: counters of arrived partials (zero between calls), then what a call keeps for itself.
 constexpr size_t kCounterBytes = MAGICPIG_PAGED_COUNTER_BYTES;
@@ -68,6 +71,48 @@ static_assert(kCounterBytes == mp::kPagedCounters * sizeof(unsigned), "");
 size_t ws_attention(const mp::PagedForm& f) { return kCounterBytes + align256((size_t)f.slots * f.rows * mp::kPartialStride * sizeof(float)); }
 size_t ws_plan(const Params* p) {
   return !mp::page_plan_needs_workspace(p->batch, p->max_tokens) ? 0 : kCounterBytes + align256((size_t)3 * (p->batch + 1) * sizeof(int));
+}
+
+// Attention over pools of any kind, behind check().
+int attend(const Params* p, const void* q, const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
+           const uint8_t* k_block, const uint8_t* v_block, const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,
+           void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int st;
+  if ((st = check_pools(p)) != MAGICPIG_OK) return st;
+  if ((st = check_rows(p->q_stride_token, p->q_stride_head)) != MAGICPIG_OK) return st;
+  if (!token_start && p->max_tokens < p->batch) return MAGICPIG_INVALID_ARG;   // (row b of request b)
+  if (!q || !k_pages || !v_pages || !out || (p->batch > 0 && (!block_table || !lengths))) return MAGICPIG_INVALID_ARG;
+  if (p->kv_dtype != MAGICPIG_KV_FP8_E4M3 && (k_scale || v_scale)) return MAGICPIG_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(block_table, 4) ||
+      !aligned(lengths, 4) || !aligned(token_start, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(workspace))
+    return MAGICPIG_INVALID_ARG;
+  const mp::PagedForm f = form_of(p, token_start != nullptr);
+  if (!mp::paged_grid_fits(f)) return MAGICPIG_UNSUPPORTED;
+  const size_t need = ws_attention(f);
+  if (!workspace || workspace_bytes < need) return MAGICPIG_WORKSPACE_TOO_SMALL;
+  if (p->batch == 0) return MAGICPIG_OK;
+  mp::PagedArgs a{};
+  a.q = q; a.k = k_pages; a.v = v_pages; a.k_scale = k_scale; a.v_scale = v_scale;
+  a.k_block = k_block; a.v_block = v_block;
+  a.table = block_table; a.lengths = lengths; a.token_start = token_start;
+  a.out = out; a.lse = lse;
+  a.arrived = reinterpret_cast<unsigned*>(workspace);
+  a.partial = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + kCounterBytes);
+  a.batch = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
+  a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages; a.max_new = token_start ? most_new(p) : 1;
+  a.n_sink = p->n_sink; a.n_local = p->n_local;
+  a.max_len = p->max_pages * p->page_size; a.max_tokens = (int)p->max_tokens; a.n_pages = (int)p->n_pages;
+  a.tile_tokens = f.tile_tokens; a.head_blocks = f.head_blocks;
+  a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * kLog2e;
+  a.per_piece = 1.0001f / (float)f.target;                  // (the margin keeps float32's rounding from making more pieces)
+  a.target = f.target; a.min_tiles = f.min_tiles; a.slots = (int)f.slots;
+  a.near_shift = f.near_shift; a.set_shift = f.set_shift; a.group_shift = f.group_shift;
+  for (int i = 0; i <= f.set_shift; ++i) a.shares[i] = f.shares[i];
+  a.k_page = p->k_stride_page; a.k_key = p->k_stride_key; a.k_head = p->k_stride_head;
+  a.v_page = p->v_stride_page; a.v_key = p->v_stride_key; a.v_head = p->v_stride_head;
+  a.q_t = p->q_stride_token; a.q_h = p->q_stride_head;
+  const int element = four(p) ? mp::kFP4 : (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? mp::kFP8 : (p->dtype == MAGICPIG_FP32 ? mp::kFP32 : mp::kBF16));
+  return mp::hip_status(mp::launch_paged_attention(a, element, f, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 }  // namespace
@@ -111,6 +156,7 @@ int magicpig_page_append(const Params* p, const void* k_new, const void* v_new, 
                          const float* v_scale, void* k_pages, void* v_pages, void* hip_stream) {
   int st = check(p);
   if (st != MAGICPIG_OK) return st;
+  if (four(p)) return MAGICPIG_UNSUPPORTED;
   if ((st = check_pools(p)) != MAGICPIG_OK) return st;
   if ((st = check_rows(p->k_new_stride_token, p->k_new_stride_head)) != MAGICPIG_OK) return st;
   if ((st = check_rows(p->v_new_stride_token, p->v_new_stride_head)) != MAGICPIG_OK) return st;
@@ -134,42 +180,72 @@ int magicpig_page_append(const Params* p, const void* k_new, const void* v_new, 
 int magicpig_paged_attention(const Params* p, const void* q, const void* k_pages, const void* v_pages, const float* k_scale,
                              const float* v_scale, const int32_t* block_table, const int32_t* lengths, const int32_t* token_start, void* out,
                              float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int st = check(p);
+  if (st != MAGICPIG_OK) return st;
+  if (four(p)) return MAGICPIG_UNSUPPORTED;
+  return attend(p, q, k_pages, v_pages, k_scale, v_scale, nullptr, nullptr, block_table, lengths, token_start, out, lse, workspace,
+                workspace_bytes, hip_stream);
+}
+
+int magicpig_paged_attention_mxfp(const Params* p, const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_block_scales,
+                                   const uint8_t* v_block_scales, const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,
+                                   void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int st = check(p);
+  if (st != MAGICPIG_OK) return st;
+  if (!four(p)) return MAGICPIG_UNSUPPORTED;
+  if (!k_block_scales || !v_block_scales || !aligned(k_block_scales, 4) || !aligned(v_block_scales, 4)) return MAGICPIG_INVALID_ARG;
+  return attend(p, q, k_pages, v_pages, nullptr, nullptr, k_block_scales, v_block_scales, block_table, lengths, token_start, out, lse, workspace,
+                workspace_bytes, hip_stream);
+}
+
+namespace {
+
+// Rows to or from pools in four bits; the rows are written by a call that reads the pools.
+int check_mxfp4(const Params* p, const void* k_rows, const void* v_rows, const int64_t* slots, const void* k_pages, const void* v_pages,
+                const uint8_t* k_block, const uint8_t* v_block) {
   int st = check(p);
   if (st != MAGICPIG_OK) return st;
+  if (!four(p)) return MAGICPIG_UNSUPPORTED;
   if ((st = check_pools(p)) != MAGICPIG_OK) return st;
-  if ((st = check_rows(p->q_stride_token, p->q_stride_head)) != MAGICPIG_OK) return st;
-  if (!token_start && p->max_tokens < p->batch) return MAGICPIG_INVALID_ARG;   // (row b of request b)
-  if (!q || !k_pages || !v_pages || !out || (p->batch > 0 && (!block_table || !lengths))) return MAGICPIG_INVALID_ARG;
-  if (p->kv_dtype != MAGICPIG_KV_FP8_E4M3 && (k_scale || v_scale)) return MAGICPIG_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(block_table, 4) ||
-      !aligned(lengths, 4) || !aligned(token_start, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(workspace))
+  if ((st = check_rows(p->k_new_stride_token, p->k_new_stride_head)) != MAGICPIG_OK) return st;
+  if ((st = check_rows(p->v_new_stride_token, p->v_new_stride_head)) != MAGICPIG_OK) return st;
+  if (!k_rows || !v_rows || !slots || !k_pages || !v_pages || !k_block || !v_block) return MAGICPIG_INVALID_ARG;
+  if (!aligned16(k_rows) || !aligned16(v_rows) || !aligned(slots, 8) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned(k_block, 4) ||
+      !aligned(v_block, 4))
     return MAGICPIG_INVALID_ARG;
-  const mp::PagedForm f = form_of(p, token_start != nullptr);
-  if (!mp::paged_grid_fits(f)) return MAGICPIG_UNSUPPORTED;
-  const size_t need = ws_attention(f);
-  if (!workspace || workspace_bytes < need) return MAGICPIG_WORKSPACE_TOO_SMALL;
-  if (p->batch == 0) return MAGICPIG_OK;
-  mp::PagedArgs a{};
-  a.q = q; a.k = k_pages; a.v = v_pages; a.k_scale = k_scale; a.v_scale = v_scale;
-  a.table = block_table; a.lengths = lengths; a.token_start = token_start;
-  a.out = out; a.lse = lse;
-  a.arrived = reinterpret_cast<unsigned*>(workspace);
-  a.partial = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + kCounterBytes);
-  a.batch = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
-  a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages; a.max_new = token_start ? most_new(p) : 1;
-  a.n_sink = p->n_sink; a.n_local = p->n_local;
-  a.max_len = p->max_pages * p->page_size; a.max_tokens = (int)p->max_tokens; a.n_pages = (int)p->n_pages;
-  a.tile_tokens = f.tile_tokens; a.head_blocks = f.head_blocks;
-  a.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * kLog2e;
-  a.per_piece = 1.0001f / (float)f.target;                  // (the margin keeps float32's rounding from making more pieces)
-  a.target = f.target; a.min_tiles = f.min_tiles; a.slots = (int)f.slots;
-  a.near_shift = f.near_shift; a.set_shift = f.set_shift; a.group_shift = f.group_shift;
-  for (int i = 0; i <= f.set_shift; ++i) a.shares[i] = f.shares[i];
+  return MAGICPIG_OK;
+}
+
+mp::PageMxfp4Args mxfp4_args(const Params* p, const void* k_rows, const void* v_rows, const int64_t* slots, const void* k_pages,
+                             const void* v_pages, const uint8_t* k_block, const uint8_t* v_block) {
+  mp::PageMxfp4Args a{};
+  a.k_rows = const_cast<void*>(k_rows); a.v_rows = const_cast<void*>(v_rows); a.slots = slots;
+  a.k_pages = static_cast<uint8_t*>(const_cast<void*>(k_pages)); a.v_pages = static_cast<uint8_t*>(const_cast<void*>(v_pages));
+  a.k_block = const_cast<uint8_t*>(k_block); a.v_block = const_cast<uint8_t*>(v_block);
+  a.heads = p->n_kv_heads; a.page_shift = __builtin_ctz(p->page_size);
+  a.n_slots = p->n_pages * p->page_size; a.tokens = p->max_tokens;
+  a.kn_t = p->k_new_stride_token; a.kn_h = p->k_new_stride_head; a.vn_t = p->v_new_stride_token; a.vn_h = p->v_new_stride_head;
   a.k_page = p->k_stride_page; a.k_key = p->k_stride_key; a.k_head = p->k_stride_head;
   a.v_page = p->v_stride_page; a.v_key = p->v_stride_key; a.v_head = p->v_stride_head;
-  a.q_t = p->q_stride_token; a.q_h = p->q_stride_head;
-  const int element = p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? mp::kFP8 : (p->dtype == MAGICPIG_FP32 ? mp::kFP32 : mp::kBF16);
-  return mp::hip_status(mp::launch_paged_attention(a, element, f, reinterpret_cast<hipStream_t>(hip_stream)));
+  return a;
+}
+
+}  // namespace
+
+int magicpig_page_append_mxfp(const Params* p, const void* k_new, const void* v_new, const int64_t* slots, void* k_pages, void* v_pages,
+                               uint8_t* k_block_scales, uint8_t* v_block_scales, void* hip_stream) {
+  const int st = check_mxfp4(p, k_new, v_new, slots, k_pages, v_pages, k_block_scales, v_block_scales);
+  if (st != MAGICPIG_OK) return st;
+  return mp::hip_status(mp::launch_page_append_mxfp4(mxfp4_args(p, k_new, v_new, slots, k_pages, v_pages, k_block_scales, v_block_scales),
+                                                     reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+int magicpig_page_read_mxfp(const Params* p, const void* k_pages, const void* v_pages, const uint8_t* k_block_scales,
+                             const uint8_t* v_block_scales, const int64_t* slots, void* k_out, void* v_out, void* hip_stream) {
+  const int st = check_mxfp4(p, k_out, v_out, slots, k_pages, v_pages, k_block_scales, v_block_scales);
+  if (st != MAGICPIG_OK) return st;
+  return mp::hip_status(mp::launch_page_read_mxfp4(mxfp4_args(p, k_out, v_out, slots, k_pages, v_pages, k_block_scales, v_block_scales),
+                                                   reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -162,10 +162,10 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
 template <int ET, int NR>
 struct FewRows {
   static constexpr bool kF32 = ET == kFP32;
-  static constexpr int kTile = kF32 ? 16 : 32;           // keys per tile
+  static constexpr int kTile = kF32 ? 16 : (ET == kFP4 ? 64 : 32);   // keys per tile
   static constexpr int kHalves = kTile / 16;
-  static constexpr int kFrags = 8;                       // loads of a lane per tile for V, and for K, which e4m3 takes 16 elements at a time
-  static constexpr int kKeyFrags = ET == kFP8 ? 4 : 8;
+  static constexpr int kFrags = ET == kFP4 ? 4 : 8;      // loads of a lane per tile for V, and for K, which e4m3 takes 16 elements at a time
+  static constexpr int kKeyFrags = ET == kFP8 || ET == kFP4 ? 4 : 8;
   typedef typename std::conditional<ET == kFP8, u32x2, u32x4>::type Raw;
 
   u32x4 q[NR][kF32 ? 8 : 4];                             // query rows, as the B operand
@@ -173,14 +173,15 @@ struct FewRows {
   float m[NR], l[NR];
   u32x4 kf[kKeyFrags];
   Raw vf[kFrags];
+  uint32_t ks[ET == kFP4 ? kHalves : 1], vs[ET == kFP4 ? kHalves : 1];   // four bits: scales as they come
 };
 
 template <int ET, int NR, bool SETS>
 __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const PagedArgs a) {
   using F = FewRows<ET, NR>;
-  constexpr bool kF32 = F::kF32;
+  constexpr bool kF32 = F::kF32, kFour = ET == kFP4;
   constexpr int KT = F::kTile, R = 16 * NR;
-  constexpr int kElem = ET == kFP32 ? 4 : (ET == kFP8 ? 1 : 2);
+  constexpr int kElem = ET == kFP32 ? 4 : (ET == kFP8 ? 1 : 2);   // (not of kFP4)
   __shared__ float joined[kPagedGroup][R][kPartialRow];
   __shared__ int last_one;
 
@@ -238,17 +239,28 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   const float to_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[g] : 1.f);
 
   const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)item.b * a.max_pages);
-  const char* kbase = reinterpret_cast<const char*>(a.k) + (int64_t)g * a.k_head * kElem;
-  const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)g * a.v_head * kElem;
+  const char* kbase = reinterpret_cast<const char*>(a.k) + pool_bytes<ET>((int64_t)g * a.k_head);
+  const char* vbase = reinterpret_cast<const char*>(a.v) + pool_bytes<ET>((int64_t)g * a.v_head);
   const int page_mask = (1 << a.page_shift) - 1;
-  const uint32_t k_key = (uint32_t)a.k_key * kElem, v_key = (uint32_t)a.v_key * kElem;
+  const uint32_t k_key = (uint32_t)pool_bytes<ET>(a.k_key), v_key = (uint32_t)pool_bytes<ET>(a.v_key);
   // This lane's place in 16 keys.  K: a quad of lanes takes keys 4 (c / 4) + i, one (e4m3: two) at a time, of which each lane
   // 16 bytes; V: keys 4u .. 4u + 3.
   const int quad = c >> 2, in_quad = c & 3;
   const bool odd = c & 1, upper = c & 2;
-  const uint32_t k_lane = (ET == kFP8 ? 4 * quad + (in_quad >> 1) : 4 * quad) * k_key +
-                          (ET == kFP8 ? 32 * u + 16 * (in_quad & 1) : 64 * u + 16 * in_quad);
-  const uint32_t v_lane = 4 * u * v_key + (kF32 ? 16 * c : 8 * c * kElem);
+  uint32_t k_lane = (ET == kFP8 ? 4 * quad + (in_quad >> 1) : 4 * quad) * k_key +
+                    (ET == kFP8 ? 32 * u + 16 * (in_quad & 1) : 64 * u + 16 * in_quad);
+  uint32_t v_lane = 4 * u * v_key + (kF32 ? 16 * c : 8 * c * kElem);
+  // Four bits: sixteen rows of 64 bytes are one load, a quad of lanes to a row; rows change lanes through the wavefront's own part of LDS (K in its
+  // first 4096 bytes, V in the next, V's scales behind them), where lane 4 r + p leaves what it has at 16 times its number: chunk p ^ (r / 4) of
+  // row r, so that lanes which read a chunk of 16 rows, or one of rows 4u + j, meet different banks.
+  char* const exchange = reinterpret_cast<char*>(&joined[wave][0][0]);
+  if constexpr (kFour) {
+    k_lane = (lane >> 2) * k_key + 16 * (in_quad ^ u);
+    v_lane = (lane >> 2) * v_key + 16 * (in_quad ^ u);
+  }
+  const char* const ksbase = reinterpret_cast<const char*>(a.k_block) + ((int64_t)g * a.k_head >> 5);
+  const char* const vsbase = reinterpret_cast<const char*>(a.v_block) + ((int64_t)g * a.v_head >> 5);
+  const uint32_t ks_key = (uint32_t)(a.k_key >> 5), vs_key = (uint32_t)(a.v_key >> 5);
 
   auto tile_key = [&](int v) { return (v < span.sink ? v : v + span.skip) * KT; };
   auto tile_pages = [&](int v, TilePages<KT>& p) {
@@ -263,7 +275,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   auto request_k = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
-      const auto rows = rows16(kbase, a.k_page * kElem, k_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
+      const auto rows = rows16(kbase, pool_bytes<ET>(a.k_page), k_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
+      if constexpr (kFour) {
+        const auto scales = rows16(ksbase, a.k_page >> 5, ks_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
+        load_once(rows, k_lane, f.kf[h]);
+        f.ks[h] = load_byte(scales, c * ks_key + u);
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < F::kKeyFrags / F::kHalves; ++i) {
         const uint32_t at = ET == kFP8 ? 2 * i * k_key : (i & 3) * k_key + 256 * (i >> 2);
@@ -274,7 +292,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   auto request_v = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
-      const auto rows = rows16(vbase, a.v_page * kElem, v_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
+      const auto rows = rows16(vbase, pool_bytes<ET>(a.v_page), v_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
+      if constexpr (kFour) {
+        const auto scales = rows16(vsbase, a.v_page >> 5, vs_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
+        load_once(rows, v_lane, f.vf[h]);
+        load_once(scales, c * vs_key, f.vs[h]);
+        continue;
+      } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (kF32) {
@@ -284,12 +308,20 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
           load_once(rows, v_lane + j * v_key, f.vf[4 * h + j]);
         }
       }
+      }
     }
   };
   constexpr int kScores = 4 * F::kHalves;                // of a lane: key 16 (i / 4) + 4 u + i % 4 of the tile is number i
   auto scores = [&](float (&s)[NR][kScores]) {
     // a key per lane: its elements 32 u .. 32 u + 31 (float32: 16 u .. 16 u + 15 of both halves of the row)
-    if constexpr (ET == kFP8) {
+    if constexpr (kFour) {
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) *reinterpret_cast<u32x4*>(exchange + 1024 * h + 16 * lane) = f.kf[h];
+      in_order();
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) f.kf[h] = *reinterpret_cast<const u32x4*>(exchange + 1024 * h + 64 * c + 16 * (u ^ quad));
+      in_order();
+    } else if constexpr (ET == kFP8) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) join_halves(f.kf[2 * h], f.kf[2 * h + 1], upper);
     } else {
@@ -313,7 +345,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           u32x4 k;
-          if constexpr (ET == kFP8) {
+          if constexpr (kFour) {
+            k = e2m1_to_bf16(f.kf[h][i], f.ks[h] << 23);
+          } else if constexpr (ET == kFP8) {
             const u32x4 w = f.kf[2 * h + (i >> 1)];
             k = e4m3_to_bf16(i & 1 ? u32x2{w.z, w.w} : u32x2{w.x, w.y});
           } else {
@@ -363,7 +397,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       }
     }
   };
-  auto add_values = [&](const float (&s)[NR][kScores], const u32x4 (&v)[8]) {
+  // (of the weights those from `at` on)
+  auto add_values = [&](const float (&s)[NR][kScores], const u32x4 (&v)[8], int at0) {
     if constexpr (kF32) {
 #pragma unroll
       for (int d = 0; d < 2; ++d)
@@ -380,8 +415,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          ph[n][i] = pack_bf16(s[n][2 * i], s[n][2 * i + 1]);
-          pl[n][i] = pack_bf16(s[n][2 * i] - __uint_as_float(ph[n][i] << 16), s[n][2 * i + 1] - __uint_as_float(ph[n][i] & 0xffff0000u));
+          const float s0 = s[n][at0 + 2 * i], s1 = s[n][at0 + 2 * i + 1];
+          ph[n][i] = pack_bf16(s0, s1);
+          pl[n][i] = pack_bf16(s0 - __uint_as_float(ph[n][i] << 16), s1 - __uint_as_float(ph[n][i] & 0xffff0000u));
         }
 #pragma unroll
       for (int t8 = 0; t8 < 8; ++t8) {                   // V^T of elements 8 c + t8, two keys a register
@@ -394,13 +430,37 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       }
     }
   };
-  auto values = [&](u32x4 (&v)[8]) {
+  // Four bits: V into LDS, from where values() takes 32 keys at a time, those from 32 `group` on.
+  auto stage_v = [&]() {
+    if constexpr (kFour) {
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) *reinterpret_cast<u32x4*>(exchange + 4096 + 1024 * h + 16 * lane) = f.vf[h];
+      const uint32_t lower = u & 1 ? f.vs[1] : f.vs[0], higher = u & 1 ? f.vs[3] : f.vs[2];
+      *reinterpret_cast<uint32_t*>(exchange + 8192 + 4 * lane) = u & 2 ? higher : lower;
+      in_order();
+    }
+  };
+  auto values = [&](u32x4 (&v)[8], int group) {
+    if constexpr (kFour) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 scale = *reinterpret_cast<const u32x4*>(exchange + 8192 + 64 * (2 * group + h) + 16 * u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(exchange + 4096 + 1024 * (2 * group + h) + 64 * (4 * u + j) + 16 * (quad ^ u) + 4 * in_quad);
+          v[4 * h + j] = e2m1_to_bf16(w, rotate_right(scale[j], to_scale(quad)));
+        }
+      }
+      return;
+    } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (ET == kFP8) v[i] = e4m3_to_bf16(f.vf[i]);
       else v[i] = f.vf[i];
     }
+    }
   };
+  constexpr int kGroups = kFour ? 2 : 1;                 // of keys, in which the values are taken
 
   // whether every row attends all keys of a tile
   auto in_full = [&](int v) {
@@ -492,11 +552,20 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       valid_rows(key1, p, valid);
       request_k(key1, p, valid);
     }
+    if constexpr (kFour) {
+      stage_v();
+      if (ahead < t_end) request_v(key1, p, valid);
+    }
     weigh(s);
-    u32x4 vb[8];
-    values(vb);
-    add_values(s, vb);
-    if (ahead < t_end) request_v(key1, p, valid);
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) {
+      u32x4 vb[8];
+      values(vb, x);
+      add_values(s, vb, 8 * x);
+    }
+    if constexpr (!kFour) {
+      if (ahead < t_end) request_v(key1, p, valid);
+    }
     v = v1;
     v1 = v2;
     next = after;
@@ -517,11 +586,20 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       valid_rows(tile_key(w1), p, valid);
       request_k(tile_key(w1), p, valid);
     }
+    if constexpr (kFour) {
+      stage_v();
+      if (w1 < t_end) request_v(tile_key(w1), p, valid);
+    }
     weigh(s);
-    u32x4 vb[8];
-    values(vb);
-    add_values(s, vb);
-    if (w1 < t_end) request_v(tile_key(w1), p, valid);
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) {
+      u32x4 vb[8];
+      values(vb, x);
+      add_values(s, vb, 8 * x);
+    }
+    if constexpr (!kFour) {
+      if (w1 < t_end) request_v(tile_key(w1), p, valid);
+    }
     w = w1;
   }
 
@@ -546,18 +624,23 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
       float s[NR][kScores];
       scores(s);
       mask(key0, valid, s);
+      stage_v();
       weigh(s);
-      u32x4 vb[8];
-      values(vb);
       uint32_t cleared = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const u32x4 x = finite_part<kF32>(vb[i]), d = x ^ vb[i];
-        cleared |= d.x | d.y | d.z | d.w;
-        vb[i] = x;
+      for (int group = 0; group < kGroups; ++group) {
+        u32x4 vb[8];
+        values(vb, group);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const u32x4 x = finite_part<kF32>(vb[i]), d = x ^ vb[i];
+          cleared |= d.x | d.y | d.z | d.w;
+          vb[i] = x;
+        }
+        add_values(s, vb, 8 * group);
       }
-      add_values(s, vb);
       if (!__any(cleared != 0)) continue;
+      if constexpr (kFour) in_order();
       // (the weights change lanes through LDS)
 #pragma unroll
       for (int n = 0; n < NR; ++n)
@@ -565,15 +648,22 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
         for (int i = 0; i < kScores; ++i) joined[wave][c + 16 * n][16 * (i >> 2) + 4 * u + (i & 3)] = s[n][i];
 #pragma unroll 1
       for (int k = 0; k < KT; ++k) {
-        const int key = key0 + k, id = F::kHalves == 2 && k >= 16 ? now.id[F::kHalves - 1] : now.id[0];
+        const int key = key0 + k;
+        int id = F::kHalves == 2 && k >= 16 ? now.id[F::kHalves - 1] : now.id[0];
+        if constexpr (F::kHalves == 4) id = k >= 32 ? (k >= 48 ? now.id[3] : now.id[2]) : (k >= 16 ? now.id[1] : now.id[0]);
         if (!page_ok(id) || key >= end) continue;
-        const char* row = vbase + id * (a.v_page * kElem) + (uint32_t)(key & page_mask) * v_key;
+        const char* row = vbase + id * pool_bytes<ET>(a.v_page) + (uint32_t)(key & page_mask) * v_key;
 #pragma unroll
         for (int i = 0; i < (kF32 ? 8 : 4); ++i) {          // four elements at a time, or eight
           float x[8];
           if constexpr (kF32) {
             const float4 w = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(row) + 64 * (i >> 2) + 16 * u + 4 * (i & 3));
             x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+          } else if constexpr (kFour) {
+            const uint32_t scale = reinterpret_cast<const uint8_t*>(vsbase + id * (a.v_page >> 5) + (uint32_t)(key & page_mask) * vs_key)[u];
+            const u32x4 w = e2m1_to_bf16(*reinterpret_cast<const uint32_t*>(row + 16 * u + 4 * i), scale << 23);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
           } else {
             load8<ET>(row, 32 * u + 8 * i, x);
           }
@@ -696,10 +786,11 @@ hipError_t launch_few_rows(const PagedArgs& a, const PagedForm& form, hipStream_
 hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s) {
   if (element == kFP32) return launch_few_rows<kFP32, 1>(a, form, s);
   if (form.rows == kPagedManyRows) {
-    launch_paged_many_rows(a, element == kFP8, form, s);
+    launch_paged_many_rows(a, element, form, s);
     if (form.units > 0) paged_join_kernel<<<dim3((unsigned)form.units, 2), kJoinThreads, 0, s>>>(a);
     return hipGetLastError();
   }
+  if (element == kFP4) return form.rows == 16 ? launch_few_rows<kFP4, 1>(a, form, s) : launch_few_rows<kFP4, 2>(a, form, s);
   if (form.rows == 16) return element == kFP8 ? launch_few_rows<kFP8, 1>(a, form, s) : launch_few_rows<kBF16, 1>(a, form, s);
   return element == kFP8 ? launch_few_rows<kFP8, 2>(a, form, s) : launch_few_rows<kBF16, 2>(a, form, s);
 }

@@ -22,6 +22,16 @@ struct PageAppendArgs {
   int64_t k_page, k_key, k_head, v_page, v_key, v_head;
 };
 
+// Rows to or from pools in four bits (page_mxfp4.hip): strides in elements, those of the scales are the pools' / 32.
+struct PageMxfp4Args {
+  void* k_rows; void* v_rows; const int64_t* slots;
+  uint8_t* k_pages; uint8_t* v_pages; uint8_t* k_block; uint8_t* v_block;
+  int heads, page_shift;
+  int64_t n_slots, tokens;
+  int64_t kn_t, kn_h, vn_t, vn_h;
+  int64_t k_page, k_key, k_head, v_page, v_key, v_head;
+};
+
 // Paged attention.  The rows of a request (its new tokens times the query heads of a KV head) are taken
 // in row tiles of whole tokens (tile_tokens each; where one token has more heads than a tile has rows,
 // head_blocks tiles per token).  An item is a row tile of one request and KV head; its keys are counted
@@ -49,6 +59,7 @@ struct PagedArgs {
   int near_shift, set_shift, group_shift, shares[kPagedGroupShift + 1];   // few rows: see PagedForm
   unsigned* arrived;      // few rows: partials of the cut item that begins in a share which are there (0 between calls)
   int64_t k_page, k_key, k_head, v_page, v_key, v_head, q_t, q_h;
+  const uint8_t* k_block; const uint8_t* v_block;         // scales of pools in four bits: strides are those of the elements / 32
 };
 
 struct PagedRequest {
@@ -427,7 +438,9 @@ __device__ inline void paged_write_row(const PagedArgs& a, int64_t row, int e0, 
 
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s);
 hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s);
-void launch_paged_many_rows(const PagedArgs& a, bool fp8, const PagedForm& form, hipStream_t s);
+hipError_t launch_page_append_mxfp4(const PageMxfp4Args& a, hipStream_t s);
+hipError_t launch_page_read_mxfp4(const PageMxfp4Args& a, hipStream_t s);
+void launch_paged_many_rows(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s);
 hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s);
 
 }  // namespace mp

@@ -24,6 +24,27 @@ __device__ inline u32x4 e4m3_to_bf16(u32x2 w) {
   return r;
 }
 
+// Eight e2m1 elements, four bytes, times 2^(scale - 127) as eight bf16, two per instruction: exact but where bf16 overflows (to an
+// infinity) or ends (below 2^-133); scale 255 gives NaN.  scale: the e8m0 byte in bits 23 .. 30 (the instruction looks at no others).
+__device__ inline u32x4 e2m1_to_bf16(uint32_t w, uint32_t scale) {
+  const float s = __uint_as_float(scale);
+  u32x4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+  return r;
+}
+// What has to be rotated right to bring byte `i` of a word to bits 23 .. 30.
+__device__ inline int to_scale(int i) { return (8 * i + 9) & 31; }
+__device__ inline uint32_t rotate_right(uint32_t w, int by) { return __builtin_amdgcn_alignbit(w, w, by); }
+
+// Bytes of so many elements of a pool (a multiple of two of kFP4).
+template <int ET>
+__device__ inline int64_t pool_bytes(int64_t elements) {
+  return ET == kFP4 ? elements >> 1 : elements * (ET == kFP32 ? 4 : (ET == kFP8 ? 1 : 2));
+}
+
 __device__ inline uint32_t pack_bf16(float lo, float hi) {
   const bf16x2 v = {(__bf16)lo, (__bf16)hi};
   return __builtin_bit_cast(uint32_t, v);
@@ -42,6 +63,10 @@ __device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4
 __device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
   to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, kNonTemporal));
 }
+__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, uint32_t& to) {
+  to = __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, kNonTemporal);
+}
+__device__ inline uint32_t load_byte(__amdgpu_buffer_rsrc_t rows, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b8(rows, at, 0, 0); }
 // The same, kept: workgroups of other row tiles read the row too.
 __device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
   to = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0));
@@ -67,6 +92,14 @@ __device__ inline f32x2 load_through(const float* from) {
   return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 __device__ inline void stored() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Between what a wavefront's lanes write to its own part of LDS and what others of its lanes read there: the unit takes a wavefront's
+// accesses in their order, so only the compiler has to keep it.
+__device__ inline void in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // w without infinities and NaN: a float32, or two bf16.
 template <bool F32>

@@ -50,8 +50,11 @@ __device__ inline void each(F&& f) {
 // after the scores instead of beside the next tile's, and staging through registers, took 2364 us for 1922.
 template <int ET>
 __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(const PagedArgs a) {
-  constexpr int kElem = ET == kFP8 ? 1 : 2;
-  typedef typename std::conditional<ET == kFP8, u32x2, u32x4>::type Raw;
+  constexpr bool kWiden = ET == kFP8 || ET == kFP4;        // stored in fewer bits than they are in LDS
+  // A load of a lane.  Four bits: a quarter of a row and the scale of its elements; one load takes sixteen rows, of the others four.
+  struct Quarter { u32x4 w; uint32_t scale; };
+  typedef typename std::conditional<ET == kFP4, Quarter, typename std::conditional<ET == kFP8, u32x2, u32x4>::type>::type Raw;
+  constexpr int kLoads = ET == kFP4 ? 1 : 4;
   __shared__ __align__(16) char lds[2][2][kTileBytes];     // [buffer][keys, values]
   __shared__ int bad_pages;                               // whether a tile had a page that is none
 
@@ -98,13 +101,14 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
   }
 
   const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)pc.b * a.max_pages);
-  const char* kbase = reinterpret_cast<const char*>(a.k) + (int64_t)pc.g * a.k_head * kElem;
-  const char* vbase = reinterpret_cast<const char*>(a.v) + (int64_t)pc.g * a.v_head * kElem;
+  const char* kbase = reinterpret_cast<const char*>(a.k) + pool_bytes<ET>((int64_t)pc.g * a.k_head);
+  const char* vbase = reinterpret_cast<const char*>(a.v) + pool_bytes<ET>((int64_t)pc.g * a.v_head);
   const int page_mask = (1 << a.page_shift) - 1;
-  const uint32_t k_key = (uint32_t)a.k_key * kElem, v_key = (uint32_t)a.v_key * kElem;
+  const uint32_t k_key = (uint32_t)pool_bytes<ET>(a.k_key), v_key = (uint32_t)pool_bytes<ET>(a.v_key);
   // Staging: a wavefront takes sixteen keys of a tile, K and V, four rows at a time (sixteen lanes a row): one page and two descriptors each.
   const int srow = lane >> 4, chunk = lane & 15;
-  const uint32_t k_from = srow * k_key + 8 * chunk * kElem, v_from = srow * v_key + 8 * chunk * kElem;
+  const uint32_t k_from = ET == kFP4 ? (lane >> 2) * k_key + 16 * (lane & 3) : srow * k_key + (uint32_t)pool_bytes<ET>(8 * chunk);
+  const uint32_t v_from = ET == kFP4 ? (lane >> 2) * v_key + 16 * (lane & 3) : srow * v_key + (uint32_t)pool_bytes<ET>(8 * chunk);
   const int k_to = (16 * wave + srow) * 256, k_chunk = (chunk ^ srow) << 4, v_to = (16 * wave + srow) * 256 + ((chunk ^ srow << 2) << 4);
   // reading
   const int k_at = c * 256, k_swap = (u ^ (c & 15)) << 4;
@@ -120,33 +124,65 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
   };
   auto valid_keys = [&](int v, int id) { return page_ok(id) ? min(max(end - tile_key(v) - 16 * wave, 0), 16) : 0; };
   auto k_rows = [&](int v, int id) {
-    return rows16(kbase, a.k_page * kElem, k_key, id, (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id));
+    return rows16(kbase, pool_bytes<ET>(a.k_page), k_key, id, (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id));
   };
   auto v_rows = [&](int v, int id) {
-    return rows16(vbase, a.v_page * kElem, v_key, id, (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id));
+    return rows16(vbase, pool_bytes<ET>(a.v_page), v_key, id, (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id));
   };
-  // Through registers (e4m3, which is widened on the way, and sixteens that are not whole): fetch(), and put() some time later.
-  auto fetch = [&](__amdgpu_buffer_rsrc_t rows, uint32_t from, uint32_t key_stride, Raw (&r)[4]) {
+  // Through registers (e4m3 and four bits, which are widened on the way, and sixteens that are not whole): fetch(), and put() some time later.
+  auto fetch = [&](__amdgpu_buffer_rsrc_t rows, uint32_t from, uint32_t key_stride, Raw (&r)[kLoads]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_shared(rows, from + 4 * i * key_stride, r[i]);
+    for (int i = 0; i < kLoads; ++i) {
+      if constexpr (ET == kFP4) load_shared(rows, from, r[i].w);
+      else load_shared(rows, from + 4 * i * key_stride, r[i]);
+    }
   };
-  auto put_k = [&](int buf, const Raw (&r)[4]) {
+  auto fetch_k = [&](__amdgpu_buffer_rsrc_t rows, int v, int id, Raw (&r)[kLoads]) {
+    fetch(rows, k_from, k_key, r);
+    if constexpr (ET == kFP4) {
+      const uint32_t key = (uint32_t)(a.k_key >> 5);
+      r[0].scale = load_byte(rows16(reinterpret_cast<const char*>(a.k_block) + ((int64_t)pc.g * a.k_head >> 5), a.k_page >> 5, key, id,
+                                    (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id)), (lane >> 2) * key + (lane & 3));
+    }
+  };
+  auto fetch_v = [&](__amdgpu_buffer_rsrc_t rows, int v, int id, Raw (&r)[kLoads]) {
+    fetch(rows, v_from, v_key, r);
+    if constexpr (ET == kFP4) {
+      const uint32_t key = (uint32_t)(a.v_key >> 5);
+      r[0].scale = load_byte(rows16(reinterpret_cast<const char*>(a.v_block) + ((int64_t)pc.g * a.v_head >> 5), a.v_page >> 5, key, id,
+                                    (tile_key(v) + 16 * wave) & page_mask, valid_keys(v, id)), (lane >> 2) * key + (lane & 3));
+    }
+  };
+  // (four bits: a lane has chunks 4 p .. 4 p + 3 of row lane / 4, p = lane % 4)
+  auto put_k = [&](int buf, const Raw (&r)[kLoads]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       u32x4 k;
-      if constexpr (ET == kFP8) k = e4m3_to_bf16(r[i]);
-      else k = r[i];
-      *reinterpret_cast<u32x4*>(&lds[buf][0][k_to + 1024 * i + (k_chunk ^ 64 * i)]) = k;
+      if constexpr (ET == kFP4) {
+        k = e2m1_to_bf16(r[0].w[i], r[0].scale << 23);
+        const int at = (16 * wave + (lane >> 2)) * 256 + ((4 * (lane & 3) + i) ^ (lane >> 2)) * 16;
+        *reinterpret_cast<u32x4*>(&lds[buf][0][at]) = k;
+      } else {
+        if constexpr (ET == kFP8) k = e4m3_to_bf16(r[i]);
+        else k = r[i];
+        *reinterpret_cast<u32x4*>(&lds[buf][0][k_to + 1024 * i + (k_chunk ^ 64 * i)]) = k;
+      }
     }
   };
-  auto put_v = [&](int buf, const Raw (&r)[4], auto careful) {
+  auto put_v = [&](int buf, const Raw (&r)[kLoads], auto careful) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       u32x4 x;
-      if constexpr (ET == kFP8) x = e4m3_to_bf16(r[i]);
+      if constexpr (ET == kFP4) x = e2m1_to_bf16(r[0].w[i], r[0].scale << 23);
+      else if constexpr (ET == kFP8) x = e4m3_to_bf16(r[i]);
       else x = r[i];
       if constexpr (decltype(careful)::value) x = finite_part<false>(x);
-      *reinterpret_cast<u32x4*>(&lds[buf][1][v_to + 1024 * i]) = x;
+      if constexpr (ET == kFP4) {
+        const int at = (16 * wave + (lane >> 2)) * 256 + ((4 * (lane & 3) + i) ^ (lane >> 2 & 3) << 2) * 16;
+        *reinterpret_cast<u32x4*>(&lds[buf][1][at]) = x;
+      } else {
+        *reinterpret_cast<u32x4*>(&lds[buf][1][v_to + 1024 * i]) = x;
+      }
     }
   };
   // Straight into LDS: a load leaves its lanes' 16 bytes one behind the other, four rows, so a lane asks for the chunk that belongs
@@ -161,33 +197,33 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
     for (int i = 0; i < 4; ++i) load_to_lds(rows, srow * v_key + 4 * i * v_key + ((chunk ^ srow << 2) << 4), &lds[buf][1][4096 * wave + 1024 * i]);
   };
   // A tile's sixteen keys of this wavefront: on their way (bring), and there (arrived, at the latest before the next barrier).
-  Raw kr[4], vr[4];
+  Raw kr[kLoads], vr[kLoads];
   auto bring_k = [&](int buf, int v, int id) {
     const auto rows = k_rows(v, id);
-    if constexpr (ET == kFP8) {
-      fetch(rows, k_from, k_key, kr);
+    if constexpr (kWiden) {
+      fetch_k(rows, v, id, kr);
     } else if (valid_keys(v, id) == 16) {
       straight_k(buf, rows);
     } else {
-      Raw r[4];
-      fetch(rows, k_from, k_key, r);
+      Raw r[kLoads];
+      fetch_k(rows, v, id, r);
       put_k(buf, r);
     }
   };
   auto bring_v = [&](int buf, int v, int id) {
     const auto rows = v_rows(v, id);
-    if constexpr (ET == kFP8) {
-      fetch(rows, v_from, v_key, vr);
+    if constexpr (kWiden) {
+      fetch_v(rows, v, id, vr);
     } else if (valid_keys(v, id) == 16) {
       straight_v(buf, rows);
     } else {
-      Raw r[4];
-      fetch(rows, v_from, v_key, r);
+      Raw r[kLoads];
+      fetch_v(rows, v, id, r);
       put_v(buf, r, std::false_type{});
     }
   };
-  auto arrived_k = [&](int buf) { if constexpr (ET == kFP8) put_k(buf, kr); };
-  auto arrived_v = [&](int buf) { if constexpr (ET == kFP8) put_v(buf, vr, std::false_type{}); };
+  auto arrived_k = [&](int buf) { if constexpr (kWiden) put_k(buf, kr); };
+  auto arrived_v = [&](int buf) { if constexpr (kWiden) put_v(buf, vr, std::false_type{}); };
 
   f32x16 o[4];
   float m, l;
@@ -360,10 +396,10 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
 #pragma unroll 1
     for (int v = t_begin; v < t_end; ++v) {
       const int key0 = tile_key(v), id0 = tile_page(v);
-      Raw r[4];
-      fetch(k_rows(v, id0), k_from, k_key, r);
+      Raw r[kLoads];
+      fetch_k(k_rows(v, id0), v, id0, r);
       put_k(0, r);
-      fetch(v_rows(v, id0), v_from, v_key, r);
+      fetch_v(v_rows(v, id0), v, id0, r);
       put_v(0, r, std::true_type{});
       __syncthreads();
       if (key0 <= wave_hi) {
@@ -391,7 +427,8 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
         for (int k = 0; k < KT; ++k) {
           const int key = key0 + k, id = table[min(key >> a.page_shift, a.max_pages - 1)];
           if (!page_ok(id) || key >= end) continue;
-          const char* from = vbase + id * (a.v_page * kElem) + (uint32_t)(key & page_mask) * v_key;
+          const char* from = vbase + id * pool_bytes<ET>(a.v_page) + (uint32_t)(key & page_mask) * v_key;
+          const uint8_t* scales = ET == kFP4 ? a.v_block + ((int64_t)pc.g * a.v_head >> 5) + id * (a.v_page >> 5) + (uint32_t)(key & page_mask) * (uint32_t)(a.v_key >> 5) : nullptr;
           const bool attends = key <= hi && (key >= lo || key < a.n_sink);
           const float w = weights[k];
 #pragma unroll
@@ -401,6 +438,7 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
               const int e = 32 * d + 8 * (i >> 2) + 4 * u + (i & 3);
               float y;
               if constexpr (ET == kFP8) y = fp8_to_float(reinterpret_cast<const uint8_t*>(from)[e]);
+              else if constexpr (ET == kFP4) y = __uint_as_float(e2m1_to_bf16((uint32_t)reinterpret_cast<const uint8_t*>(from)[e >> 1] >> 4 * (e & 1), (uint32_t)scales[e >> 5] << 23).x << 16);
               else y = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(from)[e] << 16);
               if (attends && !(fabsf(y) < INFINITY)) o[d][i] += w * y;
             }
@@ -439,8 +477,9 @@ __global__ __launch_bounds__(kPagedManyThreads, 2) void paged_many_rows_kernel(c
 
 }  // namespace
 
-void launch_paged_many_rows(const PagedArgs& a, bool fp8, const PagedForm& form, hipStream_t s) {
-  if (fp8) paged_many_rows_kernel<kFP8><<<(unsigned)form.pieces, kPagedManyThreads, 0, s>>>(a);
+void launch_paged_many_rows(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s) {
+  if (element == kFP4) paged_many_rows_kernel<kFP4><<<(unsigned)form.pieces, kPagedManyThreads, 0, s>>>(a);
+  else if (element == kFP8) paged_many_rows_kernel<kFP8><<<(unsigned)form.pieces, kPagedManyThreads, 0, s>>>(a);
   else paged_many_rows_kernel<kBF16><<<(unsigned)form.pieces, kPagedManyThreads, 0, s>>>(a);
 }
 
