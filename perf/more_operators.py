@@ -376,7 +376,7 @@ def prepare(case, seed):
         both = dict(batch=c["batch"], n_q_heads=c["q_heads"], n_kv_heads=c["kv_heads"], dtype=c["dtype"], kv_dtype=c["kv"], page_size=c["page"])
         s["params"] = mp.make_paged_params(**both, **sizes)
         if back is not None:
-            s["back_params"] = mp.make_paged_params(**both, **back)
+            s["back_params"] = mp.make_paged_params(**both, **{**sizes, **back})
         s["ws"] = mp.alloc_paged_workspace(s["params"])
     return s
 
