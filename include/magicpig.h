@@ -404,6 +404,48 @@ MAGICPIG_API int magicpig_paged_attention_mxfp(const magicpig_paged_params* para
                                                 const int32_t* block_table, const int32_t* lengths, const int32_t* token_start, void* out,
                                                 float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- fewer keys: eviction by accumulated attention weight -------------------------------------------
+ * A server that may not keep every key of a long request keeps those that attention has looked at most, with the first and the last
+ * ones.  `weights` holds an account per slot and KV head, [n_pages, n_kv_heads, page_size] float32 beside the pools (of any kv_dtype):
+ * magicpig_page_weights adds what a step's tokens weighed each key with, as often as the server likes (every step, every few, or once
+ * with the last tokens of a prompt), magicpig_page_keep chooses the keys that stay, for each KV head its own, and magicpig_page_evict moves them to the
+ * front of the request's pages and hands back the pages behind.  The request goes on with the lengths that are left; its keys keep their order,
+ * so that n_sink and n_local count the keys that are left.  All three read lengths from device memory.
+ *
+ * magicpig_page_weights: with the step's tokens, positions and sets A as in magicpig_paged_attention, and lse [max_tokens, n_q_heads] what that call
+ * gave for them, for every key i of request b and KV head g
+ *   weights(i, g) = (i < counted[b] ? weights(i, g) : 0) + sum over tokens and query heads h of g with i in A: exp(scale q.k_i - lse);
+ * counted [batch] int32: so many of the request's keys have an account (clamped to [0, lengths[b]]); NULL: all but the new tokens' own.
+ * A row whose lse is -inf adds nothing.  k_scale as in magicpig_paged_attention (e4m3), k_block_scales with kv_dtype MAGICPIG_KV_MXFP4;
+ * NULL otherwise.  Accounts of keys that no token attends may be written with their own value.  Sums are taken in an order that depends on the
+ * parameters and lengths alone.  MAGICPIG_UNSUPPORTED where batch * n_kv_heads * max_pages * page_size is 2^35 (float32: 2^34) or more. */
+MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, const void* q, const void* k_pages, const float* k_scale,
+                                       const uint8_t* k_block_scales, const int32_t* block_table, const int32_t* lengths,
+                                       const int32_t* token_start, const float* lse, const int32_t* counted, float* weights,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Request b is left with stay = min(lengths[b], budgets[b], max_keep) keys, or stays as it is where budgets[b] < 0 or lengths[b] <= min(budgets[b], max_keep).
+ * kept [batch, n_kv_heads, max_keep] int32 gets, in ascending order, the keys of each head that stay, and -1 behind them (in all
+ * entries of a request that stays as it is): the first n_first keys and the last n_last, then those of the largest accounts; of equal ones (both zeros are) the first; an
+ * account that is NaN, or lies on a page that is none, comes below all others.  Where the first and the last are more than stay, the first stay of them.
+ * lengths_out [batch] int32 gets stay, or the length. */
+MAGICPIG_API int magicpig_page_keep(const magicpig_paged_params* params, const float* weights, const int32_t* block_table,
+                                    const int32_t* lengths, const int32_t* budgets, int32_t n_first, int32_t n_last, int32_t max_keep,
+                                    int32_t* kept, int32_t* lengths_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* For every request with lengths_kept[b] < lengths[b]: the rows of keys and values of KV head g, their block scales (MAGICPIG_KV_MXFP4) and
+ * their accounts (weights, or NULL) move from key kept[b, g, j] to key j, for j < lengths_kept[b], in place; kept ascends, as
+ * magicpig_page_keep leaves it (an entry that does not lie in [j, lengths[b]) moves nothing), or is NULL: the first keys stay and nothing moves,
+ * as when drafted tokens are rejected.  Then the pages behind the keys that stay, ceil(lengths_kept[b] / page_size) .. ceil(lengths[b] / page_size) - 1 of the
+ * request, are laid on the stack of free pages, requests in order, pages in order, and n_free_out [1] int32 (may be `n_free`) gets its height; the
+ * block table stays as it is.  status [1] int32 gets 0, or -1 if an argument does not fit (a length below 0 or beyond the table's
+ * row, lengths_kept above lengths or, with kept, above max_keep, a stack beyond n_pages): then nothing moves and nothing is handed back.  Pages
+ * that two requests share are not to be evicted from. */
+MAGICPIG_API int magicpig_page_evict(const magicpig_paged_params* params, const int32_t* kept, int32_t max_keep, const int32_t* lengths,
+                                     const int32_t* lengths_kept, const int32_t* block_table, int32_t* free_pages, const int32_t* n_free,
+                                     void* k_pages, void* v_pages, uint8_t* k_block_scales, uint8_t* v_block_scales, float* weights,
+                                     int32_t* n_free_out, int32_t* status, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Profiling aid, and the only setting the library keeps: a per-thread (thread_local) list of
  * events, empty unless this function was called on the calling host thread; production callers
  * never call it and pay one thread-local test per call.  When `events` is non-NULL it points to

@@ -67,6 +67,7 @@ EXPORTS = (
     "magicpig_prepare_centering", "magicpig_hash_query_prepared", "magicpig_hash_decode_step_prepared",
     "magicpig_paged_workspace_bytes", "magicpig_page_plan", "magicpig_page_append", "magicpig_paged_attention",
     "magicpig_page_append_mxfp", "magicpig_page_read_mxfp", "magicpig_paged_attention_mxfp",
+    "magicpig_page_weights", "magicpig_page_keep", "magicpig_page_evict",
 )
 
 _lib = None
@@ -127,6 +128,12 @@ def lib() -> ctypes.CDLL:
     L.magicpig_page_read_mxfp.argtypes = [PP] + [vp] * 8
     L.magicpig_paged_attention_mxfp.restype = ctypes.c_int
     L.magicpig_paged_attention_mxfp.argtypes = [PP] + [vp] * 11 + [sz, vp]
+    L.magicpig_page_weights.restype = ctypes.c_int
+    L.magicpig_page_weights.argtypes = [PP] + [vp] * 11 + [sz, vp]
+    L.magicpig_page_keep.restype = ctypes.c_int
+    L.magicpig_page_keep.argtypes = [PP] + [vp] * 4 + [i32] * 3 + [vp] * 3 + [sz, vp]
+    L.magicpig_page_evict.restype = ctypes.c_int
+    L.magicpig_page_evict.argtypes = [PP, vp, i32] + [vp] * 13 + [sz, vp]
     L.magicpig_status_string.restype, L.magicpig_status_string.argtypes = ctypes.c_char_p, [ctypes.c_int]
     L.magicpig_last_hip_error.restype, L.magicpig_last_hip_error.argtypes = ctypes.c_char_p, []
     L.magicpig_profile_stage_events.restype = None
@@ -344,6 +351,7 @@ class _PagedSizes:
         self.q = reach((p.q_stride_token, p.max_tokens), (p.q_stride_head, p.n_q_heads))
         self.k_new = reach((p.k_new_stride_token, p.max_tokens), (p.k_new_stride_head, p.n_kv_heads))
         self.v_new = reach((p.v_new_stride_token, p.max_tokens), (p.v_new_stride_head, p.n_kv_heads))
+        self.weights = p.n_pages * p.n_kv_heads * p.page_size
         self.lse = p.max_tokens * p.n_q_heads
         self.out = self.lse * p.head_dim
 
@@ -533,6 +541,86 @@ def magicpig_paged_attention_mxfp(params, q, k_pages, v_pages, k_block_scales, v
     _paged_call(device, lib().magicpig_paged_attention_mxfp, ctypes.byref(params), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
                 k_block_scales.data_ptr(), v_block_scales.data_ptr(), block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start),
                 out.data_ptr(), _ptr(lse), _ptr(workspace), _nbytes(workspace))
+
+
+def _block(t, device, s, elements) -> bool:
+    """Whether block scales are there exactly where the pools are in four bits."""
+    return _strided(t, device, _SCALES, elements) if s.four else t is None
+
+
+def _refuse_block(s, **tensors):
+    for name, t in tensors.items():
+        if t is not None and not s.four:
+            raise MagicpigError(f"{name} belongs to pools of kv_dtype MAGICPIG_KV_MXFP4")
+
+
+def magicpig_page_weights(params, q, k_pages, k_scale, k_block_scales, block_table, lengths, token_start, lse, counted, weights,
+                          workspace=None) -> None:
+    s, device, i32, f32 = _paged_sizes(params), _paged_device(q, workspace), torch.int32, torch.float32
+    try:
+        fits = (_strided(q, device, (s.dtype,), s.q) and _strided(k_pages, device, s.pool_dtype, s.k_pages)
+                and _block(k_block_scales, device, s, s.four and s.k_block) and _dense(block_table, device, i32, s.table)
+                and _dense(lengths, device, i32, s.batch) and (token_start is None or _dense(token_start, device, i32, s.batch + 1))
+                and _dense(lse, device, f32, s.lse) and (counted is None or _dense(counted, device, i32, s.batch))
+                and _dense(weights, device, f32, s.weights) and (k_scale is None or _dense(k_scale, device, f32, s.heads)))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse_block(s, k_block_scales=k_block_scales)
+        _refuse(device, q=(q, (s.dtype,), s.q, False, False), k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False),
+                k_scale=(k_scale, (f32,), s.heads, True, True), k_block_scales=(k_block_scales, _SCALES, s.four and s.k_block, False, not s.four),
+                block_table=(block_table, (i32,), s.table, True, False), lengths=(lengths, (i32,), s.batch, True, False),
+                token_start=(token_start, (i32,), s.batch + 1, True, True), lse=(lse, (f32,), s.lse, True, False),
+                counted=(counted, (i32,), s.batch, True, True), weights=(weights, (f32,), s.weights, True, False))
+    _paged_call(device, lib().magicpig_page_weights, ctypes.byref(params), q.data_ptr(), k_pages.data_ptr(), _ptr(k_scale), _ptr(k_block_scales),
+                block_table.data_ptr(), lengths.data_ptr(), _ptr(token_start), lse.data_ptr(), _ptr(counted), weights.data_ptr(), _ptr(workspace),
+                _nbytes(workspace))
+
+
+def magicpig_page_keep(params, weights, block_table, lengths, budgets, n_first, n_last, kept, lengths_out, workspace=None) -> None:
+    """max_keep is the last dimension of `kept`, [batch, n_kv_heads, max_keep]."""
+    s, device, i32, f32 = _paged_sizes(params), _paged_device(weights, workspace), torch.int32, torch.float32
+    try:
+        most = kept.shape[-1]
+        fits = (_dense(weights, device, f32, s.weights) and _dense(block_table, device, i32, s.table) and _dense(lengths, device, i32, s.batch)
+                and _dense(budgets, device, i32, s.batch) and _dense(kept, device, i32, s.batch * s.heads * most)
+                and _dense(lengths_out, device, i32, s.batch))
+    except (AttributeError, IndexError):
+        most, fits = 1, False
+    if not fits:
+        _refuse(device, weights=(weights, (f32,), s.weights, True, False), block_table=(block_table, (i32,), s.table, True, False),
+                lengths=(lengths, (i32,), s.batch, True, False), budgets=(budgets, (i32,), s.batch, True, False),
+                kept=(kept, (i32,), s.batch * s.heads * most, True, False), lengths_out=(lengths_out, (i32,), s.batch, True, False))
+    _paged_call(device, lib().magicpig_page_keep, ctypes.byref(params), weights.data_ptr(), block_table.data_ptr(), lengths.data_ptr(),
+                budgets.data_ptr(), n_first, n_last, most, kept.data_ptr(), lengths_out.data_ptr(), _ptr(workspace), _nbytes(workspace))
+
+
+def magicpig_page_evict(params, kept, lengths, lengths_kept, block_table, free_pages, n_free, k_pages, v_pages, k_block_scales, v_block_scales,
+                        weights, n_free_out, status, workspace=None) -> None:
+    """max_keep is the last dimension of `kept`, [batch, n_kv_heads, max_keep]; kept and weights may be None."""
+    s, device, i32, f32 = _paged_sizes(params), _paged_device(k_pages, workspace), torch.int32, torch.float32
+    try:
+        most = 0 if kept is None else kept.shape[-1]
+        fits = ((kept is None or _dense(kept, device, i32, s.batch * s.heads * most)) and _dense(lengths, device, i32, s.batch)
+                and _dense(lengths_kept, device, i32, s.batch) and _dense(block_table, device, i32, s.table)
+                and _dense(free_pages, device, i32, s.n_pages) and _dense(n_free, device, i32, 1) and _strided(k_pages, device, s.pool_dtype, s.k_pages)
+                and _strided(v_pages, device, s.pool_dtype, s.v_pages) and _block(k_block_scales, device, s, s.four and s.k_block)
+                and _block(v_block_scales, device, s, s.four and s.v_block) and (weights is None or _dense(weights, device, f32, s.weights))
+                and _dense(n_free_out, device, i32, 1) and _dense(status, device, i32, 1))
+    except (AttributeError, IndexError):
+        most, fits = 1, False
+    if not fits:
+        _refuse_block(s, k_block_scales=k_block_scales, v_block_scales=v_block_scales)
+        of = lambda t, count: (t, (i32,), count, True, False)
+        _refuse(device, kept=(kept, (i32,), s.batch * s.heads * most, True, True), lengths=of(lengths, s.batch), lengths_kept=of(lengths_kept, s.batch),
+                block_table=of(block_table, s.table), free_pages=of(free_pages, s.n_pages), n_free=of(n_free, 1),
+                k_pages=(k_pages, s.pool_dtype, s.k_pages, False, False), v_pages=(v_pages, s.pool_dtype, s.v_pages, False, False),
+                k_block_scales=(k_block_scales, _SCALES, s.four and s.k_block, False, not s.four),
+                v_block_scales=(v_block_scales, _SCALES, s.four and s.v_block, False, not s.four),
+                weights=(weights, (f32,), s.weights, True, True), n_free_out=of(n_free_out, 1), status=of(status, 1))
+    _paged_call(device, lib().magicpig_page_evict, ctypes.byref(params), _ptr(kept), most, lengths.data_ptr(), lengths_kept.data_ptr(),
+                block_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_block_scales),
+                _ptr(v_block_scales), _ptr(weights), n_free_out.data_ptr(), status.data_ptr(), _ptr(workspace), _nbytes(workspace))
 
 
 # ---- buffer helpers (allocation and layout only) ---------------------------------------------

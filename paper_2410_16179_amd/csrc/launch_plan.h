@@ -188,6 +188,29 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   return f;
 }
 
+// ---- accounts of attention weight -------------------------------------------------------------------
+// rows: query rows of a KV head (new tokens times query heads) that a wavefront has at once: 16, 32, or 128 (more than 32: the wavefronts of a workgroup
+// split them); heads: KV heads that a workgroup takes at once (16 or 32 rows); workgroups: resident ones at most.
+struct WeightsForm {
+  int rows, heads;
+  int64_t tiles, workgroups;
+};
+inline int weights_tile(bool fp32, int bits) { return fp32 ? 16 : (bits == 16 ? 32 : 64); }
+inline WeightsForm weights_form(int batch, int kv_heads, int group, bool fp32, int bits, int max_new, int64_t max_len) {
+  WeightsForm f{};
+  const int64_t rows = (int64_t)max_new * group;
+  f.rows = rows <= 16 ? 16 : (rows <= 32 && !fp32 ? 32 : 128);
+  f.heads = 1;
+  while (f.heads < 8 && kv_heads % (2 * f.heads) == 0) f.heads *= 2;
+  const int tile = weights_tile(fp32, bits);
+  f.tiles = (max_len + tile - 1) / tile * batch * kv_heads;   // at most
+  const int64_t most = 2 * kNumCU;
+  f.workgroups = f.tiles < most ? (f.tiles > 0 ? f.tiles : 1) : most;
+  return f;
+}
+// Tiles are counted in 31 bits.
+inline bool weights_fit(const WeightsForm& f) { return f.tiles <= INT32_MAX - 1024; }
+
 // Whether the form's workgroups make a grid: its threads are counted in 32 bits (those of few rows are a thousand workgroups or a few).
 constexpr int kPagedManyThreads = 256;
 inline bool paged_grid_fits(const PagedForm& f) { return f.rows != kPagedManyRows || f.pieces * kPagedManyThreads < (int64_t)1 << 32; }

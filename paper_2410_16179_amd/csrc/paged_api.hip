@@ -248,4 +248,101 @@ int magicpig_page_read_mxfp(const Params* p, const void* k_pages, const void* v_
                                                    reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
+namespace {
+
+mp::WeightsForm weights_form_of(const Params* p, bool starts) {
+  return mp::weights_form(p->batch, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->dtype == MAGICPIG_FP32,
+                          four(p) ? 4 : (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? 8 : 16), starts ? most_new(p) : 1, (int64_t)p->max_pages * p->page_size);
+}
+
+}  // namespace
+
+int magicpig_page_weights(const Params* p, const void* q, const void* k_pages, const float* k_scale, const uint8_t* k_block_scales,
+                          const int32_t* block_table, const int32_t* lengths, const int32_t* token_start, const float* lse,
+                          const int32_t* counted, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int st = check(p);
+  if (st != MAGICPIG_OK) return st;
+  if ((st = check_pool(p, p->k_stride_page, p->k_stride_key, p->k_stride_head)) != MAGICPIG_OK) return st;
+  if ((st = check_rows(p->q_stride_token, p->q_stride_head)) != MAGICPIG_OK) return st;
+  if (!token_start && p->max_tokens < p->batch) return MAGICPIG_INVALID_ARG;
+  if (!q || !k_pages || !lse || !weights || (p->batch > 0 && (!block_table || !lengths))) return MAGICPIG_INVALID_ARG;
+  if (k_scale && p->kv_dtype != MAGICPIG_KV_FP8_E4M3) return MAGICPIG_INVALID_ARG;
+  if (four(p) ? !k_block_scales : k_block_scales != nullptr) return MAGICPIG_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned(k_scale, 4) || !aligned(k_block_scales, 4) || !aligned(block_table, 4) ||
+      !aligned(lengths, 4) || !aligned(token_start, 4) || !aligned(lse, 4) || !aligned(counted, 4) || !aligned(weights, 4) || !aligned16(workspace))
+    return MAGICPIG_INVALID_ARG;
+  const mp::WeightsForm f = weights_form_of(p, token_start != nullptr);
+  if (!mp::weights_fit(f)) return MAGICPIG_UNSUPPORTED;
+  (void)workspace_bytes;
+  if (p->batch == 0) return MAGICPIG_OK;
+  mp::PageWeightsArgs a{};
+  a.paged.q = q; a.paged.k = k_pages; a.paged.k_scale = k_scale; a.paged.k_block = k_block_scales;
+  a.paged.table = block_table; a.paged.lengths = lengths; a.paged.token_start = token_start;
+  a.paged.batch = p->batch; a.paged.Hq = p->n_q_heads; a.paged.Hkv = p->n_kv_heads; a.paged.G = p->n_q_heads / p->n_kv_heads;
+  a.paged.page_shift = __builtin_ctz(p->page_size); a.paged.max_pages = p->max_pages; a.paged.max_new = token_start ? most_new(p) : 1;
+  a.paged.n_sink = p->n_sink; a.paged.n_local = p->n_local;
+  a.paged.max_len = p->max_pages * p->page_size; a.paged.max_tokens = (int)p->max_tokens; a.paged.n_pages = (int)p->n_pages;
+  a.paged.scale_log2 = (p->scale == 0.f ? 0.08838834764831845f : p->scale) * kLog2e;
+  a.paged.k_page = p->k_stride_page; a.paged.k_key = p->k_stride_key; a.paged.k_head = p->k_stride_head;
+  a.paged.q_t = p->q_stride_token; a.paged.q_h = p->q_stride_head;
+  a.lse = lse; a.counted = counted; a.weights = weights; a.heads = f.heads;
+  const int element = four(p) ? mp::kFP4 : (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? mp::kFP8 : (p->dtype == MAGICPIG_FP32 ? mp::kFP32 : mp::kBF16));
+  return mp::hip_status(mp::launch_page_weights(a, element, f, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+int magicpig_page_keep(const Params* p, const float* weights, const int32_t* block_table, const int32_t* lengths, const int32_t* budgets,
+                       int32_t n_first, int32_t n_last, int32_t max_keep, int32_t* kept, int32_t* lengths_out, void* workspace,
+                       size_t workspace_bytes, void* hip_stream) {
+  const int st = check(p);
+  if (st != MAGICPIG_OK) return st;
+  if (n_first < 0 || n_last < 0 || max_keep < 1) return MAGICPIG_INVALID_ARG;
+  if ((int64_t)p->batch * p->n_kv_heads * 1024 >= (int64_t)1 << 32) return MAGICPIG_UNSUPPORTED;   // (threads of a grid)
+  if (p->batch > 0 && (!weights || !block_table || !lengths || !budgets || !kept || !lengths_out)) return MAGICPIG_INVALID_ARG;
+  if (!aligned16(weights) || !aligned(block_table, 4) || !aligned(lengths, 4) || !aligned(budgets, 4) || !aligned(kept, 4) ||
+      !aligned(lengths_out, 4) || !aligned16(workspace))
+    return MAGICPIG_INVALID_ARG;
+  (void)workspace_bytes;
+  if (p->batch == 0) return MAGICPIG_OK;
+  mp::PageKeepArgs a{};
+  a.weights = weights; a.table = block_table; a.lengths = lengths; a.budgets = budgets; a.kept = kept; a.lengths_out = lengths_out;
+  a.batch = p->batch; a.heads = p->n_kv_heads; a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages;
+  a.max_len = p->max_pages * p->page_size; a.n_pages = (int)p->n_pages; a.n_first = n_first; a.n_last = n_last; a.max_keep = max_keep;
+  return mp::hip_status(mp::launch_page_keep(a, (int64_t)p->batch * p->n_kv_heads, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+int magicpig_page_evict(const Params* p, const int32_t* kept, int32_t max_keep, const int32_t* lengths, const int32_t* lengths_kept,
+                        const int32_t* block_table, int32_t* free_pages, const int32_t* n_free, void* k_pages, void* v_pages,
+                        uint8_t* k_block_scales, uint8_t* v_block_scales, float* weights, int32_t* n_free_out, int32_t* status,
+                        void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int st = check(p);
+  if (st != MAGICPIG_OK) return st;
+  if ((st = check_pools(p)) != MAGICPIG_OK) return st;
+  if (kept && max_keep < 1) return MAGICPIG_INVALID_ARG;
+  if (!free_pages || !n_free || !n_free_out || !status || !k_pages || !v_pages) return MAGICPIG_INVALID_ARG;
+  if (p->batch > 0 && (!lengths || !lengths_kept || !block_table)) return MAGICPIG_INVALID_ARG;
+  if (four(p) ? !k_block_scales || !v_block_scales : k_block_scales || v_block_scales) return MAGICPIG_INVALID_ARG;
+  if (!aligned(kept, 4) || !aligned(lengths, 4) || !aligned(lengths_kept, 4) || !aligned(block_table, 4) || !aligned(free_pages, 4) ||
+      !aligned(n_free, 4) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned(k_block_scales, 4) || !aligned(v_block_scales, 4) ||
+      !aligned(weights, 4) || !aligned(n_free_out, 4) || !aligned(status, 4) || !aligned16(workspace))
+    return MAGICPIG_INVALID_ARG;
+  (void)workspace_bytes;
+  mp::PageEvictArgs a{};
+  a.kept = kept; a.lengths = lengths; a.stay = lengths_kept; a.table = block_table; a.free_pages = free_pages; a.n_free = n_free;
+  a.n_free_out = n_free_out; a.status = status;
+  a.batch = p->batch; a.heads = p->n_kv_heads; a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages;
+  a.max_len = p->max_pages * p->page_size; a.max_keep = max_keep; a.n_pages = p->n_pages;
+  const int row = (int)row_bytes(p, mp::kHeadDim), slice = row < 128 ? row : 128;
+  auto array = [](void* at, int64_t page, int64_t key, int64_t head, int slice, int slices) {
+    return mp::PagedArray{static_cast<char*>(at), page, key, head, slice, slices};
+  };
+  a.arrays[0] = array(k_pages, row_bytes(p, p->k_stride_page), row_bytes(p, p->k_stride_key), row_bytes(p, p->k_stride_head), slice, row / slice);
+  a.arrays[1] = array(v_pages, row_bytes(p, p->v_stride_page), row_bytes(p, p->v_stride_key), row_bytes(p, p->v_stride_head), slice, row / slice);
+  if (weights) a.arrays[2] = array(weights, (int64_t)p->n_kv_heads * p->page_size * 4, 4, (int64_t)p->page_size * 4, 4, 1);
+  if (four(p)) {
+    a.arrays[3] = array(k_block_scales, p->k_stride_page / 32, p->k_stride_key / 32, p->k_stride_head / 32, 4, 1);
+    a.arrays[4] = array(v_block_scales, p->v_stride_page / 32, p->v_stride_key / 32, p->v_stride_head / 32, 4, 1);
+  }
+  return mp::hip_status(mp::launch_page_evict(a, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
 }  // extern "C"

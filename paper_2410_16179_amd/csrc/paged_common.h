@@ -62,6 +62,35 @@ struct PagedArgs {
   const uint8_t* k_block; const uint8_t* v_block;         // scales of pools in four bits: strides are those of the elements / 32
 };
 
+// Accounts of attention weight (page_weights.hip).
+struct PageWeightsArgs {
+  PagedArgs paged;
+  const float* lse; const int* counted; float* weights;
+  int heads;              // KV heads that a workgroup takes at once
+};
+
+// Which keys stay (page_keep.hip).
+struct PageKeepArgs {
+  const float* weights; const int* table; const int* lengths; const int* budgets;
+  int* kept; int* lengths_out;
+  int batch, heads, page_shift, max_pages, max_len, n_pages, n_first, n_last, max_keep;
+};
+
+// Eviction (page_evict.hip).  An array of rows in the pages: strides in bytes; a row is `slices` slices of `slice` bytes.
+struct PagedArray {
+  char* at;
+  int64_t page, key, head;
+  int slice, slices;
+};
+constexpr int kEvictArrays = 5;
+struct PageEvictArgs {
+  const int* kept; const int* lengths; const int* stay; const int* table; int* free_pages; const int* n_free;
+  int* n_free_out; int* status;
+  int batch, heads, page_shift, max_pages, max_len, max_keep;
+  int64_t n_pages;
+  PagedArray arrays[kEvictArrays];
+};
+
 struct PagedRequest {
   int len, tokens, row;   // keys, new tokens, row of the first one
 };
@@ -440,6 +469,9 @@ hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s);
 hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s);
 hipError_t launch_page_append_mxfp4(const PageMxfp4Args& a, hipStream_t s);
 hipError_t launch_page_read_mxfp4(const PageMxfp4Args& a, hipStream_t s);
+hipError_t launch_page_weights(const PageWeightsArgs& a, int element, const WeightsForm& form, hipStream_t s);
+hipError_t launch_page_keep(const PageKeepArgs& a, int64_t rows, hipStream_t s);
+hipError_t launch_page_evict(const PageEvictArgs& a, hipStream_t s);
 void launch_paged_many_rows(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s);
 hipError_t launch_paged_attention(const PagedArgs& a, int element, const PagedForm& form, hipStream_t s);
 
