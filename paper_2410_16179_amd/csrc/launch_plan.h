@@ -1,5 +1,6 @@
 // Rules by which the launchers choose a form from the sizes alone, host code without the HIP runtime.
 #pragma once
+#include <cstddef>
 #include <cstdint>
 
 namespace mp {
@@ -188,23 +189,50 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   return f;
 }
 
+// ---- which keys stay --------------------------------------------------------------------------------
+constexpr int kKeepShort = 16384;            // requests of up to so many keys are gone over by 512 threads, others by 1024
+// Workgroups to a KV head: one, or where few heads leave compute units idle one for each 8192 keys that a request may have, up to 16.
+constexpr int kKeepMostParts = 16;
+constexpr int kKeepPartList = 2048;          // ranks that one lists
+constexpr size_t kKeepPartBytes = 2 * 2048 + 4 * kKeepPartList + 16;
+inline int keep_parts(int64_t rows, int64_t max_len) {
+  const int64_t parts = (max_len + 8191) / 8192;
+  if (parts < 4 || rows > 32 || max_len > kKeepMostParts * 65280) return 1;   // (a part's counts have 16 bits)
+  return (int)(parts < kKeepMostParts ? parts : kKeepMostParts);
+}
+
+// ---- eviction ---------------------------------------------------------------------------------------
+// Bytes of a row that a workgroup moves: whole rows, or pieces of 64 bytes at least where requests times KV heads would leave compute units idle.
+inline int evict_slice(int row, int64_t units) {
+  int slice = row;
+  while (slice > 64 && 2 * units * (row / slice) < kNumCU) slice /= 2;
+  return slice;
+}
+
 // ---- accounts of attention weight -------------------------------------------------------------------
-// rows: query rows of a KV head (new tokens times query heads) that a wavefront has at once: 16, 32, or 128 (more than 32: the wavefronts of a workgroup
-// split them); heads: KV heads that a workgroup takes at once (16 or 32 rows); workgroups: resident ones at most.
+// rows: query rows of a KV head (new tokens times query heads) that a wavefront has at once: 16, 32, or 128, more of which come by one tile after the other;
+// heads: 16 or 32 rows: KV heads that a workgroup's eight wavefronts take at once; 128: the shares that they split the rows into; tiles: of keys, at most,
+// all KV heads together; workgroups: 16 or 32 rows: what is resident at once.
 struct WeightsForm {
   int rows, heads;
   int64_t tiles, workgroups;
 };
-inline int weights_tile(bool fp32, int bits) { return fp32 ? 16 : (bits == 16 ? 32 : 64); }
 inline WeightsForm weights_form(int batch, int kv_heads, int group, bool fp32, int bits, int max_new, int64_t max_len) {
   WeightsForm f{};
   const int64_t rows = (int64_t)max_new * group;
   f.rows = rows <= 16 ? 16 : (rows <= 32 && !fp32 ? 32 : 128);
   f.heads = 1;
-  while (f.heads < 8 && kv_heads % (2 * f.heads) == 0) f.heads *= 2;
-  const int tile = weights_tile(fp32, bits);
-  f.tiles = (max_len + tile - 1) / tile * batch * kv_heads;   // at most
-  const int64_t most = 2 * kNumCU;
+  int tile = fp32 ? 16 : (bits == 16 ? 32 : 64);
+  int64_t most = 2 * kNumCU;
+  if (f.rows < 128) {
+    while (f.heads < 8 && kv_heads % (2 * f.heads) == 0) f.heads *= 2;
+  } else {
+    // (a share of two tiles of sixteen rows at least)
+    while (f.heads < 8 && 64 * f.heads <= rows) f.heads *= 2;
+    tile = (fp32 ? 32 : 64) * (8 / f.heads);
+    most = 1 << 14;
+  }
+  f.tiles = (max_len + tile - 1) / tile * batch * kv_heads;
   f.workgroups = f.tiles < most ? (f.tiles > 0 ? f.tiles : 1) : most;
   return f;
 }

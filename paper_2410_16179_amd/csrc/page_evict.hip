@@ -4,37 +4,41 @@
 namespace mp {
 namespace {
 
-constexpr int kThreads = 512, kUnroll = 4;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kUnroll = 8;
 
 __device__ inline int pages_of(int keys, int shift) { return (int)(((int64_t)keys + (1 << shift) - 1) >> shift); }
 
-// One workgroup: what is asked for is looked at, and the pages behind the keys that stay are laid on the stack, requests in order, pages in order.
-constexpr int kBookThreads = 1024;
-__global__ __launch_bounds__(kBookThreads) void page_evict_book_kernel(const PageEvictArgs a) {
-  __shared__ int64_t total;
-  __shared__ int wrong, wave_total[kBookThreads / 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (threadIdx.x == 0) { total = 0; wrong = 0; }
-  __syncthreads();
-  const int n_free = *a.n_free;
+// Whether the arguments fit, by one workgroup; pages: those that go back.
+__device__ inline bool all_fits(const PageEvictArgs& a, int n_free, int64_t& pages) {
+  __shared__ int64_t sums[kWaves];
   int64_t sum = 0;
   bool bad = false;
-  for (int b = threadIdx.x; b < a.batch; b += kBookThreads) {
+  for (int b = threadIdx.x; b < a.batch; b += kThreads) {
     const int len = a.lengths[b], stay = a.stay[b];
-    bad = bad || len < 0 || len > a.max_len || stay < 0 || stay > len || (a.kept && stay < len && stay > a.max_keep);
-    if (!bad) sum += pages_of(len, a.page_shift) - pages_of(stay, a.page_shift);
+    const bool fits = len >= 0 && len <= a.max_len && stay >= 0 && stay <= len && !(a.kept && stay < len && stay > a.max_keep);
+    bad = bad || !fits;
+    if (fits) sum += pages_of(len, a.page_shift) - pages_of(stay, a.page_shift);
   }
-  if (bad) atomicOr(&wrong, 1);
-  atomicAdd(reinterpret_cast<unsigned long long*>(&total), (unsigned long long)sum);
-  __syncthreads();
-  const bool fine = !wrong && n_free >= 0 && n_free + total <= a.n_pages;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  bad = __syncthreads_or(bad);
+  pages = 0;
+  for (int w = 0; w < kWaves; ++w) pages += sums[w];
+  return !bad && n_free >= 0 && n_free + pages <= a.n_pages;
+}
+
+// The pages behind the keys that stay are laid on the stack, requests in order, pages in order.
+__device__ inline void give_back(const PageEvictArgs& a, int n_free, bool fits, int64_t pages) {
+  __shared__ int wave_total[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) {
-    *a.status = fine ? 0 : -1;
-    *a.n_free_out = fine ? n_free + (int)total : n_free;
+    *a.status = fits ? 0 : -1;
+    *a.n_free_out = fits ? n_free + (int)pages : n_free;
   }
-  if (!fine) return;
+  if (!fits) return;
   int top = n_free;
-  for (int b0 = 0; b0 < a.batch; b0 += kBookThreads) {
+  for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
     const int b = b0 + threadIdx.x;
     int first = 0, count = 0;
     if (b < a.batch) {
@@ -46,11 +50,17 @@ __global__ __launch_bounds__(kBookThreads) void page_evict_book_kernel(const Pag
     if (lane == 63) wave_total[wave] = upto;
     __syncthreads();
     int at = top + upto - count;
-    for (int w = 0; w < kBookThreads / 64; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       at += w < wave ? wave_total[w] : 0;
       top += wave_total[w];
     }
-    for (int j = 0; j < count; ++j) a.free_pages[at + j] = a.table[(int64_t)b * a.max_pages + first + j];
+    // a wavefront's requests one after the other, their pages by its lanes
+    for (uint64_t todo = __ballot(count > 0); todo; todo &= todo - 1) {
+      const int f = __ffsll((unsigned long long)todo) - 1;
+      const int n = __builtin_amdgcn_readlane(count, f), to = __builtin_amdgcn_readlane(at, f);
+      const int* from = a.table + (int64_t)__builtin_amdgcn_readlane(b, f) * a.max_pages + __builtin_amdgcn_readlane(first, f);
+      for (int j = lane; j < n; j += 64) a.free_pages[to + j] = from[j];
+    }
   }
 }
 
@@ -80,45 +90,70 @@ __device__ inline void move_rows(const PageEvictArgs& a, const PagedArray& r, in
     hi = min(hi, lo + f * each);
     lo = low;
   }
+  // three steps in flight: a tile's list, its rows, its writing
   Part now[kUnroll], next[kUnroll];
-  auto fetch = [&](int j0, Part (&to)[kUnroll], bool (&there)[kUnroll]) {
+  int from[kUnroll];
+  auto list = [&](int j0) {
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
-      const int j = j0 + row0 + i * step, from = j < stay ? kept[j] : -1;
-      const char* src = from > j && from < len ? place(from) : nullptr;
-      there[i] = src != nullptr;
-      if (src) to[i] = *reinterpret_cast<const Part*>(src);
+      const int j = j0 + row0 + i * step;
+      from[i] = j < stay ? kept[j] : -1;
     }
   };
-  bool here[kUnroll], ahead[kUnroll];
+  auto fetch = [&](int j0, Part (&to)[kUnroll]) {
+    uint32_t there = 0;
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      const int j = j0 + row0 + i * step;
+      const char* src = from[i] > j && from[i] < len ? place(from[i]) : nullptr;
+      if (src) {
+        to[i] = *reinterpret_cast<const Part*>(src);
+        there |= 1u << i;
+      }
+    }
+    return there;
+  };
   int j0 = __builtin_amdgcn_readfirstlane(lo);
-  fetch(j0, now, here);
+  list(j0);
+  uint32_t here = fetch(j0, now);
+  list(j0 + tile);
 #pragma unroll 1
   for (; j0 < stay; j0 += tile) {
-    fetch(j0 + tile, next, ahead);
+    const uint32_t ahead = fetch(j0 + tile, next);
+    list(j0 + 2 * tile);
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) asm volatile("" : "+v"(now[i]));   // (read before the barrier)
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
-      char* to = here[i] ? place(j0 + row0 + i * step) : nullptr;
+      char* to = here >> i & 1 ? place(j0 + row0 + i * step) : nullptr;
       if (to) *reinterpret_cast<Part*>(to) = now[i];
       now[i] = next[i];
-      here[i] = ahead[i];
     }
+    here = ahead;
   }
 }
 
-__global__ __launch_bounds__(kThreads) void page_evict_move_kernel(const PageEvictArgs a) {
-  if (*a.status != 0) return;
-  const int64_t units = (int64_t)a.batch * a.heads;
-  int job = blockIdx.x, array = 0;
-  while (job >= a.arrays[array].slices) job -= a.arrays[array++].slices;
-  const PagedArray r = a.arrays[array];
+// Workgroups that move rows, and one that keeps the books, the first (`books` 1); each looks at the arguments for itself, so the stack's height must not
+// change meanwhile: where it is written in place the books come in a launch of their own (no job is left for the others).
+__global__ __launch_bounds__(kThreads) void page_evict_kernel(const PageEvictArgs a, int jobs, int books) {
+  const int n_free = *a.n_free;
+  int64_t pages;
+  const bool fits = all_fits(a, n_free, pages);
+  if (blockIdx.x < books) {
+    give_back(a, n_free, fits, pages);
+    return;
+  }
+  if (!fits) return;
+  const int64_t all = (int64_t)a.batch * a.heads * jobs;
 #pragma unroll 1
-  for (int64_t unit = blockIdx.y; unit < units; unit += gridDim.y) {
+  for (int64_t n = (int64_t)blockIdx.x - books; n < all; n += gridDim.x - books) {
+    const int64_t unit = n / jobs;
+    int job = (int)(n - unit * jobs), array = 0;
     const int b = (int)(unit / a.heads), g = (int)(unit - (int64_t)b * a.heads);
     if (a.stay[b] == a.lengths[b]) continue;
+    while (job >= a.arrays[array].slices) job -= a.arrays[array++].slices;
+    const PagedArray r = a.arrays[array];
     if (r.slice == 4) move_rows<uint32_t>(a, r, b, g, job);
     else move_rows<u32x4>(a, r, b, g, job);
   }
@@ -127,12 +162,14 @@ __global__ __launch_bounds__(kThreads) void page_evict_move_kernel(const PageEvi
 }  // namespace
 
 hipError_t launch_page_evict(const PageEvictArgs& a, hipStream_t s) {
-  page_evict_book_kernel<<<1, kBookThreads, 0, s>>>(a);
   int jobs = 0;
-  for (const PagedArray& r : a.arrays) jobs += r.slices;
-  const int64_t units = (int64_t)a.batch * a.heads;
-  if (a.kept && units > 0 && jobs > 0)
-    page_evict_move_kernel<<<dim3((unsigned)jobs, (unsigned)(units < 65535 ? units : 65535)), kThreads, 0, s>>>(a);
+  if (a.kept)
+    for (const PagedArray& r : a.arrays) jobs += r.slices;
+  const int64_t all = (int64_t)a.batch * a.heads * jobs, most = 65535;
+  const unsigned movers = (unsigned)(all < most ? all : most);
+  const bool in_place = a.n_free == a.n_free_out;
+  if (movers > 0) page_evict_kernel<<<movers + !in_place, kThreads, 0, s>>>(a, jobs, !in_place);
+  if (movers == 0 || in_place) page_evict_kernel<<<1, kThreads, 0, s>>>(a, 1, 1);
   return hipGetLastError();
 }
 

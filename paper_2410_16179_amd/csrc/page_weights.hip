@@ -1,6 +1,8 @@
 // What the step's attention weighs each cached key with, added to the key's account.
 #include "paged_device.h"
 
+#include <type_traits>
+
 namespace mp {
 namespace {
 
@@ -20,8 +22,7 @@ struct Tile {
 struct Reach {
   int len, tokens, row, counted, tiles, sink, skip;
 };
-template <int KT>
-__device__ inline Reach reach_of(const PageWeightsArgs& a, int b) {
+__device__ inline Reach reach_of(const PageWeightsArgs& a, int b, int KT) {
   const PagedRequest r = paged_request(a.paged, b);
   Reach x{r.len, r.tokens, r.row, 0, 0, 0, 0};
   const int old = r.len - r.tokens;                        // (below 0 where there are more new tokens than keys)
@@ -63,10 +64,10 @@ struct Keys {
 };
 
 // A tile's keys: on their way, and then as the A operand of S^T = K Q^T - lane (c, u) has elements 32 u .. 32 u + 31 of key c (float32: 16 u .. and 64 + 16 u ..).
-template <int ET>
+template <int ET, int H = Tile<ET>::kHalves>
 struct Operand {
-  u32x4 k[Tile<ET>::kHalves][Tile<ET>::kFrags];
-  uint32_t scale[ET == kFP4 ? Tile<ET>::kHalves : 1];
+  u32x4 k[H][Tile<ET>::kFrags];
+  uint32_t scale[ET == kFP4 ? H : 1];
 
   // `valid` of sixteen keys from `at` of page id on
   __device__ inline void request(const Keys<ET>& keys, const Place& p, int h, int id, int at, int valid) {
@@ -86,14 +87,17 @@ struct Operand {
   __device__ inline void arrange(const Place& p, char* lds) {
     if constexpr (ET == kFP4) {
 #pragma unroll
-      for (int h = 0; h < Tile<ET>::kHalves; ++h) *reinterpret_cast<u32x4*>(lds + 1024 * h + 16 * p.lane) = k[h][0];
-      in_order();
+      for (int h0 = 0; h0 < H; h0 += 4) {
 #pragma unroll
-      for (int h = 0; h < Tile<ET>::kHalves; ++h) k[h][0] = *reinterpret_cast<const u32x4*>(lds + 1024 * h + 64 * p.c + 16 * (p.u ^ p.quad));
-      in_order();
+        for (int h = h0; h < h0 + 4 && h < H; ++h) *reinterpret_cast<u32x4*>(lds + 1024 * (h - h0) + 16 * p.lane) = k[h][0];
+        in_order();
+#pragma unroll
+        for (int h = h0; h < h0 + 4 && h < H; ++h) k[h][0] = *reinterpret_cast<const u32x4*>(lds + 1024 * (h - h0) + 64 * p.c + 16 * (p.u ^ p.quad));
+        in_order();
+      }
     } else {
 #pragma unroll
-      for (int h = 0; h < Tile<ET>::kHalves; ++h) {
+      for (int h = 0; h < H; ++h) {
         if constexpr (ET == kFP8) join_halves(k[h][0], k[h][1], p.c & 2);
         else
 #pragma unroll
@@ -181,20 +185,19 @@ __device__ inline float sum_rows(float (&v)[N], const Place& p) {
 
 __device__ inline bool page_ok(const PagedArgs& a, int id) { return (uint32_t)id < (uint32_t)a.n_pages; }
 
-template <int ET>
-__device__ inline void tile_pages(const PagedArgs& a, const_i32_ptr table, int key0, int (&id)[Tile<ET>::kHalves]) {
+template <int H>
+__device__ inline void tile_pages(const PagedArgs& a, const_i32_ptr table, int key0, int (&id)[H]) {
 #pragma unroll
-  for (int h = 0; h < Tile<ET>::kHalves; ++h) {
+  for (int h = 0; h < H; ++h) {
     const int at = (key0 + 16 * h) >> a.page_shift;
     id[h] = table[at < a.max_pages ? at : a.max_pages - 1];
   }
 }
-template <int ET>
-__device__ inline void request_tile(const PagedArgs& a, const Keys<ET>& keys, const Place& p, int key0, int end, const int (&id)[Tile<ET>::kHalves],
-                                    Operand<ET>& k) {
+template <int ET, int H>
+__device__ inline void request_tile(const PagedArgs& a, const Keys<ET>& keys, const Place& p, int key0, int end, const int (&id)[H], Operand<ET, H>& k) {
   const int page_mask = (1 << a.page_shift) - 1;
 #pragma unroll
-  for (int h = 0; h < Tile<ET>::kHalves; ++h)
+  for (int h = 0; h < H; ++h)
     k.request(keys, p, h, id[h], (key0 + 16 * h) & page_mask, page_ok(a, id[h]) ? min(max(end - key0 - 16 * h, 0), 16) : 0);
 }
 // Where the account of the lane's key is, key 16 (v / 4) + 4 u + v % 4 of the tile for v = c % (4 halves); null where it has none, or another lane has it.
@@ -221,7 +224,7 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
   const Place p;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int at_once = kWaves / w.heads, head = wave % w.heads, place = wave / w.heads, sets = a.Hkv / w.heads;
-  auto groups_of = [&](int b) { return (reach_of<KT>(w, b).tiles + at_once - 1) / at_once * sets; };
+  auto groups_of = [&](int b) { return (reach_of(w, b, KT).tiles + at_once - 1) / at_once * sets; };
   int total = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) total += __builtin_amdgcn_readlane(wave_prefix(b0 + p.lane < a.batch ? groups_of(b0 + p.lane) : 0), 63);
   const int each = (total + gridDim.x - 1) / gridDim.x;
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
 #pragma unroll 1
   while (pos < end) {
     b = __builtin_amdgcn_readfirstlane(b);
-    const Reach x = reach_of<KT>(w, b);
+    const Reach x = reach_of(w, b, KT);
     const int groups = (x.tiles + at_once - 1) / at_once;
     if (groups * sets <= pos - base) {                     // (requests without tiles)
       base += groups * sets;
@@ -286,8 +289,8 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
     float old = 0.f;
     auto bring = [&](int v) {
       const int key0 = tile_key(v);
-      tile_pages<ET>(a, table, key0, id);
-      request_tile<ET>(a, keys, p, key0, x.len, id, k);
+      tile_pages<T::kHalves>(a, table, key0, id);
+      request_tile<ET, T::kHalves>(a, keys, p, key0, x.len, id, k);
       to_account = account<ET>(w, p, g, key0, x.len, id, key);
       old = to_account && key < x.counted ? *to_account : 0.f;
     };
@@ -336,24 +339,35 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
   }
 }
 
-// ---- many rows: the wavefronts of a workgroup share a tile and split the rows ----------------------------
+// ---- many rows: a wavefront has a tile of 64 keys and goes over its share of the rows ---------------------
+// The keys stay in registers as bf16 (float32: 32 keys as they are), the rows come by: 32 at a time, loaded with neighbouring lanes on neighbouring addresses and
+// handed over in the wavefront's part of LDS, the next ones on their way.  The wavefronts of a workgroup are `row_split` shares of the rows, of one tile or of several.
+template <int ET>
+struct Many {
+  static constexpr bool kF32 = ET == kFP32;
+  static constexpr int kHalves = kF32 ? 2 : 4, kKeys = 16 * kHalves, kFrags = q_frags(ET), kValues = 4 * kHalves;
+  static constexpr int kTiles = 2, kRows = 16 * kTiles;  // query rows that come by at once
+  static constexpr int kRowBytes = kF32 ? 512 : 256, kPerLoad = 1024 / kRowBytes, kLoads = kRows / kPerLoad;   // of a row; rows of a load of the wavefront
+};
+
 template <int ET>
 __global__ __launch_bounds__(kThreads, 2) void page_weights_many_kernel(const PageWeightsArgs w) {
-  using T = Tile<ET>;
-  constexpr int KT = T::kKeys;
-  __shared__ __align__(16) char lds[kWaves * 4096];
-  __shared__ float sums[kWaves][KT];
+  using M = Many<ET>;
+  __shared__ __align__(16) char lds[kWaves][M::kRows * M::kRowBytes];
+  __shared__ float sums[kWaves][M::kKeys];
   const PagedArgs& a = w.paged;
   const Place p;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row_split = w.heads, tile_of = wave / row_split, share = wave % row_split, block = kWaves / row_split * M::kKeys;
+  char* const mine = lds[wave];
 #pragma unroll 1
   for (int64_t index = blockIdx.x;; index += gridDim.x) {
-    // item: KV head, tile, request
+    // item: KV head, block of keys, request
     const int g = (int)(index % a.Hkv);
     int64_t rest = index / a.Hkv;
     int b = -1;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      const int n = b0 + p.lane < a.batch ? reach_of<KT>(w, b0 + p.lane).tiles : 0, upto = wave_prefix(n);
+      const int n = b0 + p.lane < a.batch ? reach_of(w, b0 + p.lane, block).tiles : 0, upto = wave_prefix(n);
       const uint64_t found = __ballot(upto > rest);
       if (found) {
         const int f = __ffsll((unsigned long long)found) - 1;
@@ -365,65 +379,182 @@ __global__ __launch_bounds__(kThreads, 2) void page_weights_many_kernel(const Pa
     }
     if (b < 0) return;
     b = __builtin_amdgcn_readfirstlane(b);
-    const Reach x = reach_of<KT>(w, b);
-    const int v = __builtin_amdgcn_readfirstlane((int)rest), key0 = (v < x.sink ? v : v + x.skip) * KT;
+    const Reach x = reach_of(w, b, block);
+    const int v = __builtin_amdgcn_readfirstlane((int)rest), block0 = (v < x.sink ? v : v + x.skip) * block, key0 = block0 + tile_of * M::kKeys;
     const float to_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[g] : 1.f);
     const const_i32_ptr table = (const_i32_ptr)(a.table + (int64_t)b * a.max_pages);
-    int id[T::kHalves];
-    tile_pages<ET>(a, table, key0, id);
-    Operand<ET> k;
-    request_tile<ET>(a, Keys<ET>(a, g), p, key0, x.len, id, k);
-    k.arrange(p, lds + 4096 * wave);
+    u32x4 k[M::kHalves][M::kFrags];
+    {
+      const Keys<ET> keys(a, g);
+      Operand<ET, M::kHalves> raw;
+      int id[M::kHalves];
+      tile_pages<M::kHalves>(a, table, key0, id);
+      request_tile<ET, M::kHalves>(a, keys, p, key0, x.len, id, raw);
+      raw.arrange(p, mine);
+#pragma unroll
+      for (int h = 0; h < M::kHalves; ++h)
+#pragma unroll
+        for (int i = 0; i < M::kFrags; ++i) {
+          if constexpr (M::kF32) k[h][i] = raw.k[h][i];
+          else k[h][i] = raw.bf16(h, i);
+        }
+    }
     // rows of tokens that attend a key of the tile: from the first one at or behind its first key, to the last one whose window has its last key
-    const int old = x.len - x.tokens;
-    const int t_begin = max(key0 - old, 0);
+    const int old = x.len - x.tokens, rows = x.tokens * a.G;
     int t_end = x.tokens;
-    if (a.n_local > 0 && key0 >= a.n_sink) t_end = (int)min((int64_t)t_end, (int64_t)key0 + KT - 1 + a.n_local - old);
-    const int rows = x.tokens * a.G, r_end = max(t_end, 0) * a.G;
-    float s[T::kValues];
+    if (a.n_local > 0 && key0 >= a.n_sink) t_end = (int)min((int64_t)t_end, (int64_t)key0 + M::kKeys - 1 + a.n_local - old);
+    const int r_end = key0 < x.len ? max(t_end, 0) * a.G : 0, r_begin = max(key0 - old, 0) * a.G / 16 * 16 + M::kRows * share, r_step = M::kRows * row_split;
+    // This lane's rows: those it loads a part of, and its column's.  They go on by r_step rows, dt tokens and dh heads; addresses are added up, not
+    // multiplied out, which took longer than the products did.
+    const int dt = r_step / a.G, dh = r_step - dt * a.G;
+    constexpr int kElem = M::kF32 ? 4 : 2, kRowLanes = 64 / M::kPerLoad;
+    const int part = p.lane & (kRowLanes - 1);             // of a row's sixteen bytes, those of this lane
+    const char* const q0 = reinterpret_cast<const char*>(a.q) + ((int64_t)x.row * a.q_t + (int64_t)g * a.G * a.q_h) * kElem + 16 * part;
+    const int64_t q_step = (dt * a.q_t + dh * a.q_h) * kElem, q_wrap = (a.q_t - a.G * a.q_h) * kElem;
+    const char* from[M::kLoads];
+    int head[M::kLoads], own_t[M::kTiles], own_h[M::kTiles];
 #pragma unroll
-    for (int i = 0; i < T::kValues; ++i) s[i] = 0.f;
-#pragma unroll 1
-    for (int r0 = t_begin * a.G / 16 * 16 + 16 * wave; r0 < r_end; r0 += 16 * kWaves) {
-      const int row = r0 + p.c, t = row / a.G, h = row - t * a.G;
-      bool real = row < rows;
-      float lse = INFINITY;
-      if (real) lse = w.lse[(int64_t)(x.row + t) * a.Hq + g * a.G + h] * 1.4426950408889634f;
-      real = real && lse != -INFINITY;
-      const int hi = real ? old + t : -1, lo = a.n_local > 0 ? hi - a.n_local + 1 : 0;
-      u32x4 q[q_frags(ET)];
-      load_query<ET>(a, (int64_t)(x.row + t) * a.q_t + (int64_t)(g * a.G + h) * a.q_h, p, real, q);
-      const int first = old + r0 / a.G, last = old + (r0 + 15) / a.G;
-      const bool full = key0 + KT - 1 <= first && (a.n_local == 0 || key0 > last - a.n_local || key0 + KT <= a.n_sink);
+    for (int i = 0; i < M::kLoads; ++i) {
+      const int row = r_begin + M::kPerLoad * i + p.lane / kRowLanes, t = row / a.G;
+      head[i] = row - t * a.G;
+      from[i] = q0 + (t * a.q_t + head[i] * a.q_h) * kElem;
+    }
+    const float* lse_at[M::kTiles];
 #pragma unroll
-      for (int h = 0; h < T::kHalves; ++h) {
-        const f32x4 x4 = scores<ET>(k, h, q);
+    for (int n = 0; n < M::kTiles; ++n) {
+      own_t[n] = (r_begin + 16 * n + p.c) / a.G;
+      own_h[n] = r_begin + 16 * n + p.c - own_t[n] * a.G;
+      lse_at[n] = w.lse + ((int64_t)x.row + own_t[n]) * a.Hq + g * a.G + own_h[n];
+    }
+    const int64_t lse_step = (int64_t)dt * a.Hq + dh, lse_wrap = a.Hq - a.G;
+    u32x4 next[M::kLoads];
+    float next_lse[M::kTiles];
+    auto fetch = [&](int r) {
+      if (r + M::kRows <= rows) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float e = __builtin_amdgcn_exp2f(fmaf(x4[i], to_log2, -lse));
-          if (!full) {
-            const int at = key0 + 16 * h + 4 * p.u + i;
-            e = at <= hi && (at >= lo || at < a.n_sink) ? e : 0.f;
-          } else {
-            e = real ? e : 0.f;
-          }
-          s[4 * h + i] += e;
+        for (int i = 0; i < M::kLoads; ++i) next[i] = *reinterpret_cast<const u32x4*>(from[i]);
+#pragma unroll
+        for (int n = 0; n < M::kTiles; ++n) next_lse[n] = *lse_at[n];
+      } else {                                             // (rows behind the last one count as the first)
+#pragma unroll
+        for (int i = 0; i < M::kLoads; ++i)
+          next[i] = *reinterpret_cast<const u32x4*>(r + M::kPerLoad * i + p.lane / kRowLanes < rows ? from[i] : q0);
+#pragma unroll
+        for (int n = 0; n < M::kTiles; ++n) next_lse[n] = r + 16 * n + p.c < rows ? *lse_at[n] : INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < M::kLoads; ++i) from[i] += q_step;
+#pragma unroll
+      for (int n = 0; n < M::kTiles; ++n) lse_at[n] += lse_step;
+      if (dh > 0) {
+#pragma unroll
+        for (int i = 0; i < M::kLoads; ++i) {
+          head[i] += dh;
+          from[i] += head[i] >= a.G ? q_wrap : 0;
+          head[i] -= head[i] >= a.G ? a.G : 0;
         }
       }
-    }
-    const float add = sum_rows<T::kValues>(s, p);
-    constexpr int H = T::kHalves;
-    if (p.c < 4 * H) sums[wave][16 * (p.quad & (H - 1)) + 4 * p.u + p.in_quad] = add;
-    __syncthreads();
-    if (wave == 0) {
-      int key;
-      float* const to = account<ET>(w, p, g, key0, x.len, id, key);
-      if (to) {
-        float total = key < x.counted ? *to : 0.f;
+    };
+    float s[M::kValues];
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) total += sums[i][key - key0];
-        *to = total;
+    for (int i = 0; i < M::kValues; ++i) s[i] = 0.f;
+    if (r_begin < r_end) fetch(r_begin);
+#pragma unroll 1
+    for (int r0 = r_begin; r0 < r_end; r0 += r_step) {
+      // chunk e of row r lies at chunk e ^ r % 16 of its place
+#pragma unroll
+      for (int i = 0; i < M::kLoads; ++i) {
+        const int r = M::kPerLoad * i + p.lane / kRowLanes;
+        *reinterpret_cast<u32x4*>(mine + r * M::kRowBytes + (part ^ (r & 15)) * 16) = next[i];
       }
+      in_order();
+      float lse[M::kTiles];
+      int hi[M::kTiles], lo[M::kTiles], first = 0, last = 0;
+      bool real = true;
+#pragma unroll
+      for (int n = 0; n < M::kTiles; ++n) {
+        lse[n] = next_lse[n] * 1.4426950408889634f;
+        const bool counts = r0 + 16 * n + p.c < rows && lse[n] != -INFINITY;
+        real = real && counts;
+        hi[n] = counts ? old + own_t[n] : -1;
+        lo[n] = a.n_local > 0 ? hi[n] - a.n_local + 1 : 0;
+        if (n == 0) first = old + __builtin_amdgcn_readlane(own_t[n], 0);
+        last = old + __builtin_amdgcn_readlane(own_t[n], 15);
+        own_t[n] += dt;
+        if (dh > 0) {
+          own_h[n] += dh;
+          own_t[n] += own_h[n] >= a.G ? 1 : 0;
+          lse_at[n] += own_h[n] >= a.G ? lse_wrap : 0;
+          own_h[n] -= own_h[n] >= a.G ? a.G : 0;
+        }
+      }
+      if (r0 + r_step < r_end) fetch(r0 + r_step);
+      const bool full = __all(real) && key0 + M::kKeys - 1 <= first && (a.n_local == 0 || key0 > last - a.n_local || key0 + M::kKeys <= a.n_sink);
+      auto add = [&](int n, auto masked) {
+        u32x4 q[M::kFrags];
+#pragma unroll
+        for (int i = 0; i < M::kFrags; ++i) {
+          const int chunk = M::kF32 ? 16 * (i >> 2) + 4 * p.u + (i & 3) : 4 * p.u + i;
+          q[i] = *reinterpret_cast<const u32x4*>(mine + (16 * n + p.c) * M::kRowBytes + (chunk ^ p.c) * 16);
+        }
+        f32x4 x4[M::kHalves];                              // (the products of different keys in turn: none waits for the one before it)
+#pragma unroll
+        for (int h = 0; h < M::kHalves; ++h) x4[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < M::kFrags; ++i) {
+          if constexpr (M::kF32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int h = 0; h < M::kHalves; ++h)
+                x4[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[h][i][e]), __uint_as_float(q[i][e]), x4[h], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int h = 0; h < M::kHalves; ++h) x4[h] = mfma_bf16(k[h][i], q[i], x4[h]);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < M::kHalves; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float e = __builtin_amdgcn_exp2f(fmaf(x4[h][i], to_log2, -lse[n]));
+            if constexpr (decltype(masked)::value) {
+              const int at = key0 + 16 * h + 4 * p.u + i;
+              e = (at <= hi[n]) & ((at >= lo[n]) | (at < a.n_sink)) ? e : 0.f;
+            }
+            s[4 * h + i] += e;
+          }
+      };
+      if (full) {
+#pragma unroll
+        for (int n = 0; n < M::kTiles; ++n) add(n, std::false_type{});
+      } else {
+#pragma unroll
+        for (int n = 0; n < M::kTiles; ++n) add(n, std::true_type{});
+      }
+      in_order();
+    }
+    // over the rows of a wavefront, then over the wavefronts
+    constexpr int kAtOnce = 8;
+#pragma unroll
+    for (int n = 0; n < M::kValues; n += kAtOnce) {
+      float part[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) part[i] = s[n + i];
+      const float add = sum_rows<kAtOnce>(part, p);
+      if (p.c < kAtOnce) sums[wave][4 * n + 16 * (p.c >> 2) + 4 * p.u + (p.c & 3)] = add;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < block; i += kThreads) {
+      const int key = block0 + i;
+      if (key >= x.len) continue;
+      const int id = table[key >> a.page_shift];
+      if (!page_ok(a, id)) continue;
+      float* const to = w.weights + ((((int64_t)id * a.Hkv + g) << a.page_shift) + (key & ((1 << a.page_shift) - 1)));
+      float total = key < x.counted ? *to : 0.f;
+      const int first = i / M::kKeys * row_split;
+      for (int n = 0; n < row_split; ++n) total += sums[first + n][i % M::kKeys];
+      *to = total;
     }
     __syncthreads();
   }

@@ -73,6 +73,12 @@ size_t ws_plan(const Params* p) {
   return !mp::page_plan_needs_workspace(p->batch, p->max_tokens) ? 0 : kCounterBytes + align256((size_t)3 * (p->batch + 1) * sizeof(int));
 }
 
+int keep_parts_of(const Params* p) { return mp::keep_parts((int64_t)p->batch * p->n_kv_heads, (int64_t)p->max_pages * p->page_size); }
+size_t ws_keep(const Params* p) {
+  const int parts = keep_parts_of(p);
+  return parts == 1 ? 0 : kCounterBytes + align256((size_t)p->batch * p->n_kv_heads * parts * mp::kKeepPartBytes);
+}
+
 // Attention over pools of any kind, behind check().
 int attend(const Params* p, const void* q, const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
            const uint8_t* k_block, const uint8_t* v_block, const int32_t* block_table, const int32_t* lengths, const int32_t* token_start,
@@ -127,6 +133,8 @@ size_t magicpig_paged_workspace_bytes(const Params* p) {
     const size_t a = mp::paged_grid_fits(f) ? ws_attention(f) : 0;   // (attention refuses the others)
     if (a > m) m = a;
   }
+  const size_t keep = ws_keep(p);
+  if (keep > m) m = keep;
   return m < 256 ? 256 : m;
 }
 
@@ -301,12 +309,15 @@ int magicpig_page_keep(const Params* p, const float* weights, const int32_t* blo
   if (!aligned16(weights) || !aligned(block_table, 4) || !aligned(lengths, 4) || !aligned(budgets, 4) || !aligned(kept, 4) ||
       !aligned(lengths_out, 4) || !aligned16(workspace))
     return MAGICPIG_INVALID_ARG;
-  (void)workspace_bytes;
+  const size_t need = ws_keep(p);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return MAGICPIG_WORKSPACE_TOO_SMALL;
   if (p->batch == 0) return MAGICPIG_OK;
   mp::PageKeepArgs a{};
   a.weights = weights; a.table = block_table; a.lengths = lengths; a.budgets = budgets; a.kept = kept; a.lengths_out = lengths_out;
   a.batch = p->batch; a.heads = p->n_kv_heads; a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages;
   a.max_len = p->max_pages * p->page_size; a.n_pages = (int)p->n_pages; a.n_first = n_first; a.n_last = n_last; a.max_keep = max_keep;
+  a.parts = keep_parts_of(p);
+  if (need > 0) a.workspace = reinterpret_cast<char*>(workspace) + kCounterBytes;
   return mp::hip_status(mp::launch_page_keep(a, (int64_t)p->batch * p->n_kv_heads, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
@@ -331,7 +342,7 @@ int magicpig_page_evict(const Params* p, const int32_t* kept, int32_t max_keep, 
   a.n_free_out = n_free_out; a.status = status;
   a.batch = p->batch; a.heads = p->n_kv_heads; a.page_shift = __builtin_ctz(p->page_size); a.max_pages = p->max_pages;
   a.max_len = p->max_pages * p->page_size; a.max_keep = max_keep; a.n_pages = p->n_pages;
-  const int row = (int)row_bytes(p, mp::kHeadDim), slice = row < 128 ? row : 128;
+  const int row = (int)row_bytes(p, mp::kHeadDim), slice = mp::evict_slice(row, (int64_t)p->batch * p->n_kv_heads);
   auto array = [](void* at, int64_t page, int64_t key, int64_t head, int slice, int slices) {
     return mp::PagedArray{static_cast<char*>(at), page, key, head, slice, slices};
   };

@@ -66,7 +66,7 @@ struct PagedArgs {
 struct PageWeightsArgs {
   PagedArgs paged;
   const float* lse; const int* counted; float* weights;
-  int heads;              // KV heads that a workgroup takes at once
+  int heads;              // few rows: KV heads that a workgroup takes at once; many: shares of the rows
 };
 
 // Which keys stay (page_keep.hip).
@@ -74,6 +74,8 @@ struct PageKeepArgs {
   const float* weights; const int* table; const int* lengths; const int* budgets;
   int* kept; int* lengths_out;
   int batch, heads, page_shift, max_pages, max_len, n_pages, n_first, n_last, max_keep;
+  int parts;              // workgroups to a request's KV head
+  void* workspace;        // of several: what they tell one another
 };
 
 // Eviction (page_evict.hip).  An array of rows in the pages: strides in bytes; a row is `slices` slices of `slice` bytes.
