@@ -120,6 +120,8 @@ struct PagedForm {
 // 37.5 | 24.4, 1 x 65536 85.5 | 80.9, 1 x 2048 19.8 | 24.5; 64 rows 64 x 1000 91.5 | 66.5, 1 x 65536 86.9 | 92.1.
 constexpr int kPagedManyRows = 128, kPagedManyKeys = 64;
 constexpr int kPagedNearParts = 16, kPagedNearTiles = 128;   // few rows: see paged_share
+constexpr int kPagedFourTile = 64;           // few rows, pools in four bits: keys of a tile
+constexpr int paged_near_tiles(int tile) { return tile == kPagedFourTile ? 16 : kPagedNearTiles; }
 constexpr int kPagedCounters = 1024;         // words at the start of the workspace, one per share (at most kNumCU, or one for each KV head)
 inline int paged_rows(bool fp32, int64_t rows) { return fp32 || rows <= 16 ? 16 : (rows <= 32 ? 32 : kPagedManyRows); }
 
@@ -138,7 +140,7 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
   PagedForm f{};
   f.rows = paged_rows(fp32, (int64_t)max_new * group);
   const bool many = f.rows == kPagedManyRows;
-  f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : (four ? 64 : 32));
+  f.key_tile = many ? kPagedManyKeys : (fp32 ? 16 : (four ? kPagedFourTile : 32));
   f.tile_tokens = group <= f.rows ? f.rows / group : 1;
   f.head_blocks = group <= f.rows ? 1 : (group + f.rows - 1) / f.rows;
   // target: workgroups that are resident at once.  Many rows, us with half as many | these | twice as many, 32 heads over 8: 64 rows over 65536 keys
@@ -168,7 +170,7 @@ inline PagedForm paged_form(int batch, int kv_heads, int group, bool fp32, int64
     const int tokens = max_new < f.tile_tokens ? max_new : f.tile_tokens, used = group < f.rows ? group * tokens : f.rows;
     while (row_bytes > 0 && row_bytes << f.near_shift < 512 && used << (f.near_shift + 1) <= 32) ++f.near_shift;
     while (f.set_shift < kPagedGroupShift && kv_heads % (2 << f.set_shift) == 0 &&
-           f.target * (2 << f.set_shift) <= f.items * (f.set_shift < f.near_shift && f.items * charge >= kPagedNearTiles * f.target ? kPagedNearParts : 1))
+           f.target * (2 << f.set_shift) <= f.items * (f.set_shift < f.near_shift && f.items * charge >= paged_near_tiles(f.key_tile) * f.target ? kPagedNearParts : 1))
       ++f.set_shift;
     // (a group has a key tile for each wavefront of a head; the groups of all row tiles are counted in 31 bits, in sets too)
     auto groups = [&](int shift) { return (charge + (1 << shift) - 1) >> shift; };

@@ -47,6 +47,7 @@ int check_pool(const Params* p, int64_t page, int64_t key, int64_t head) {
   if (page < 0 || key < mp::kHeadDim || head < 0) return MAGICPIG_INVALID_ARG;
   const int64_t unit = four(p) ? mp::kHeadDim : (p->kv_dtype == MAGICPIG_KV_FP8_E4M3 ? 16 : 8);   // (four bits: a row's scales are a word)
   if (page % unit || key % unit || head % unit) return MAGICPIG_UNSUPPORTED;
+  if (four(p) && page / unit > UINT32_MAX) return MAGICPIG_UNSUPPORTED;   // (the kernels count its rows in 32 bits)
   // rows inside a page are addressed by 32-bit byte offsets
   if (key > ((int64_t)1 << 31) || row_bytes(p, key * p->page_size) >= ((int64_t)1 << 31)) return MAGICPIG_UNSUPPORTED;
   return MAGICPIG_OK;
@@ -100,6 +101,9 @@ int attend(const Params* p, const void* q, const void* k_pages, const void* v_pa
   mp::PagedArgs a{};
   a.q = q; a.k = k_pages; a.v = v_pages; a.k_scale = k_scale; a.v_scale = v_scale;
   a.k_block = k_block; a.v_block = v_block;
+  a.k_page_rows = (uint32_t)(p->k_stride_page / mp::kHeadDim); a.k_key_rows = (uint32_t)(p->k_stride_key / mp::kHeadDim);
+  a.v_page_rows = (uint32_t)(p->v_stride_page / mp::kHeadDim); a.v_key_rows = (uint32_t)(p->v_stride_key / mp::kHeadDim);
+  a.same_strides = p->k_stride_page == p->v_stride_page && p->k_stride_key == p->v_stride_key;
   a.table = block_table; a.lengths = lengths; a.token_start = token_start;
   a.out = out; a.lse = lse;
   a.arrived = reinterpret_cast<unsigned*>(workspace);

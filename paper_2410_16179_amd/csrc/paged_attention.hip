@@ -162,7 +162,7 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
 template <int ET, int NR>
 struct FewRows {
   static constexpr bool kF32 = ET == kFP32;
-  static constexpr int kTile = kF32 ? 16 : (ET == kFP4 ? 64 : 32);   // keys per tile
+  static constexpr int kTile = kF32 ? 16 : (ET == kFP4 ? kPagedFourTile : 32);   // keys per tile
   static constexpr int kHalves = kTile / 16;
   static constexpr int kFrags = ET == kFP4 ? 4 : 8;      // loads of a lane per tile for V, and for K, which e4m3 takes 16 elements at a time
   static constexpr int kKeyFrags = ET == kFP8 || ET == kFP4 ? 4 : 8;
@@ -261,10 +261,22 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
   const char* const ksbase = reinterpret_cast<const char*>(a.k_block) + ((int64_t)g * a.k_head >> 5);
   const char* const vsbase = reinterpret_cast<const char*>(a.v_block) + ((int64_t)g * a.v_head >> 5);
   const uint32_t ks_key = (uint32_t)(a.k_key >> 5), vs_key = (uint32_t)(a.v_key >> 5);
+  const bool one_page = kFour && (KT >> a.page_shift) <= 1;   // whether a tile lies in one
+  // Four bits, where addresses weigh more than elsewhere: in rows of 128 elements (64 bytes of a pool, four of its scales) from the head's first one on.
+  auto row_of = [&](int id, int at, uint32_t page_rows, uint32_t key_rows) {
+    return (uint64_t)(uint32_t)id * page_rows + (uint32_t)at * key_rows;
+  };
+  uint64_t k_row[kFour ? F::kHalves : 1];                // of the tile that is requested; V's where the pools have the same strides
 
   auto tile_key = [&](int v) { return (v < span.sink ? v : v + span.skip) * KT; };
   auto tile_pages = [&](int v, TilePages<KT>& p) {
     const int key0 = tile_key(v);
+    if (one_page) {
+      const int at = key0 >> a.page_shift, id = table[at < a.max_pages ? at : a.max_pages - 1];
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) p.id[h] = id;
+      return;
+    }
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
       const int at = (key0 + 16 * h) >> a.page_shift;
@@ -272,33 +284,72 @@ __global__ __launch_bounds__(kFewThreads, 2) void paged_few_rows_kernel(const Pa
     }
   };
   auto page_ok = [&](int id) { return (uint32_t)id < (uint32_t)a.n_pages; };
+  auto descriptor = [&](const char* base, uint64_t offset, int rows, uint32_t stride) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + offset), 0, rows * stride, kBufferWord3);
+  };
+  // (four bits: where a workgroup takes neighbouring heads their rows share lines)
+  auto load_four = [&](__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
+    if constexpr (SETS) load_shared(rows, at, to);
+    else load_once(rows, at, to);
+  };
   auto request_k = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
+    if constexpr (kFour) {
+      if (one_page) {
+        int there = 0;
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h) there += valid[h];
+        const uint64_t row = row_of(there ? p.id[0] : 0, key0 & page_mask, a.k_page_rows, a.k_key_rows);
+        const auto rows = descriptor(kbase, row * 64, there, k_key), scales = descriptor(ksbase, row * 4, there, ks_key);
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h) {
+          load_four(rows, k_lane + 16 * h * k_key, f.kf[h]);
+          f.ks[h] = load_byte(scales, (16 * h + c) * ks_key + u);
+        }
+        k_row[0] = row;
+        return;
+      }
+    }
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
-      const auto rows = rows16(kbase, pool_bytes<ET>(a.k_page), k_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
       if constexpr (kFour) {
-        const auto scales = rows16(ksbase, a.k_page >> 5, ks_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
-        load_once(rows, k_lane, f.kf[h]);
-        f.ks[h] = load_byte(scales, c * ks_key + u);
-        continue;
-      }
+        k_row[h] = row_of(valid[h] ? p.id[h] : 0, (key0 + 16 * h) & page_mask, a.k_page_rows, a.k_key_rows);
+        load_four(descriptor(kbase, k_row[h] * 64, valid[h], k_key), k_lane, f.kf[h]);
+        f.ks[h] = load_byte(descriptor(ksbase, k_row[h] * 4, valid[h], ks_key), c * ks_key + u);
+      } else {
+      const auto rows = rows16(kbase, pool_bytes<ET>(a.k_page), k_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
 #pragma unroll
       for (int i = 0; i < F::kKeyFrags / F::kHalves; ++i) {
         const uint32_t at = ET == kFP8 ? 2 * i * k_key : (i & 3) * k_key + 256 * (i >> 2);
         load_once(rows, k_lane + at, f.kf[h * (F::kKeyFrags / F::kHalves) + i]);
       }
+      }
     }
   };
+  // (behind request_k of the same tile)
   auto request_v = [&](int key0, const TilePages<KT>& p, const int (&valid)[F::kHalves]) {
+    if constexpr (kFour) {
+      if (one_page) {
+        int there = 0;
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h) there += valid[h];
+        const uint64_t row = a.same_strides ? k_row[0] : row_of(there ? p.id[0] : 0, key0 & page_mask, a.v_page_rows, a.v_key_rows);
+        const auto rows = descriptor(vbase, row * 64, there, v_key), scales = descriptor(vsbase, row * 4, there, vs_key);
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h) {
+          load_four(rows, v_lane + 16 * h * v_key, f.vf[h]);
+          load_shared(scales, (16 * h + c) * vs_key, f.vs[h]);
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int h = 0; h < F::kHalves; ++h) {
-      const auto rows = rows16(vbase, pool_bytes<ET>(a.v_page), v_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
       if constexpr (kFour) {
-        const auto scales = rows16(vsbase, a.v_page >> 5, vs_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
-        load_once(rows, v_lane, f.vf[h]);
-        load_once(scales, c * vs_key, f.vs[h]);
-        continue;
+        const uint64_t row = a.same_strides ? k_row[h] : row_of(valid[h] ? p.id[h] : 0, (key0 + 16 * h) & page_mask, a.v_page_rows, a.v_key_rows);
+        load_four(descriptor(vbase, row * 64, valid[h], v_key), v_lane, f.vf[h]);
+        load_shared(descriptor(vsbase, row * 4, valid[h], vs_key), c * vs_key, f.vs[h]);
       } else {
+      const auto rows = rows16(vbase, pool_bytes<ET>(a.v_page), v_key, p.id[h], (key0 + 16 * h) & page_mask, valid[h]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (kF32) {

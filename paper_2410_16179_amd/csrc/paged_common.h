@@ -59,7 +59,10 @@ struct PagedArgs {
   int near_shift, set_shift, group_shift, shares[kPagedGroupShift + 1];   // few rows: see PagedForm
   unsigned* arrived;      // few rows: partials of the cut item that begins in a share which are there (0 between calls)
   int64_t k_page, k_key, k_head, v_page, v_key, v_head, q_t, q_h;
-  const uint8_t* k_block; const uint8_t* v_block;         // scales of pools in four bits: strides are those of the elements / 32
+  // Pools in four bits: scales, whose strides are those of the elements / 32; strides in rows of 128 elements; whether both pools have the same.
+  const uint8_t* k_block; const uint8_t* v_block;
+  uint32_t k_page_rows, k_key_rows, v_page_rows, v_key_rows;
+  int same_strides;
 };
 
 // Accounts of attention weight (page_weights.hip).
@@ -319,6 +322,8 @@ __device__ inline int paged_groups(const PagedArgs& a, int len, int group_shift)
 //   Query rows of a set beyond the 32 that are joined at once: 16 x 4096, 32 rows 39.9 | 69.
 //   Where items are short, at most a share, sets of any heads save the way from item to item: 8 KV heads, 256 x 300 e4m3 62 | 36, bf16 77 | 58, stored
 //   head by head 59 | 35, 1000 x 50 171 | 52, 32 rows 256 x 300 84 | 51.
+//   Four bits: two heads' rows share a line of 128 bytes and eight heads' scales do, so sets pay from two tiles for each wavefront on (and lines are kept in
+//   the caches): 8 KV heads, token by token, 48 requests of up to 30011 keys 106 | 88, 16 x 16384 89 | 79.
 // The sets of a share follow one another on one XCD (workgroups go to the eight XCDs in turn).
 // SETS: whether it may be more than one (the way there costs a small call 0.5 us, of 12).
 template <int KT, bool SETS>
@@ -337,7 +342,7 @@ __device__ inline bool paged_share(const PagedArgs& a, int index, PagedShare& ou
     }
     sum = wave_sum(sum) * (float)a.Hkv;
     longest = wave_max(longest) * (float)a.target;
-    const float near = sum * (sum >= (float)(kPagedNearTiles * a.target) ? (float)kPagedNearParts : 1.f);
+    const float near = sum * (sum >= (float)(paged_near_tiles(KT) * a.target) ? (float)kPagedNearParts : 1.f);
     while (shift < a.set_shift && longest * (float)(2 << shift) <= (shift < a.near_shift ? near : sum)) ++shift;
     shift = __builtin_amdgcn_readfirstlane(shift);
 #pragma unroll

@@ -63,9 +63,6 @@ __device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4
 __device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
   to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, kNonTemporal));
 }
-__device__ inline void load_once(__amdgpu_buffer_rsrc_t rows, uint32_t at, uint32_t& to) {
-  to = __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, kNonTemporal);
-}
 __device__ inline uint32_t load_byte(__amdgpu_buffer_rsrc_t rows, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b8(rows, at, 0, 0); }
 // The same, kept: workgroups of other row tiles read the row too.
 __device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x4& to) {
@@ -73,6 +70,9 @@ __device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32
 }
 __device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, u32x2& to) {
   to = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, 0));
+}
+__device__ inline void load_shared(__amdgpu_buffer_rsrc_t rows, uint32_t at, uint32_t& to) {
+  to = __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, 0);
 }
 
 // The lanes' 16 bytes one behind the other from `to` on (the same for the wavefront); there behind stored().
