@@ -73,7 +73,7 @@ struct Operand {
   __device__ inline void request(const Keys<ET>& keys, const Place& p, int h, int id, int at, int valid) {
     const auto rows = rows16(keys.base, keys.page, keys.key, id, at, valid);
     if constexpr (ET == kFP4) {
-      load_once(rows, (p.lane >> 2) * keys.key + 16 * (p.in_quad ^ p.u), k[h][0]);
+      load_shared(rows, (p.lane >> 2) * keys.key + 16 * (p.in_quad ^ p.u), k[h][0]);   // (neighbouring heads' rows share lines)
       scale[h] = load_byte(rows16(keys.blocks, keys.block_page, keys.block_key, id, at, valid), p.c * keys.block_key + p.u);
     } else if constexpr (ET == kFP8) {
 #pragma unroll
