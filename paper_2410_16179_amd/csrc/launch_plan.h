@@ -212,27 +212,32 @@ inline int evict_slice(int row, int64_t units) {
 }
 
 // ---- accounts of attention weight -------------------------------------------------------------------
-// rows: query rows of a KV head (new tokens times query heads) that a wavefront has at once: 16, 32, or 128, more of which come by one tile after the other;
-// heads: 16 or 32 rows: KV heads that a workgroup's eight wavefronts take at once; 128: the shares that they split the rows into; tiles: of keys, at most,
-// all KV heads together; workgroups: 16 or 32 rows: what is resident at once.
+// rows: query rows of a KV head (new tokens times query heads) that a wavefront has at once: up to 128 (float32: 16), in registers, its keys going by; many: more of
+// them, 32 of which go by at a time, the keys in registers.  heads: KV heads that a workgroup's wavefronts take at once; many: shares that they split the rows
+// into; tiles: of keys, at most, all KV heads together; workgroups: what is resident at once; many: at most.
+constexpr int kWeightsManyWaves = 4;         // wavefronts of a workgroup, many rows
+constexpr int weights_tile(bool fp32, int bits, int rows) { return fp32 ? 16 : (bits == 16 || rows > 16 ? 32 : 64); }   // keys of a tile, few rows
 struct WeightsForm {
+  bool many;
   int rows, heads;
   int64_t tiles, workgroups;
 };
 inline WeightsForm weights_form(int batch, int kv_heads, int group, bool fp32, int bits, int max_new, int64_t max_len) {
   WeightsForm f{};
   const int64_t rows = (int64_t)max_new * group;
-  f.rows = rows <= 16 ? 16 : (rows <= 32 && !fp32 ? 32 : 128);
+  f.many = rows > (fp32 ? 16 : 128);
+  f.rows = 16;
+  while (f.rows < 128 && f.rows < rows) f.rows *= 2;
   f.heads = 1;
-  int tile = fp32 ? 16 : (bits == 16 ? 32 : 64);
-  int64_t most = 2 * kNumCU;
-  if (f.rows < 128) {
-    while (f.heads < 8 && kv_heads % (2 * f.heads) == 0) f.heads *= 2;
-  } else {
+  int tile = weights_tile(fp32, bits, f.rows);
+  int64_t most = (f.rows <= 32 ? 2 : 1) * kNumCU;
+  if (f.many) {
     // (a share of two tiles of sixteen rows at least)
-    while (f.heads < 8 && 64 * f.heads <= rows) f.heads *= 2;
-    tile = (fp32 ? 32 : 64) * (8 / f.heads);
+    while (f.heads < kWeightsManyWaves && 64 * f.heads <= rows) f.heads *= 2;
+    tile = (fp32 ? 32 : 64) * (kWeightsManyWaves / f.heads);
     most = 1 << 14;
+  } else {
+    while (f.heads < 8 && kv_heads % (2 * f.heads) == 0) f.heads *= 2;
   }
   f.tiles = (max_len + tile - 1) / tile * batch * kv_heads;
   f.workgroups = f.tiles < most ? (f.tiles > 0 ? f.tiles : 1) : most;

@@ -8,10 +8,10 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
-// Keys of a tile, and loads of a lane for sixteen of them.
-template <int ET>
+// Few rows: keys of a tile, and loads of a lane for sixteen of them.
+template <int ET, int NR = 1>
 struct Tile {
-  static constexpr int kKeys = ET == kFP32 ? 16 : (ET == kBF16 ? 32 : 64);
+  static constexpr int kKeys = weights_tile(ET == kFP32, ET == kBF16 ? 16 : 8, 16 * NR);
   static constexpr int kHalves = kKeys / 16;
   static constexpr int kFrags = ET == kFP32 ? 8 : (ET == kBF16 ? 4 : (ET == kFP8 ? 2 : 1));
   static constexpr int kValues = 4 * kHalves;              // scores of a lane: key 16 (i / 4) + 4 u + i % 4 is number i
@@ -130,8 +130,8 @@ __device__ inline void load_query(const PagedArgs& a, int64_t at, const Place& p
 }
 
 // Scores of half h with sixteen rows.
-template <int ET>
-__device__ inline f32x4 scores(const Operand<ET>& k, int h, const u32x4 (&q)[q_frags(ET)]) {
+template <int ET, int H>
+__device__ inline f32x4 scores(const Operand<ET, H>& k, int h, const u32x4 (&q)[q_frags(ET)]) {
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if constexpr (ET == kFP32) {
 #pragma unroll
@@ -201,9 +201,8 @@ __device__ inline void request_tile(const PagedArgs& a, const Keys<ET>& keys, co
     k.request(keys, p, h, id[h], (key0 + 16 * h) & page_mask, page_ok(a, id[h]) ? min(max(end - key0 - 16 * h, 0), 16) : 0);
 }
 // Where the account of the lane's key is, key 16 (v / 4) + 4 u + v % 4 of the tile for v = c % (4 halves); null where it has none, or another lane has it.
-template <int ET>
-__device__ inline float* account(const PageWeightsArgs& a, const Place& p, int g, int key0, int len, const int (&id)[Tile<ET>::kHalves], int& key) {
-  constexpr int H = Tile<ET>::kHalves;
+template <int H>
+__device__ inline float* account(const PageWeightsArgs& a, const Place& p, int g, int key0, int len, const int (&id)[H], int& key) {
   key = key0 + 16 * (p.quad & (H - 1)) + 4 * p.u + p.in_quad;
   int page = id[0];
 #pragma unroll
@@ -216,9 +215,9 @@ __device__ inline float* account(const PageWeightsArgs& a, const Place& p, int g
 // Workgroups take equal, contiguous shares of all tiles; the wavefronts of one take `heads` neighbouring KV heads, whose rows lie side by side in
 // many pools, and waves / heads tiles at a time.
 template <int ET, int NR>
-__global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const PageWeightsArgs w) {
-  using T = Tile<ET>;
-  constexpr int KT = T::kKeys;
+__global__ __launch_bounds__(kThreads, NR <= 2 ? 4 : 2) void page_weights_few_kernel(const PageWeightsArgs w) {
+  using T = Tile<ET, NR>;
+  constexpr int KT = T::kKeys, kTogether = NR < 2 ? NR : 2;   // rows (sixteens of them) whose scores are there at once
   __shared__ __align__(16) char lds[ET == kFP4 ? kWaves * 4096 : 16];
   const PagedArgs& a = w.paged;
   const Place p;
@@ -283,7 +282,7 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
     auto tile_key = [&](int v) { return (v < x.sink ? v : v + x.skip) * KT; };
     int v = from * at_once + place;
     const int v_end = min(to * at_once, x.tiles);
-    Operand<ET> k;
+    Operand<ET, T::kHalves> k;
     int id[T::kHalves], key = 0;
     float* to_account = nullptr;
     float old = 0.f;
@@ -291,7 +290,7 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
       const int key0 = tile_key(v);
       tile_pages<T::kHalves>(a, table, key0, id);
       request_tile<ET, T::kHalves>(a, keys, p, key0, x.len, id, k);
-      to_account = account<ET>(w, p, g, key0, x.len, id, key);
+      to_account = account(w, p, g, key0, x.len, id, key);
       old = to_account && key < x.counted ? *to_account : 0.f;
     };
     if (v < v_end) bring(v);
@@ -299,37 +298,40 @@ __global__ __launch_bounds__(kThreads, 4) void page_weights_few_kernel(const Pag
     while (v < v_end) {
       const int key0 = tile_key(v);
       k.arrange(p, mine);
-      float s[T::kValues], sum[T::kValues];
-      float part[NR][T::kValues];
+      float s[T::kValues];
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int h = 0; h < T::kHalves; ++h) {
-          const f32x4 x4 = scores<ET>(k, h, q[n]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) part[n][4 * h + i] = x4[i];
-        }
+      for (int i = 0; i < T::kValues; ++i) s[i] = 0.f;
+      float part[kTogether][T::kValues];
+      const bool full = key0 + KT - 1 <= min_hi && (key0 >= max_lo || key0 + KT <= a.n_sink);
       float* const to_now = to_account;
       const float old_now = old;
       v += at_once;
-      if (v < v_end) bring(v);
-      const bool full = key0 + KT - 1 <= min_hi && (key0 >= max_lo || key0 + KT <= a.n_sink);
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
+      for (int n0 = 0; n0 < NR; n0 += kTogether) {
 #pragma unroll
-        for (int i = 0; i < T::kValues; ++i) {
-          float e = __builtin_amdgcn_exp2f(fmaf(part[n][i], to_log2, -lse[n]));
-          if (!full) {
-            const int at = key0 + 16 * (i >> 2) + 4 * p.u + (i & 3);
-            e = at <= hi[n] && (at >= lo[n] || at < a.n_sink) ? e : 0.f;
-          } else if (!all) {
-            e = hi[n] >= 0 ? e : 0.f;                      // (the position of a row that counts is min_hi or more)
+        for (int n = 0; n < kTogether; ++n)
+#pragma unroll
+          for (int h = 0; h < T::kHalves; ++h) {
+            const f32x4 x4 = scores(k, h, q[n0 + n]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[n][4 * h + i] = x4[i];
           }
-          s[i] = n == 0 ? e : s[i] + e;
-        }
+        if (n0 + kTogether == NR && v < v_end) bring(v);
 #pragma unroll
-      for (int i = 0; i < T::kValues; ++i) sum[i] = s[i];
-      const float add = sum_rows<T::kValues>(sum, p);
+        for (int n = 0; n < kTogether; ++n)
+#pragma unroll
+          for (int i = 0; i < T::kValues; ++i) {
+            float e = __builtin_amdgcn_exp2f(fmaf(part[n][i], to_log2, -lse[n0 + n]));
+            if (!full) {
+              const int at = key0 + 16 * (i >> 2) + 4 * p.u + (i & 3);
+              e = at <= hi[n0 + n] && (at >= lo[n0 + n] || at < a.n_sink) ? e : 0.f;
+            } else if (!all) {
+              e = hi[n0 + n] >= 0 ? e : 0.f;               // (the position of a row that counts is min_hi or more)
+            }
+            s[i] += e;
+          }
+      }
+      const float add = sum_rows<T::kValues>(s, p);
       if (to_now) *to_now = old_now + add;
     }
     if (set + 1 == sets && to == groups) {
@@ -351,8 +353,9 @@ struct Many {
 };
 
 template <int ET>
-__global__ __launch_bounds__(kThreads, 2) void page_weights_many_kernel(const PageWeightsArgs w) {
+__global__ __launch_bounds__(64 * kWeightsManyWaves, 2) void page_weights_many_kernel(const PageWeightsArgs w) {
   using M = Many<ET>;
+  constexpr int kWaves = kWeightsManyWaves, kThreads = 64 * kWaves;
   __shared__ __align__(16) char lds[kWaves][M::kRows * M::kRowBytes];
   __shared__ float sums[kWaves][M::kKeys];
   const PagedArgs& a = w.paged;
@@ -404,48 +407,45 @@ __global__ __launch_bounds__(kThreads, 2) void page_weights_many_kernel(const Pa
     int t_end = x.tokens;
     if (a.n_local > 0 && key0 >= a.n_sink) t_end = (int)min((int64_t)t_end, (int64_t)key0 + M::kKeys - 1 + a.n_local - old);
     const int r_end = key0 < x.len ? max(t_end, 0) * a.G : 0, r_begin = max(key0 - old, 0) * a.G / 16 * 16 + M::kRows * share, r_step = M::kRows * row_split;
-    // This lane's rows: those it loads a part of, and its column's.  They go on by r_step rows, dt tokens and dh heads; addresses are added up, not
-    // multiplied out, which took longer than the products did.
-    const int dt = r_step / a.G, dh = r_step - dt * a.G;
+    // This lane's rows: those it loads a part of, and its column's.  They go on by r_step rows, dt tokens and dh heads.  Addresses are a pointer of the
+    // wavefront's, to the first row's token, and a lane's offset, which changes where a row's head goes past the last one.  (Multiplied out they took longer
+    // than the products did; 64-bit ones for each lane took registers that kept a wavefront from the compute unit.)
+    const int dt = r_step / a.G, dh = r_step - dt * a.G, t0 = r_begin / a.G;
     constexpr int kElem = M::kF32 ? 4 : 2, kRowLanes = 64 / M::kPerLoad;
     const int part = p.lane & (kRowLanes - 1);             // of a row's sixteen bytes, those of this lane
-    const char* const q0 = reinterpret_cast<const char*>(a.q) + ((int64_t)x.row * a.q_t + (int64_t)g * a.G * a.q_h) * kElem + 16 * part;
-    const int64_t q_step = (dt * a.q_t + dh * a.q_h) * kElem, q_wrap = (a.q_t - a.G * a.q_h) * kElem;
-    const char* from[M::kLoads];
-    int head[M::kLoads], own_t[M::kTiles], own_h[M::kTiles];
+    const char* q_at = reinterpret_cast<const char*>(a.q) + ((x.row + (int64_t)t0) * a.q_t + (int64_t)g * a.G * a.q_h) * kElem;
+    const float* lse_at = w.lse + (x.row + (int64_t)t0) * a.Hq + g * a.G;
+    const int q_t = (int)a.q_t * kElem, q_h = (int)a.q_h * kElem, q_wrap = q_t - a.G * q_h;
+    int from[M::kLoads], head[M::kLoads], own_t[M::kTiles], own_h[M::kTiles], lse_from[M::kTiles];
 #pragma unroll
     for (int i = 0; i < M::kLoads; ++i) {
       const int row = r_begin + M::kPerLoad * i + p.lane / kRowLanes, t = row / a.G;
       head[i] = row - t * a.G;
-      from[i] = q0 + (t * a.q_t + head[i] * a.q_h) * kElem;
+      from[i] = (t - t0) * q_t + head[i] * q_h + 16 * part;
     }
-    const float* lse_at[M::kTiles];
 #pragma unroll
     for (int n = 0; n < M::kTiles; ++n) {
       own_t[n] = (r_begin + 16 * n + p.c) / a.G;
       own_h[n] = r_begin + 16 * n + p.c - own_t[n] * a.G;
-      lse_at[n] = w.lse + ((int64_t)x.row + own_t[n]) * a.Hq + g * a.G + own_h[n];
+      lse_from[n] = (own_t[n] - t0) * a.Hq + own_h[n];
     }
-    const int64_t lse_step = (int64_t)dt * a.Hq + dh, lse_wrap = a.Hq - a.G;
     u32x4 next[M::kLoads];
     float next_lse[M::kTiles];
     auto fetch = [&](int r) {
       if (r + M::kRows <= rows) {
 #pragma unroll
-        for (int i = 0; i < M::kLoads; ++i) next[i] = *reinterpret_cast<const u32x4*>(from[i]);
+        for (int i = 0; i < M::kLoads; ++i) next[i] = *reinterpret_cast<const u32x4*>(q_at + from[i]);
 #pragma unroll
-        for (int n = 0; n < M::kTiles; ++n) next_lse[n] = *lse_at[n];
-      } else {                                             // (rows behind the last one count as the first)
+        for (int n = 0; n < M::kTiles; ++n) next_lse[n] = lse_at[lse_from[n]];
+      } else {                                             // (rows behind the last one read the tile's first)
+        const int first = __builtin_amdgcn_readfirstlane(from[0]);
 #pragma unroll
-        for (int i = 0; i < M::kLoads; ++i)
-          next[i] = *reinterpret_cast<const u32x4*>(r + M::kPerLoad * i + p.lane / kRowLanes < rows ? from[i] : q0);
+        for (int i = 0; i < M::kLoads; ++i) next[i] = *reinterpret_cast<const u32x4*>(q_at + (r + M::kPerLoad * i + p.lane / kRowLanes < rows ? from[i] : first));
 #pragma unroll
-        for (int n = 0; n < M::kTiles; ++n) next_lse[n] = r + 16 * n + p.c < rows ? *lse_at[n] : INFINITY;
+        for (int n = 0; n < M::kTiles; ++n) next_lse[n] = r + 16 * n + p.c < rows ? lse_at[lse_from[n]] : INFINITY;
       }
-#pragma unroll
-      for (int i = 0; i < M::kLoads; ++i) from[i] += q_step;
-#pragma unroll
-      for (int n = 0; n < M::kTiles; ++n) lse_at[n] += lse_step;
+      q_at += (int64_t)dt * q_t + dh * q_h;
+      lse_at += (int64_t)dt * a.Hq + dh;
       if (dh > 0) {
 #pragma unroll
         for (int i = 0; i < M::kLoads; ++i) {
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(kThreads, 2) void page_weights_many_kernel(const Pa
         if (dh > 0) {
           own_h[n] += dh;
           own_t[n] += own_h[n] >= a.G ? 1 : 0;
-          lse_at[n] += own_h[n] >= a.G ? lse_wrap : 0;
+          lse_from[n] += own_h[n] >= a.G ? a.Hq - a.G : 0;
           own_h[n] -= own_h[n] >= a.G ? a.G : 0;
         }
       }
@@ -560,11 +560,21 @@ __global__ __launch_bounds__(kThreads, 2) void page_weights_many_kernel(const Pa
   }
 }
 
+template <int ET, int NR>
+void launch_few(const PageWeightsArgs& a, const WeightsForm& f, hipStream_t s) {
+  page_weights_few_kernel<ET, NR><<<(unsigned)f.workgroups, kThreads, 0, s>>>(a);
+}
 template <int ET>
 hipError_t launch(const PageWeightsArgs& a, const WeightsForm& f, hipStream_t s) {
-  if (f.rows == 16) page_weights_few_kernel<ET, 1><<<(unsigned)f.workgroups, kThreads, 0, s>>>(a);
-  else if (f.rows == 32 && ET != kFP32) page_weights_few_kernel<ET == kFP32 ? kBF16 : ET, 2><<<(unsigned)f.workgroups, kThreads, 0, s>>>(a);
-  else page_weights_many_kernel<ET><<<(unsigned)f.workgroups, kThreads, 0, s>>>(a);
+  if (f.many) {
+    page_weights_many_kernel<ET><<<(unsigned)f.workgroups, 64 * kWeightsManyWaves, 0, s>>>(a);
+  } else if (f.rows == 16) {
+    launch_few<ET, 1>(a, f, s);
+  } else if constexpr (ET != kFP32) {                      // (sixteen rows of float32 at most)
+    if (f.rows == 32) launch_few<ET, 2>(a, f, s);
+    else if (f.rows == 64) launch_few<ET, 4>(a, f, s);
+    else launch_few<ET, 8>(a, f, s);
+  }
   return hipGetLastError();
 }
 

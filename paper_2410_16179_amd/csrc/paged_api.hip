@@ -285,6 +285,7 @@ int magicpig_page_weights(const Params* p, const void* q, const void* k_pages, c
     return MAGICPIG_INVALID_ARG;
   const mp::WeightsForm f = weights_form_of(p, token_start != nullptr);
   if (!mp::weights_fit(f)) return MAGICPIG_UNSUPPORTED;
+  if (p->q_stride_token > (1 << 22) || p->q_stride_head > (1 << 22)) return MAGICPIG_UNSUPPORTED;   // (a tile's rows lie within 2^31 bytes)
   (void)workspace_bytes;
   if (p->batch == 0) return MAGICPIG_OK;
   mp::PageWeightsArgs a{};

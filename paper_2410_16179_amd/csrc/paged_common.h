@@ -69,7 +69,7 @@ struct PagedArgs {
 struct PageWeightsArgs {
   PagedArgs paged;
   const float* lse; const int* counted; float* weights;
-  int heads;              // few rows: KV heads that a workgroup takes at once; many: shares of the rows
+  int heads;              // KV heads that a workgroup takes at once; many rows: shares of the rows
 };
 
 // Which keys stay (page_keep.hip).
