@@ -417,14 +417,16 @@ MAGICPIG_API int magicpig_paged_attention_mxfp(const magicpig_paged_params* para
  *   weights(i, g) = (i < counted[b] ? weights(i, g) : 0) + sum over tokens and query heads h of g with i in A: exp(scale q.k_i - lse);
  * counted [batch] int32: so many of the request's keys have an account (clamped to [0, lengths[b]]); NULL: all but the new tokens' own.
  * A row whose lse is -inf adds nothing.  k_scale as in magicpig_paged_attention (e4m3), k_block_scales with kv_dtype MAGICPIG_KV_MXFP4;
- * NULL otherwise.  Accounts of keys that no token attends may be written with their own value.  Sums are taken in an order that depends on the
- * parameters and lengths alone.  MAGICPIG_UNSUPPORTED where batch * n_kv_heads * max_pages * page_size is 2^35 (float32: 2^34) or more. */
+ * NULL otherwise.  What lies in a key that a token does not attend does not reach its sum; keys of pages that are none have no account.  Accounts of keys
+ * that no token attends may be written with their own value.  Sums are taken in an order that depends on the parameters and lengths alone.
+ * MAGICPIG_UNSUPPORTED where batch * n_kv_heads * max_pages * page_size is 2^36 (float32: 2^35) or more, or a stride of q above 2^22.  No workspace is
+ * needed (NULL); magicpig_page_evict needs none either, magicpig_page_keep for few requests of more than 24576 keys at most. */
 MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, const void* q, const void* k_pages, const float* k_scale,
                                        const uint8_t* k_block_scales, const int32_t* block_table, const int32_t* lengths,
                                        const int32_t* token_start, const float* lse, const int32_t* counted, float* weights,
                                        void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Request b is left with stay = min(lengths[b], budgets[b], max_keep) keys, or stays as it is where budgets[b] < 0 or lengths[b] <= min(budgets[b], max_keep).
+/* Lengths are clamped to [0, max_pages * page_size].  Request b is left with stay = min(lengths[b], budgets[b], max_keep) keys, or stays as it is where budgets[b] < 0 or lengths[b] <= min(budgets[b], max_keep).
  * kept [batch, n_kv_heads, max_keep] int32 gets, in ascending order, the keys of each head that stay, and -1 behind them (in all
  * entries of a request that stays as it is): the first n_first keys and the last n_last, then those of the largest accounts; of equal ones (both zeros are) the first; an
  * account that is NaN, or lies on a page that is none, comes below all others.  Where the first and the last are more than stay, the first stay of them.
