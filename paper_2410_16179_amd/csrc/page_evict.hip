@@ -4,7 +4,7 @@
 namespace mp {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kUnroll = 8;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kUnroll = 4;
 
 __device__ inline int pages_of(int keys, int shift) { return (int)(((int64_t)keys + (1 << shift) - 1) >> shift); }
 
@@ -67,18 +67,28 @@ __device__ inline void give_back(const PageEvictArgs& a, int n_free, bool fits, 
 // A workgroup takes one array (keys, values, their block scales, accounts) of one request and KV head, or a slice of its rows, and goes over the
 // keys that stay in order.  Row j comes from row kept[j] >= j: what a tile of rows overwrites are sources of its own rows and of earlier ones,
 // never of later ones.  So a tile's rows are read by all of the workgroup before one of them is written, and later tiles may be on their way.
+// Loads come back in the order in which they were asked for, so nothing that is needed at once is asked for behind a tile's rows: page ids come from LDS, the
+// list of the tile after next before the next one's rows; and all loads are made by all lanes (those without a row read the first one), so that their number is known.
+// (Where a page's rows begin is multiplied out once for each page: for each row it took longer than the rows did.)
+constexpr int kTable = 4096;                               // pages in LDS; longer requests look in memory
 template <class Part>
-__device__ inline void move_rows(const PageEvictArgs& a, const PagedArray& r, int b, int g, int64_t slice) {
+__device__ inline void move_rows(const PageEvictArgs& a, const PagedArray& r, int b, int g, int64_t slice, int64_t* pages) {
   constexpr int kPart = sizeof(Part);
-  const int len = a.lengths[b], stay = a.stay[b];
+  const int len = a.lengths[b], stay = a.stay[b], held = pages_of(len, a.page_shift), mask = (1 << a.page_shift) - 1;
+  if (stay == 0) return;
   const int* const kept = a.kept + ((int64_t)b * a.heads + g) * a.max_keep;
   const int* const table = a.table + (int64_t)b * a.max_pages;
+  const uint32_t key_bytes = (uint32_t)r.key;
+  const bool near = held <= kTable;
+  __syncthreads();                                         // (the last request's are done with)
+  auto page_at = [&](int i) {                              // -1: there is none
+    const int id = table[i];
+    return (uint32_t)id < (uint32_t)a.n_pages ? id * r.page : (int64_t)-1;
+  };
+  if (near)
+    for (int i = threadIdx.x; i < held; i += kThreads) pages[i] = page_at(i);
   const int lanes = r.slice / kPart, step = kThreads / lanes, row0 = threadIdx.x / lanes, tile = step * kUnroll;
   char* const base = r.at + g * r.head + slice * r.slice + (threadIdx.x - row0 * lanes) * kPart;
-  auto place = [&](int key) -> char* {
-    const int id = table[key >> a.page_shift];
-    return (uint32_t)id < (uint32_t)a.n_pages ? base + id * r.page + (key & ((1 << a.page_shift) - 1)) * r.key : nullptr;
-  };
   // the first key that moves: kept[j] == j up to it, and nowhere behind
   int lo = 0, hi = stay;
   while (lo < hi) {
@@ -90,44 +100,52 @@ __device__ inline void move_rows(const PageEvictArgs& a, const PagedArray& r, in
     hi = min(hi, lo + f * each);
     lo = low;
   }
+  __syncthreads();
+  // where a key's row is; a key on a page that is none has none
+  auto place = [&](int key, bool& there) -> char* {
+    const int64_t page = near ? pages[key >> a.page_shift] : page_at(key >> a.page_shift);
+    there = page >= 0;
+    return base + (there ? page : 0) + (uint32_t)(key & mask) * key_bytes;   // (below 2^31 within a page)
+  };
   // three steps in flight: a tile's list, its rows, its writing
   Part now[kUnroll], next[kUnroll];
-  int from[kUnroll];
-  auto list = [&](int j0) {
+  int from[kUnroll], after[kUnroll];
+  auto list = [&](int j0, int (&to)[kUnroll]) {
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i) {
-      const int j = j0 + row0 + i * step;
-      from[i] = j < stay ? kept[j] : -1;
-    }
+    for (int i = 0; i < kUnroll; ++i) to[i] = kept[min(j0 + row0 + i * step, stay - 1)];
   };
   auto fetch = [&](int j0, Part (&to)[kUnroll]) {
-    uint32_t there = 0;
+    uint32_t moves = 0;
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
       const int j = j0 + row0 + i * step;
-      const char* src = from[i] > j && from[i] < len ? place(from[i]) : nullptr;
-      if (src) {
-        to[i] = *reinterpret_cast<const Part*>(src);
-        there |= 1u << i;
-      }
+      bool there;
+      const bool real = j < stay && from[i] > j && from[i] < len;
+      const char* src = place(real ? from[i] : 0, there);
+      to[i] = *reinterpret_cast<const Part*>(src);
+      moves |= real && there ? 1u << i : 0u;
     }
-    return there;
+    return moves;
   };
   int j0 = __builtin_amdgcn_readfirstlane(lo);
-  list(j0);
+  list(j0, from);
+  list(j0 + tile, after);
   uint32_t here = fetch(j0, now);
-  list(j0 + tile);
 #pragma unroll 1
   for (; j0 < stay; j0 += tile) {
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) from[i] = after[i];
+    list(j0 + 2 * tile, after);
     const uint32_t ahead = fetch(j0 + tile, next);
-    list(j0 + 2 * tile);
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) asm volatile("" : "+v"(now[i]));   // (read before the barrier)
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
-      char* to = here >> i & 1 ? place(j0 + row0 + i * step) : nullptr;
-      if (to) *reinterpret_cast<Part*>(to) = now[i];
+      bool there = false;
+      char* to = nullptr;
+      if (here >> i & 1) to = place(j0 + row0 + i * step, there);
+      if (there) *reinterpret_cast<Part*>(to) = now[i];
       now[i] = next[i];
     }
     here = ahead;
@@ -145,6 +163,7 @@ __global__ __launch_bounds__(kThreads) void page_evict_kernel(const PageEvictArg
     return;
   }
   if (!fits) return;
+  __shared__ int64_t pages_at[kTable];
   const int64_t all = (int64_t)a.batch * a.heads * jobs;
 #pragma unroll 1
   for (int64_t n = (int64_t)blockIdx.x - books; n < all; n += gridDim.x - books) {
@@ -154,8 +173,8 @@ __global__ __launch_bounds__(kThreads) void page_evict_kernel(const PageEvictArg
     if (a.stay[b] == a.lengths[b]) continue;
     while (job >= a.arrays[array].slices) job -= a.arrays[array++].slices;
     const PagedArray r = a.arrays[array];
-    if (r.slice == 4) move_rows<uint32_t>(a, r, b, g, job);
-    else move_rows<u32x4>(a, r, b, g, job);
+    if (r.slice == 4) move_rows<uint32_t>(a, r, b, g, job, pages_at);
+    else move_rows<u32x4>(a, r, b, g, job, pages_at);
   }
 }
 
