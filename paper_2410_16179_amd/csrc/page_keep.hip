@@ -251,7 +251,8 @@ __device__ inline void fill_behind(const PageKeepArgs& a, const Row& r) {
   for (int j = (r.stay == r.len ? 0 : r.stay) + (int)threadIdx.x; j < a.max_keep; j += THREADS) r.kept[j] = -1;
 }
 
-// A workgroup per request and KV head.
+// A workgroup per request and KV head.  Bound by one compute unit's instructions and its chain of reads, counts and barriers: 64 requests of 500 to 9001 keys, eight
+// heads each (7.5 MB), 19.4 us with 512 threads (256: 26.2, 1024: 25.9); one of 98304 keys 65, of which counting 14, listing 15, writing 30.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void page_keep_kernel(const PageKeepArgs a) {
   __shared__ __align__(16) Counts counts;
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(THREADS) void page_keep_kernel(const PageKeepArgs a
 // ---- few long requests: several workgroups to a KV head, in three launches --------------------------------
 // First each counts its part's first digits; then each adds the counts up, finds the digit of the bar, and lists its part's ranks of that digit; then each finds
 // the bar from all lists, knows from them how many keys of earlier parts stay, and writes its own.  Where too many ranks share the digit, the first
-// workgroup does all of it by itself.
+// workgroup does all of it by itself.  One request of 98304 keys, eight heads: 4.5 + 9.7 + 12.6 us, 65 by one workgroup a head.
 constexpr int kPartThreads = 512;
 
 struct Part {

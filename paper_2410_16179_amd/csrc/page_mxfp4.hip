@@ -6,7 +6,9 @@ namespace {
 
 // Sixteen lanes take a row of 128 elements, eight a lane, of the keys and of the values; a quad of lanes has a block of 32.  The scale is
 // the least power of two 2^e with max |x| <= 6 * 2^e: with max = 1.m * 2^k, e = k - 2, or k - 1 where 1.m is over 1.5.  Division by it and
-// rounding (to nearest, ties to the even code) are one instruction for two elements.  Bound by memory.
+// rounding (to nearest, ties to the even code) are one instruction for two elements.  Bound by memory: 16384 tokens of eight heads, 15360 of them with a slot
+// (80 MB either way), are stored in 19.4 us, 4.1 TB/s, and read back in 14.3, 5.6 TB/s (four lanes a row, 64 bytes in a lane: 25.6 and 24.1); 64 tokens
+// 3.9 and 3.1 us, a launch.
 
 // Magnitudes above 3 * 2^126 as that: their scale is 2^126, of which 4 would be an infinity again.
 __device__ inline uint32_t bounded(uint32_t two) {
