@@ -71,7 +71,7 @@ __device__ inline void give_back(const PageEvictArgs& a, int n_free, bool fits, 
 // list of the tile after next before the next one's rows; and all loads are made by all lanes (those without a row read the first one), so that their number is known.
 // (Where a page's rows begin is multiplied out once for each page: for each row it took longer than the rows did.)
 // Bound by memory: 32 requests of up to 4160 keys back to 4096 (e4m3, 537 MB moved) 129 us, 4.2 TB/s (154 with page ids asked for behind the rows); one request's
-// 32768 keys to 8192 (67 MB) 37 to 42 us, 1.7 TB/s: rows of 256 bytes in slices of 64, or too few workgroups would be at it (whole rows 103 us, slices of 128 44, of 32 48).
+// 32768 keys to 8192 (67 MB) 30 us, 2.2 TB/s: rows of 256 bytes in slices of 32, or too few workgroups would be at it (whole rows 103 us).
 constexpr int kTable = 4096;                               // pages in LDS; longer requests look in memory
 template <class Part>
 __device__ inline void move_rows(const PageEvictArgs& a, const PagedArray& r, int b, int g, int64_t slice, int64_t* pages) {
@@ -166,11 +166,11 @@ __global__ __launch_bounds__(kThreads) void page_evict_kernel(const PageEvictArg
   }
   if (!fits) return;
   __shared__ int64_t pages_at[kTable];
-  const int64_t all = (int64_t)a.batch * a.heads * jobs;
+  const int64_t units = (int64_t)a.batch * a.heads, all = units * jobs;
 #pragma unroll 1
   for (int64_t n = (int64_t)blockIdx.x - books; n < all; n += gridDim.x - books) {
-    const int64_t unit = n / jobs;
-    int job = (int)(n - unit * jobs), array = 0;
+    int job = (int)(n / units), array = 0;                 // (the slices of a unit's rows, which share lines, on one XCD where units go with eight)
+    const int64_t unit = n - job * units;
     const int b = (int)(unit / a.heads), g = (int)(unit - (int64_t)b * a.heads);
     if (a.stay[b] == a.lengths[b]) continue;
     while (job >= a.arrays[array].slices) job -= a.arrays[array++].slices;

@@ -309,6 +309,7 @@ int magicpig_page_keep(const Params* p, const float* weights, const int32_t* blo
   const int st = check(p);
   if (st != MAGICPIG_OK) return st;
   if (n_first < 0 || n_last < 0 || max_keep < 1) return MAGICPIG_INVALID_ARG;
+  if (max_keep > (1 << 30)) return MAGICPIG_UNSUPPORTED;   // (no request has more keys)
   if ((int64_t)p->batch * p->n_kv_heads * 1024 >= (int64_t)1 << 32) return MAGICPIG_UNSUPPORTED;   // (threads of a grid)
   if (p->batch > 0 && (!weights || !block_table || !lengths || !budgets || !kept || !lengths_out)) return MAGICPIG_INVALID_ARG;
   if (!aligned16(weights) || !aligned(block_table, 4) || !aligned(lengths, 4) || !aligned(budgets, 4) || !aligned(kept, 4) ||
@@ -334,6 +335,7 @@ int magicpig_page_evict(const Params* p, const int32_t* kept, int32_t max_keep, 
   if (st != MAGICPIG_OK) return st;
   if ((st = check_pools(p)) != MAGICPIG_OK) return st;
   if (kept && max_keep < 1) return MAGICPIG_INVALID_ARG;
+  if (kept && max_keep > (1 << 30)) return MAGICPIG_UNSUPPORTED;
   if (!free_pages || !n_free || !n_free_out || !status || !k_pages || !v_pages) return MAGICPIG_INVALID_ARG;
   if (p->batch > 0 && (!lengths || !lengths_kept || !block_table)) return MAGICPIG_INVALID_ARG;
   if (four(p) ? !k_block_scales || !v_block_scales : k_block_scales || v_block_scales) return MAGICPIG_INVALID_ARG;

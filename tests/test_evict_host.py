@@ -87,6 +87,7 @@ def test_numbers():
     for name in ("n_first", "n_last"):
         assert keep(p, **{name: -1}) == INVALID
     assert keep(p, max_keep=0) == INVALID and evict(p, max_keep=0) == INVALID
+    assert keep(p, max_keep=(1 << 30) + 1) == evict(p, max_keep=(1 << 30) + 1) == UNSUPPORTED
     assert keep(params(batch=65536, n_q_heads=1024, n_kv_heads=1024)) == UNSUPPORTED
     # (more tiles than are counted in 31 bits)
     assert weigh(params(batch=65536, max_pages=1 << 20, n_q_heads=64, n_kv_heads=64)) == UNSUPPORTED

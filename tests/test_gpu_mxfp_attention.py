@@ -115,6 +115,13 @@ def test_one_token_per_request(heads, kv_heads, page, layout):
     Problem(heads=heads, kv_heads=kv_heads, page=page, lengths=EDGES, layout=layout, seed=page + heads).check()
 
 
+@pytest.mark.parametrize("page", [128, 1024])
+@pytest.mark.parametrize("new", [None, [5, 1, 3], [60, 1, 64]])
+def test_large_pages(page, new):
+    Problem(heads=8, kv_heads=2, page=page, lengths=[2100, 1, 1024], new=new, n_local=0, seed=page).check()
+    Problem(heads=8, kv_heads=2, page=page, lengths=[2100, 1, 1024], new=new, n_sink=70, n_local=300, seed=page).check()
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(20, 1), (64, 1), (128, 2)])
 def test_more_heads_per_kv_head_than_a_tile_has_rows(heads, kv_heads):
     Problem(heads=heads, kv_heads=kv_heads, page=32, lengths=[40, 0, 513], seed=heads).check()
