@@ -219,6 +219,10 @@ inline int evict_slice(int row, int64_t units) {
 // them, 32 of which go by at a time, the keys in registers.  heads: KV heads that a workgroup's wavefronts take at once; many: shares that they split the rows
 // into; tiles: of keys, at most, all KV heads together; workgroups: what is resident at once; many: at most.
 constexpr int kWeightsManyWaves = 4;         // wavefronts of a workgroup, many rows
+// Rows from which on they split them; where there are few tiles they do so sooner.  Measured, us, 16 requests of 32768 keys, 32 heads over 8, split from 128 rows on | from
+// 512 | 1024 | 4096: 160 rows 968 | 425 | 425 | 426, 512 rows 1353 | 1043 | 878 | 878, 1024 rows 1995 | 1984 | 1686 | 1536, 2048 rows - | 3307 | 3306 | 2844; one request of 4096
+// keys, 256 rows: split 12.3, not 19.2.
+constexpr int kWeightsShareRows = 4096;
 constexpr int weights_tile(bool fp32, int bits, int rows) { return fp32 ? 16 : (bits == 16 || rows > 16 ? 32 : 64); }   // keys of a tile, few rows
 struct WeightsForm {
   bool many;
@@ -235,9 +239,11 @@ inline WeightsForm weights_form(int batch, int kv_heads, int group, bool fp32, i
   int tile = weights_tile(fp32, bits, f.rows);
   int64_t most = (f.rows <= 32 ? 2 : 1) * kNumCU;
   if (f.many) {
-    // (a share of two tiles of sixteen rows at least)
-    while (f.heads < kWeightsManyWaves && 64 * f.heads <= rows) f.heads *= 2;
-    tile = (fp32 ? 32 : 64) * (kWeightsManyWaves / f.heads);
+    // a workgroup's wavefronts split the rows of one tile of keys, or have tiles of their own
+    const int own = fp32 ? 32 : 64;
+    auto blocks = [&](int shares) { return (max_len + own * (kWeightsManyWaves / shares) - 1) / (own * (kWeightsManyWaves / shares)) * batch * kv_heads; };
+    while (f.heads < kWeightsManyWaves && 64 * f.heads <= rows && (kWeightsShareRows * f.heads <= rows || blocks(f.heads) < 2 * kNumCU)) f.heads *= 2;
+    tile = own * (kWeightsManyWaves / f.heads);
     most = 1 << 14;
   } else {
     while (f.heads < 8 && kv_heads % (2 * f.heads) == 0) f.heads *= 2;

@@ -216,7 +216,7 @@ __device__ inline float* account(const PageWeightsArgs& a, const Place& p, int g
 // known first, and a key's sum over the rows is one over registers and sixteen lanes.  Every key belongs to one wavefront: no atomics, and the same bits
 // every time.  Workgroups take equal, contiguous shares of all tiles; the wavefronts of one take `heads` neighbouring KV heads, whose rows lie side by side in
 // many pools, and waves / heads tiles at a time.  Bound by memory: 16 requests of 32768 keys, four rows (bf16, 1.11 GB) 194 us, 5.7 TB/s; 32 rows 203, 64 rows
-// 215, 128 rows 376 (their exponentials); e4m3 113, four bits 91 (3.2 TB/s: widening), float32, 8 requests, 182, 6.0 TB/s.  64 rows by the form for many 476, 128 rows 862.
+// 215, 128 rows 376 (their exponentials); e4m3 113, four bits 91 (3.2 TB/s: widening), float32, 8 requests, 182, 6.0 TB/s.  64 rows by the form for many 476, 128 rows 862 (its rows then split among wavefronts).
 template <int ET, int NR>
 __global__ __launch_bounds__(kThreads, NR <= 2 ? 4 : 2) void page_weights_few_kernel(const PageWeightsArgs w) {
   using T = Tile<ET, NR>;

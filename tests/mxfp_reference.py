@@ -11,9 +11,8 @@ def quantise(x):
     x = np.asarray(x, np.float64).reshape(*x.shape[:-1], 4, 32)
     top = np.abs(x).max(-1)
     fine = np.isfinite(top)
-    e = np.full(top.shape, -127)
-    for k in range(-126, 127):                                # the least power of two that leaves no element above 6
-        e = np.where(top > 6 * 2.0 ** (k - 1), k, e)
+    m, k = np.frexp(np.where(fine, top, 0.0))                 # top = m 2^k with m in [0.5, 1): the least e with top <= 0.75 * 2^(e + 3)
+    e = np.where((top > 0) & fine, np.maximum(np.where(m <= 0.75, k - 3, k - 2), -127), -127)
     y = np.minimum(np.abs(np.where(fine[..., None], x, 0.0)), 3 * 2.0 ** 126) / 2.0 ** e[..., None].astype(np.float64)
     off = np.abs(y[..., None] - GRID)
     # the nearest, of two as near the one of even code
