@@ -17,12 +17,12 @@ class Problem:
     """A paged cache with random keys in the slots that requests hold and NaN in all others; accounts are random everywhere."""
 
     def __init__(self, *, kind, heads, kv_heads, page, lengths, new=None, layout="token", n_sink=0, n_local=0, scale=0.0, seed=0, spread=1.0,
-                 spare_rows=0, bad=(), counted=None):
+                 spare_rows=0, bad=(), counted=None, table_width=0):
         rng = np.random.default_rng(seed)
         self.kind, self.page, self.lengths, self.n_sink, self.n_local, self.scale, self.layout = kind, page, lengths, n_sink, n_local, scale, layout
         batch = len(lengths)
         held = [-(-n // page) for n in lengths]
-        max_pages, n_pages = max(max(held), 1) + 1, sum(held) + 3
+        max_pages, n_pages = max(max(max(held), 1) + 1, table_width), sum(held) + 3
         ids = rng.permutation(n_pages)[:sum(held)]
         self.table = np.full((batch, max_pages), -1, np.int32)
         used, at = np.zeros((n_pages, page), bool), 0
@@ -138,6 +138,15 @@ def test_long_caches(kind, lengths):
 def test_several_tokens(kind, heads, kv_heads, new):
     # (more new tokens than cached keys too: the first ones attend nothing)
     Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=16, lengths=[70, 2, 33, 5, 530], new=new, spare_rows=2, seed=7).check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("table_width", [60, 200, 700])
+@pytest.mark.parametrize("heads,kv_heads,new,n_local", [(32, 8, [50, 33], 0), (24, 8, [44, 50], 100), (40, 8, [1, 40], 0)])
+def test_many_rows_in_tables_of_many_widths(kind, table_width, heads, kv_heads, new, n_local):
+    # (the more keys the tables have room for the fewer wavefronts split a tile's rows)
+    Problem(kind=kind, heads=heads, kv_heads=kv_heads, page=32, lengths=[333, 700], new=new, n_local=n_local, n_sink=5 if n_local else 0,
+            table_width=table_width, seed=table_width).check()
 
 
 @pytest.mark.parametrize("kind", KINDS)
