@@ -252,6 +252,17 @@ inline WeightsForm weights_form(int batch, int kv_heads, int group, bool fp32, i
   f.workgroups = f.tiles < most ? (f.tiles > 0 ? f.tiles : 1) : most;
   return f;
 }
+// Many rows go by in steps of dt tokens and dh heads of a KV head's `group`.  The wavefront has a 64-bit pointer to the step's first row, a lane 32 bits from there to its own,
+// one of 32 behind it: both go on by the step, and by `wrap` (a token's stride less that of `group` heads) where their head goes past the last one.  So a lane's offset stays
+// within a token and 126 heads (one head a token: 31 tokens) of the pointer, below 2^31 bytes with strides of up to 2^22 elements, however far the rows reach.
+constexpr bool next_head(int& head, int dh, int group) {   // whether it goes past the last one
+  head += dh;
+  const bool past = head >= group;
+  head -= past ? group : 0;
+  return past;
+}
+constexpr int offset_step(bool past, bool first_past, int wrap) { return (past ? wrap : 0) - (first_past ? wrap : 0); }
+
 // Tiles are counted in 31 bits.
 inline bool weights_fit(const WeightsForm& f) { return f.tiles <= INT32_MAX - 1024; }
 

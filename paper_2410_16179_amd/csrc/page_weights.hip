@@ -415,9 +415,11 @@ __global__ __launch_bounds__(64 * kWeightsManyWaves, 2) void page_weights_many_k
     if (a.n_local > 0 && key0 >= a.n_sink) t_end = (int)min((int64_t)t_end, (int64_t)key0 + M::kKeys - 1 + a.n_local - old);
     const int r_end = key0 < x.len ? max(t_end, 0) * a.G : 0, r_begin = max(key0 - old, 0) * a.G / 16 * 16 + M::kRows * share, r_step = M::kRows * row_split;
     // This lane's rows: those it loads a part of, and its column's.  They go on by r_step rows, dt tokens and dh heads.  Addresses are a pointer of the
-    // wavefront's, to the first row's token, and a lane's offset, which changes where a row's head goes past the last one.  (Multiplied out they took longer
+    // wavefront's, which goes with the first row, and a lane's offset from there (see next_head).  (Multiplied out they took longer
     // than the products did; 64-bit ones for each lane took registers that kept a wavefront from the compute unit.)
     const int dt = r_step / a.G, dh = r_step - dt * a.G, t0 = r_begin / a.G;
+    int first_head = r_begin - t0 * a.G;
+    bool first_past = false;                               // whether the first row's head went past the last one in the step of the last fetch
     constexpr int kElem = M::kF32 ? 4 : 2, kRowLanes = 64 / M::kPerLoad;
     const int part = p.lane & (kRowLanes - 1);             // of a row's sixteen bytes, those of this lane
     const char* q_at = reinterpret_cast<const char*>(a.q) + ((x.row + (int64_t)t0) * a.q_t + (int64_t)g * a.G * a.q_h) * kElem;
@@ -451,15 +453,12 @@ __global__ __launch_bounds__(64 * kWeightsManyWaves, 2) void page_weights_many_k
 #pragma unroll
         for (int n = 0; n < M::kTiles; ++n) next_lse[n] = r + 16 * n + p.c < rows ? lse_at[lse_from[n]] : INFINITY;
       }
-      q_at += (int64_t)dt * q_t + dh * q_h;
-      lse_at += (int64_t)dt * a.Hq + dh;
+      first_past = next_head(first_head, dh, a.G);
+      q_at += (int64_t)dt * q_t + dh * q_h + (first_past ? q_wrap : 0);
+      lse_at += (int64_t)dt * a.Hq + dh + (first_past ? a.Hq - a.G : 0);
       if (dh > 0) {
 #pragma unroll
-        for (int i = 0; i < M::kLoads; ++i) {
-          head[i] += dh;
-          from[i] += head[i] >= a.G ? q_wrap : 0;
-          head[i] -= head[i] >= a.G ? a.G : 0;
-        }
+        for (int i = 0; i < M::kLoads; ++i) from[i] += offset_step(next_head(head[i], dh, a.G), first_past, q_wrap);
       }
     };
     float s[M::kValues];
@@ -489,10 +488,9 @@ __global__ __launch_bounds__(64 * kWeightsManyWaves, 2) void page_weights_many_k
         last = old + __builtin_amdgcn_readlane(own_t[n], 15);
         own_t[n] += dt;
         if (dh > 0) {
-          own_h[n] += dh;
-          own_t[n] += own_h[n] >= a.G ? 1 : 0;
-          lse_from[n] += own_h[n] >= a.G ? a.Hq - a.G : 0;
-          own_h[n] -= own_h[n] >= a.G ? a.G : 0;
+          const bool past = next_head(own_h[n], dh, a.G);
+          own_t[n] += past ? 1 : 0;
+          lse_from[n] += offset_step(past, first_past, a.Hq - a.G);
         }
       }
       if (r0 + r_step < r_end) fetch(r0 + r_step);
