@@ -430,7 +430,7 @@ MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, cons
  * kept [batch, n_kv_heads, max_keep] int32 gets, in ascending order, the keys of each head that stay, and -1 behind them (in all
  * entries of a request that stays as it is): the first n_first keys and the last n_last, then those of the largest accounts; of equal ones (both zeros are) the first; an
  * account that is NaN, or lies on a page that is none, comes below all others.  Where the first and the last are more than stay, the first stay of them.
- * lengths_out [batch] int32 gets stay, or the length.  max_keep is 1 .. 2^30. */
+ * lengths_out [batch] int32 gets stay, or the length (may be `lengths` or `budgets`).  max_keep is 1 .. 2^30. */
 MAGICPIG_API int magicpig_page_keep(const magicpig_paged_params* params, const float* weights, const int32_t* block_table,
                                     const int32_t* lengths, const int32_t* budgets, int32_t n_first, int32_t n_last, int32_t max_keep,
                                     int32_t* kept, int32_t* lengths_out, void* workspace, size_t workspace_bytes, void* hip_stream);

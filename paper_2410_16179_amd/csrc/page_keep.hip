@@ -22,13 +22,21 @@ struct Row {
   int len, stay, first, last;                            // keys [first, last) are chosen by their accounts, `want` of them
   int want;
 };
-__device__ inline Row row_of(const PageKeepArgs& a, int b, int g) {
+// A request's keys, and those that stay.
+struct Size {
+  int len, stay;
+};
+__device__ inline Size size_of(const PageKeepArgs& a, int b) {
   int len = a.lengths[b];
   len = len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
   const int budget = a.budgets[b], most = budget < a.max_keep ? budget : a.max_keep;
-  Row r{a.table + (int64_t)b * a.max_pages, a.weights + ((int64_t)g << a.page_shift), a.kept + ((int64_t)b * a.heads + g) * a.max_keep, len, 0, a.n_first,
+  return Size{len, budget < 0 || len <= most ? len : most};
+}
+__device__ inline Row row_of(const PageKeepArgs& a, int b, int g) {
+  const Size n = size_of(a, b);
+  const int len = n.len;
+  Row r{a.table + (int64_t)b * a.max_pages, a.weights + ((int64_t)g << a.page_shift), a.kept + ((int64_t)b * a.heads + g) * a.max_keep, len, n.stay, a.n_first,
         len - a.n_last, 0};
-  r.stay = budget < 0 || len <= most ? len : most;
   if (r.first >= r.last) r.first = r.last = len;           // (no key is chosen by its account)
   r.want = max(r.stay - (len - (r.last - r.first)), 0);
   return r;
@@ -259,7 +267,7 @@ __global__ __launch_bounds__(THREADS) void page_keep_kernel(const PageKeepArgs a
   __shared__ uint32_t list[kList];
   const int b = blockIdx.x / a.heads, g = blockIdx.x - b * a.heads;
   const Row r = row_of(a, b, g);
-  if (g == 0 && threadIdx.x == 0) a.lengths_out[b] = r.stay;
+  if (a.lengths_out && g == 0 && threadIdx.x == 0) a.lengths_out[b] = r.stay;
   if (r.stay < r.len) {
     Ranks held;
     uint32_t bar = 0;
@@ -301,7 +309,7 @@ __global__ __launch_bounds__(kPartThreads) void page_keep_parts_kernel(const Pag
   Part* const parts = reinterpret_cast<Part*>(a.workspace) + (int64_t)row * a.parts;
   const Row r = row_of(a, b, g);
   if (STEP == 2 && part == 0) {
-    if (g == 0 && threadIdx.x == 0) a.lengths_out[b] = r.stay;
+    if (a.lengths_out && g == 0 && threadIdx.x == 0) a.lengths_out[b] = r.stay;
     fill_behind<kPartThreads>(a, r);
   }
   if (r.stay == r.len || (STEP < 2 && r.want == 0)) return;
@@ -391,9 +399,18 @@ __global__ __launch_bounds__(kPartThreads) void page_keep_parts_kernel(const Pag
   }
 }
 
+// Lengths that are written where lengths or budgets are read: in a launch of their own behind all workgroups that read them.
+__global__ __launch_bounds__(256) void page_keep_lengths_kernel(const PageKeepArgs a, int* out) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b < a.batch) out[b] = size_of(a, b).stay;
+}
+
 }  // namespace
 
-hipError_t launch_page_keep(const PageKeepArgs& a, int64_t rows, hipStream_t s) {
+hipError_t launch_page_keep(const PageKeepArgs& args, int64_t rows, hipStream_t s) {
+  PageKeepArgs a = args;
+  const bool in_place = a.lengths_out == a.lengths || a.lengths_out == a.budgets;
+  if (in_place) a.lengths_out = nullptr;
   if (a.parts > 1) {
     const unsigned n = (unsigned)(rows * a.parts);
     page_keep_parts_kernel<0><<<n, kPartThreads, 0, s>>>(a);
@@ -404,6 +421,7 @@ hipError_t launch_page_keep(const PageKeepArgs& a, int64_t rows, hipStream_t s) 
   } else {
     page_keep_kernel<1024><<<(unsigned)rows, 1024, 0, s>>>(a);
   }
+  if (in_place) page_keep_lengths_kernel<<<(unsigned)((a.batch + 255) / 256), 256, 0, s>>>(a, args.lengths_out);
   return hipGetLastError();
 }
 
