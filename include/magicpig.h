@@ -419,6 +419,9 @@ MAGICPIG_API int magicpig_paged_attention_mxfp(const magicpig_paged_params* para
  * A row whose lse is -inf adds nothing.  k_scale as in magicpig_paged_attention (e4m3), k_block_scales with kv_dtype MAGICPIG_KV_MXFP4;
  * NULL otherwise.  What lies in a key that a token does not attend does not reach its sum; keys of pages that are none have no account.  Accounts of keys
  * that no token attends may be written with their own value.  Sums are taken in an order that depends on the parameters and lengths alone.
+ * A page that the tables name in two places, as where requests share a prompt's beginning, has no defined accounts behind the call (its places' sums
+ * are not joined, and may differ from call to call); all other accounts are as said.  magicpig_page_keep does not look at accounts of the first
+ * n_first keys, so requests go on with such pages as long as n_first covers them.
  * MAGICPIG_UNSUPPORTED where batch * n_kv_heads * max_pages * page_size is 2^36 (float32: 2^35) or more, or a stride of q above 2^22.  No workspace is
  * needed (NULL); magicpig_page_evict needs none either, magicpig_page_keep for few requests of more than 24576 keys at most. */
 MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, const void* q, const void* k_pages, const float* k_scale,
@@ -442,7 +445,7 @@ MAGICPIG_API int magicpig_page_keep(const magicpig_paged_params* params, const f
  * request, are laid on the stack of free pages, requests in order, pages in order, and n_free_out [1] int32 (may be `n_free`) gets its height; the
  * block table stays as it is.  status [1] int32 gets 0, or -1 if an argument does not fit (a length below 0 or beyond the table's
  * row, lengths_kept above lengths or, with kept, above max_keep, a stack beyond n_pages): then nothing moves and nothing is handed back.  Pages
- * that two requests share are not to be evicted from. */
+ * that two requests share are not to be evicted from: kept[b, g, j] is j for all their keys, as n_first of magicpig_page_keep sees to. */
 MAGICPIG_API int magicpig_page_evict(const magicpig_paged_params* params, const int32_t* kept, int32_t max_keep, const int32_t* lengths,
                                      const int32_t* lengths_kept, const int32_t* block_table, int32_t* free_pages, const int32_t* n_free,
                                      void* k_pages, void* v_pages, uint8_t* k_block_scales, uint8_t* v_block_scales, float* weights,
