@@ -422,7 +422,8 @@ MAGICPIG_API int magicpig_paged_attention_mxfp(const magicpig_paged_params* para
  * A page that the tables name in two places, as where requests share a prompt's beginning, has no defined accounts behind the call (its places' sums
  * are not joined, and may differ from call to call); all other accounts are as said.  magicpig_page_keep does not look at accounts of the first
  * n_first keys, so requests go on with such pages as long as n_first covers them.
- * MAGICPIG_UNSUPPORTED where batch * n_kv_heads * max_pages * page_size is 2^36 (float32: 2^35) or more, or a stride of q above 2^22.  No workspace is
+ * Sizes batch * n_kv_heads * max_pages * page_size up to 2^35 (float32: 2^34) are always taken; larger ones are where the form that the types and rows
+ * call for counts their tiles of keys in 31 bits, else MAGICPIG_UNSUPPORTED, as with a stride of q above 2^22.  No workspace is
  * needed (NULL); magicpig_page_evict needs none either, magicpig_page_keep for few requests of more than 24576 keys at most. */
 MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, const void* q, const void* k_pages, const float* k_scale,
                                        const uint8_t* k_block_scales, const int32_t* block_table, const int32_t* lengths,
@@ -433,7 +434,8 @@ MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, cons
  * kept [batch, n_kv_heads, max_keep] int32 gets, in ascending order, the keys of each head that stay, and -1 behind them (in all
  * entries of a request that stays as it is): the first n_first keys and the last n_last, then those of the largest accounts; of equal ones (both zeros are) the first; an
  * account that is NaN, or lies on a page that is none, comes below all others.  Where the first and the last are more than stay, the first stay of them.
- * lengths_out [batch] int32 gets stay, or the length (may be `lengths` or `budgets`).  max_keep is 1 .. 2^30. */
+ * lengths_out [batch] int32 gets stay, or the length (may be `lengths` or `budgets`).  max_keep is 1 .. 2^30.
+ * MAGICPIG_UNSUPPORTED from batch * n_kv_heads = 2^22 on. */
 MAGICPIG_API int magicpig_page_keep(const magicpig_paged_params* params, const float* weights, const int32_t* block_table,
                                     const int32_t* lengths, const int32_t* budgets, int32_t n_first, int32_t n_last, int32_t max_keep,
                                     int32_t* kept, int32_t* lengths_out, void* workspace, size_t workspace_bytes, void* hip_stream);
