@@ -447,6 +447,7 @@ MAGICPIG_API int magicpig_page_keep(const magicpig_paged_params* params, const f
  * request, are laid on the stack of free pages, requests in order, pages in order, and n_free_out [1] int32 (may be `n_free`) gets its height; the
  * block table stays as it is.  status [1] int32 gets 0, or -1 if an argument does not fit (a length below 0 or beyond the table's
  * row, lengths_kept above lengths or, with kept, above max_keep, a stack beyond n_pages): then nothing moves and nothing is handed back.  Pages
+ * that are none keep their place in this: no key moves from or to one, and table entries are handed back as they are.  Pages
  * that two requests share are not to be evicted from: kept[b, g, j] is j for all their keys, as n_first of magicpig_page_keep sees to. */
 MAGICPIG_API int magicpig_page_evict(const magicpig_paged_params* params, const int32_t* kept, int32_t max_keep, const int32_t* lengths,
                                      const int32_t* lengths_kept, const int32_t* block_table, int32_t* free_pages, const int32_t* n_free,
