@@ -316,11 +316,12 @@ typedef struct magicpig_paged_params {
   int64_t v_new_stride_token, v_new_stride_head;          /* new values, alike */
 } magicpig_paged_params;
 
-/* Scratch that is enough for any of the three calls with these params (0 on invalid params), 16-byte
+/* Scratch that is enough for any of the paged calls with these params (0 on invalid params), 16-byte
  * aligned.  Its first MAGICPIG_PAGED_COUNTER_BYTES have to be zero before its first use; the calls leave them
  * zero again (they count, within magicpig_paged_attention, the parts of a row's sum that have arrived: a row whose count
  * starts elsewhere is left unwritten, or is written before all parts are there).  The rest need not be initialised or
- * preserved.  magicpig_page_plan needs a workspace for more than 2048 requests or 4096 token rows only. */
+ * preserved.  magicpig_page_plan needs a workspace for more than 2048 requests or 4096 token rows only, magicpig_page_keep where it has few requests of many
+ * keys (see there), and the calls that append, read, weigh or evict need none. */
 #define MAGICPIG_PAGED_COUNTER_BYTES 4096u
 MAGICPIG_API size_t magicpig_paged_workspace_bytes(const magicpig_paged_params* params);
 
@@ -385,7 +386,7 @@ MAGICPIG_API int magicpig_paged_attention(const magicpig_paged_params* params, c
  *
  * magicpig_page_append_mxfp stores rows k_new[t], v_new[t] in slot slots[t], as magicpig_page_append does.  A block's scale is the
  * least power of two, 2^-127 at least, that leaves no element above 6; elements are rounded to the nearest value, of two as near to the
- * one of even code.  Magnitudes above 3 * 2^126 count as that.  A block with an infinity or a NaN becomes NaN.
+ * one of even code, magnitudes above 3 * 2^126 (whose block's scale is 2^126) as that: 4 * 2^126 would be an infinity again.  A block with an infinity or a NaN becomes NaN.
  *
  * magicpig_page_read_mxfp is the way back: rows of slots slots[t], every t < max_tokens whose slot lies in the pool, as bf16
  * (exact, but that values of 2^128 and more become infinities) to k_out[t], v_out[t], [max_tokens, n_kv_heads, 128] with the strides of
@@ -424,7 +425,8 @@ MAGICPIG_API int magicpig_paged_attention_mxfp(const magicpig_paged_params* para
  * n_first keys, so requests go on with such pages as long as n_first covers them.
  * Sizes batch * n_kv_heads * max_pages * page_size up to 2^35 (float32: 2^34) are always taken; larger ones are where the form that the types and rows
  * call for counts their tiles of keys in 31 bits, else MAGICPIG_UNSUPPORTED, as with a stride of q above 2^22.  No workspace is
- * needed (NULL); magicpig_page_evict needs none either, magicpig_page_keep for few requests of more than 24576 keys at most. */
+ * needed, and none is looked at (NULL); so with magicpig_page_evict.  magicpig_page_keep takes one where batch * n_kv_heads is at most 32 and max_pages * page_size
+ * more than 24576 and at most 1044480. */
 MAGICPIG_API int magicpig_page_weights(const magicpig_paged_params* params, const void* q, const void* k_pages, const float* k_scale,
                                        const uint8_t* k_block_scales, const int32_t* block_table, const int32_t* lengths,
                                        const int32_t* token_start, const float* lse, const int32_t* counted, float* weights,

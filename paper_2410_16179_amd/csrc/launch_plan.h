@@ -206,7 +206,7 @@ inline int keep_parts(int64_t rows, int64_t max_len) {
 
 // ---- eviction ---------------------------------------------------------------------------------------
 // Bytes of a row that a workgroup moves: whole rows, or pieces of 32 bytes at least where requests times KV heads would leave compute units idle.
-// Measured, us, 32768 keys to 8192, bf16, eight heads, slices of 32 | 64 bytes: one request 30.4 | 32.8, four (which take 64) 79; with a unit's slices on
+// Measured, us, 32768 keys to 8192, bf16, eight heads, slices of 32 | 64 bytes: one request 30.4 | 32.8 (both on one card; slices of 32 take 32 to 33 on others), four (which take 64) 79; with a unit's slices on
 // different XCDs, slices of 64 | 128 | 256: one request 35.5 | 56 | 103, four 102 | 100 | 163.
 inline int evict_slice(int row, int64_t units) {
   int slice = row;

@@ -71,7 +71,7 @@ __device__ inline void give_back(const PageEvictArgs& a, int n_free, bool fits, 
 // list of the tile after next before the next one's rows; and all loads are made by all lanes (those without a row read the first one), so that their number is known.
 // (Where a page's rows begin is multiplied out once for each page: for each row it took longer than the rows did.)
 // Bound by memory: 32 requests of up to 4160 keys back to 4096 (e4m3, 537 MB moved) 129 us, 4.2 TB/s (154 with page ids asked for behind the rows); one request's
-// 32768 keys to 8192 (67 MB) 30 us, 2.2 TB/s: rows of 256 bytes in slices of 32, or too few workgroups would be at it (whole rows 103 us).
+// 32768 keys to 8192 (67 MB) 30.4 to 32.8 us over cards, 2.0 to 2.2 TB/s: rows of 256 bytes in slices of 32, or too few workgroups would be at it (whole rows 103 us).
 constexpr int kTable = 4096;                               // pages in LDS; longer requests look in memory
 template <class Part>
 __device__ inline void move_rows(const PageEvictArgs& a, const PagedArray& r, int b, int g, int64_t slice, int64_t* pages) {

@@ -216,7 +216,7 @@ __device__ inline float* account(const PageWeightsArgs& a, const Place& p, int g
 // known first, and a key's sum over the rows is one over registers and sixteen lanes.  Every key of a request belongs to one wavefront: no atomics, and the same bits
 // every time (a page that two requests name is added to by two: its accounts are not defined).  Workgroups take equal, contiguous shares of all tiles; the wavefronts of one take `heads` neighbouring KV heads, whose rows lie side by side in
 // many pools, and waves / heads tiles at a time.  Bound by memory: 16 requests of 32768 keys, four rows (bf16, 1.11 GB) 194 us, 5.7 TB/s; 32 rows 203, 64 rows
-// 215, 128 rows 376 (their exponentials); e4m3 113, four bits 91 (3.2 TB/s: widening), float32, 8 requests, 182, 6.0 TB/s.  64 rows by the form for many 476, 128 rows 862 (its rows then split among wavefronts).
+// 215, 128 rows 376 (their exponentials); e4m3 113 to 117, four bits 74 to 79 (4.1 to 4.3 TB/s: widening), float32, 8 requests, 182 to 184, 5.9 TB/s.  64 rows by the form for many 476, 128 rows 862 (its rows then split among wavefronts).
 template <int ET, int NR>
 __global__ __launch_bounds__(kThreads, NR <= 2 ? 4 : 2) void page_weights_few_kernel(const PageWeightsArgs w) {
   using T = Tile<ET, NR>;
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kThreads, NR <= 2 ? 4 : 2) void page_weights_few_ke
 // The keys stay in registers as bf16 (float32: 32 keys as they are), the rows come by: 32 at a time, loaded with neighbouring lanes on neighbouring addresses and
 // handed over in the wavefront's part of LDS, the next ones on their way.  The wavefronts of a workgroup are `row_split` shares of the rows, of one tile or of several.
 // Bound by the exponentials' and the products' cycles where there are many keys (2048 tokens behind 59392 keys, 32 heads over 8: 1.36 ms, 0.75 PFLOP/s) and by
-// the way of the rows from L2 and the wavefronts' ends where there are few: four prompts of up to 4099 tokens 257 to 294 us, 0.5 to 0.57 PFLOP/s, matrix unit 26 % busy before
+// the way of the rows from L2 and the wavefronts' ends where there are few: four prompts of up to 4099 tokens 251 to 294 us, 0.5 to 0.58 PFLOP/s (e4m3 260, four bits 262, float32 1490; 40 heads over 8, whose tokens steps of rows end in, 380), matrix unit 26 % busy before
 // rows came 32 at a time.  Rows loaded as operands, 64 addresses a load: 660 us; 96 and 128 keys a wavefront: registers spill, and every reload waits for the
 // rows on their way, 640 and 1160.
 template <int ET>

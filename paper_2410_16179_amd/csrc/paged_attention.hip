@@ -154,7 +154,7 @@ __device__ inline void finish_item(const PagedArgs& a, const PagedShare& share, 
 // the rate of a plain read; 48 ragged ones in e4m3 (491 MB) 102, 4.8 TB/s; 6 in float32 (652 MB) 113, 5.8 TB/s.  One of 98304 keys (403 MB) 75: 60
 // at that rate, the rest is what one of 2048 keys takes, 12 us: launch, the way to the first keys, the join (2 to 4 us).
 // Four bits: a wavefront takes 64 keys at once (128: 48 ragged requests of up to 30011 keys 97 | 106 us, 2048 keys 14.2 | 17.1).  16 requests of 65536 keys (1.14 GB)
-// take 190 to 200 us, 5.7 to 6.0 TB/s: widening keys and values to bf16 and pairing them are 128 and 64 of 400 vector instructions for 64 keys, and two wavefronts a SIMD
+// take 191 to 202 us, 5.6 to 6.0 TB/s (24 without a pause 193 to 242): widening keys and values to bf16 and pairing them are 128 and 64 of 400 vector instructions for 64 keys, and two wavefronts a SIMD
 // issue one in four cycles each; with a descriptor multiplied out for every 16 keys, 350 scalar ones more, 212.
 // Shares in the same launch against pieces and a second kernel (four wavefronts a workgroup): 2048 keys 14.6 -> 12.8 us, e4m3 ragged 186 -> 107.
 // 384, 512 or 768 smaller workgroups were slower.

@@ -45,7 +45,7 @@ __device__ inline void each(F&& f) {
 // 1.15 PFLOP/s with the second products (a library product of 8192^3 reaches 1.20 on this card).  At 1.82 GHz the matrix unit is busy for 58 % of
 // the cycles, the vector instructions, those of the weights above all, take 55 %, LDS 49 % (39 for reads, 10 for bringing tiles in): two
 // wavefronts a SIMD, whose products and weights overlap, leave little between them.  Four prompts of up to 4099 tokens 435 to 460 us, 635 to 670 TFLOP/s, matrix unit 49 %: the
-// starts and ends of 5.5 rounds of workgroups are not covered (tiles on the diagonal, formed whole, are 4 % of its cycles).  e4m3, widened on the way to LDS: 2.79 ms, 460 us; four bits 2.76 to 2.85 ms.
+// starts and ends of 5.5 rounds of workgroups are not covered (tiles on the diagonal, formed whole, are 4 % of its cycles).  e4m3, widened on the way to LDS: 2.79 ms, 460 us; four bits 2.76 to 3.0 ms over cards.
 // The weights are spread over the products that they wait for; worked out in the first 24 of the 32 steps: 2797 us for 2780.  With one bf16, weights
 // after the scores instead of beside the next tile's, and staging through registers, took 2364 us for 1922.
 template <int ET>
