@@ -214,7 +214,8 @@ __device__ inline float* account(const PageWeightsArgs& a, const Place& p, int g
 // ---- few rows: a wavefront has all of a request's rows of a KV head -----------------------------------
 // Scores are formed as S^T = K Q^T, so a lane has four keys of a query row (column c) in each MFMA: a weight is exp2(score - lse), no maximum and no sum have to be
 // known first, and a key's sum over the rows is one over registers and sixteen lanes.  Every key of a request belongs to one wavefront: no atomics, and the same bits
-// every time (a page that two requests name is added to by two: its accounts are not defined).  Workgroups take equal, contiguous shares of all tiles; the wavefronts of one take `heads` neighbouring KV heads, whose rows lie side by side in
+// every time (a page that two requests name is added to by two: its accounts are not defined).  The log-sum-exp is taken to base 2 in float32, which moves a row's weights by about
+// 2^-24 |lse| of themselves at most, as a rounding of lse itself would; a second term would cost an instruction for every weight.  Workgroups take equal, contiguous shares of all tiles; the wavefronts of one take `heads` neighbouring KV heads, whose rows lie side by side in
 // many pools, and waves / heads tiles at a time.  Bound by memory: 16 requests of 32768 keys, four rows (bf16, 1.11 GB) 194 us, 5.7 TB/s; 32 rows 203, 64 rows
 // 215, 128 rows 376 (their exponentials); e4m3 113 to 117, four bits 74 to 79 (4.1 to 4.3 TB/s: widening), float32, 8 requests, 182 to 184, 5.9 TB/s.  64 rows by the form for many 476, 128 rows 862 (its rows then split among wavefronts).
 template <int ET, int NR>
